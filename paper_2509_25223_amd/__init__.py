@@ -502,3 +502,12 @@ def rdn_decode(q, k, v, alpha_s, beta, alpha_r, gamma, clip: float = 1.0, S_in=N
     """RDN recurrent step (Sec. 3.4, right box); arguments as rla_decode."""
     return _decode("rdn_decode", q, k, v, alpha_s, beta, alpha_r, gamma, clip, S_in, R_in,
                    S_out, R_out, out, stream, out_dtype, variants, decay_param)
+
+
+# the operators around a mixing layer (include/rla_layer.h)
+from .layer import (  # noqa: E402,F401
+    LAYER_SYMBOLS, RLA_SSM_BACKWARD, RLA_SSM_FORWARD, make_addnorm_problem, make_conv_problem, make_gatenorm_problem,
+    make_ssm_problem, rla_addnorm_backward, rla_addnorm_forward, rla_addnorm_problem, rla_addnorm_workspace_size,
+    rla_conv_backward, rla_conv_decode, rla_conv_forward, rla_conv_problem, rla_conv_workspace_size,
+    rla_gatenorm_backward, rla_gatenorm_forward, rla_gatenorm_problem, rla_gatenorm_workspace_size, rla_ssm_backward,
+    rla_ssm_decode, rla_ssm_forward, rla_ssm_problem, rla_ssm_workspace_size)

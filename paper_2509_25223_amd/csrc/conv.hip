@@ -1,0 +1,456 @@
+// Short causal depthwise convolution of a layer's projections:
+//   pre_t = bias + sum_i weight_i x_{t-W+1+i},  y_t = pre_t or SiLU(pre_t)
+// A channel is W multiply-adds a token, so every kernel here is bound by HBM:
+// each value is read once (twice where a stretch's first rows are its
+// neighbour's last) and written once.  A thread owns the 16-byte piece of a
+// row (8 bf16 or 4 fp32 channels) and walks a stretch of tokens with the last
+// W - 1 rows in registers, so the taps cost no loads; the lanes of a wave take
+// adjacent pieces of one row.
+//
+// Rows before a sequence's start are its state's, [W-1][D] with the oldest first:
+// the row m before the start is state row W-2-m.
+#include "layer.hpp"
+
+namespace rla {
+
+namespace {
+
+// state row r of sequence n for the piece at channel c
+template <typename T, int W, int V, bool FULL>
+__device__ __forceinline__ void load_state(const void* state, int n, int r, int64_t D, int64_t c, int left,
+                                           float (&x)[V]) {
+  if (state == nullptr || n < 0) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[e] = 0.f;
+    return;
+  }
+  load_piece<T, V, FULL>(reinterpret_cast<const T*>(state) + ((int64_t)n * (W - 1) + r) * D + c, left, x);
+}
+
+// the piece's taps and bias
+template <int W, int V, bool FULL>
+__device__ __forceinline__ void load_taps(const ConvParams& p, int64_t c, int left, float (&w)[V * W], float (&b)[V]) {
+  load_piece<float, V * W, FULL>(p.weight + c * W, left * W, w);
+  if (p.bias) load_piece<float, V, FULL>(p.bias + c, left, b);
+  else
+#pragma unroll
+    for (int e = 0; e < V; ++e) b[e] = 0.f;
+}
+
+template <int W, int V>
+__device__ __forceinline__ float tap_sum(const float (&w)[V * W], float bias, int e, float x, const float (&win)[W - 1][V]) {
+  float s = bias;
+#pragma unroll
+  for (int j = W - 2; j >= 0; --j) s = __builtin_fmaf(w[e * W + W - 2 - j], win[j][e], s);
+  return __builtin_fmaf(w[e * W + W - 1], x, s);
+}
+
+// win[j] = the row before token t by j + 1, from x or the state; returns how many
+// tokens of t's sequence lie before t (W - 1 for that many or more)
+template <typename T, int W, int V, bool FULL>
+__device__ __forceinline__ int load_window(const ConvParams& p, const T* x, int64_t t, int n, int64_t c, int left,
+                                           float (&win)[W - 1][V]) {
+  int pos = 0;
+  uint32_t before = p.map.start_bits(t) & 1u;   // bit i: token t - i is a start
+  if constexpr (W > 2) {
+    const int64_t t1 = t > W - 2 ? t - (W - 2) : 0;
+    const uint32_t bits = p.map.start_bits(t1);
+#pragma unroll
+    for (int i = 1; i < W - 1; ++i) before |= (t - i < 0 ? 1u : (bits >> (t - i - t1)) & 1u) << i;
+  }
+  while (pos < W - 1 && !((before >> pos) & 1u)) ++pos;
+#pragma unroll
+  for (int j = 0; j < W - 1; ++j) {
+    if (j < pos) load_piece<T, V, FULL>(x + (t - 1 - j) * p.xs + c, left, win[j]);
+    else load_state<T, W, V, FULL>(p.state0, n, W - 2 - (j - pos), p.D, c, left, win[j]);
+  }
+  return pos;
+}
+
+template <typename T, int W, int V, bool FULL>
+__device__ __forceinline__ void load_state_window(const ConvParams& p, int n, int64_t c, int left, float (&win)[W - 1][V]) {
+#pragma unroll
+  for (int j = 0; j < W - 1; ++j) load_state<T, W, V, FULL>(p.state0, n, W - 2 - j, p.D, c, left, win[j]);
+}
+
+template <typename T, int W, int TT, bool FULL>
+__device__ __forceinline__ void conv_fwd_stretch(const ConvParams& p, int64_t t0, int64_t c, int left) {
+  constexpr int V = kPiece<T>;
+  const T* x = reinterpret_cast<const T*>(p.x);
+  T* y = reinterpret_cast<T*>(p.y);
+  T* fin = reinterpret_cast<T*>(p.state_fin);
+  float w[V * W], bias[V], win[W - 1][V];
+  load_taps<W, V, FULL>(p, c, left, w, bias);
+  const uint32_t bits = p.map.start_bits(t0);
+  int n = p.map.seq || p.state0 || fin ? p.map.seq_of(t0) : 0;
+  load_window<T, W, V, FULL>(p, x, t0, n, c, left, win);
+  auto token = [&](const float (&xv)[V], int64_t t) {
+    float o[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float s = tap_sum<W, V>(w, bias[e], e, xv[e], win);
+      o[e] = p.silu ? s * sigmoid_fast(s) : s;
+    }
+    store_piece<T, V, FULL>(y + t * p.D + c, left, o);
+#pragma unroll
+    for (int j = W - 2; j > 0; --j)
+#pragma unroll
+      for (int e = 0; e < V; ++e) win[j][e] = win[j - 1][e];
+#pragma unroll
+    for (int e = 0; e < V; ++e) win[0][e] = xv[e];
+  };
+  // no start behind the first token: one sequence, all loads ahead
+  if (t0 + TT <= p.map.ntok && (bits & (((1u << TT) - 1u) << 1)) == 0 && n >= 0) {
+    typename RowVec<T, V>::type raw[TT];
+#pragma unroll
+    for (int k = 0; k < TT; ++k) load_raw<T, V, FULL>(x + (t0 + k) * p.xs + c, left, raw[k]);
+#pragma unroll
+    for (int k = 0; k < TT; ++k) {
+      float xv[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) xv[e] = to_f<T>(raw[k][e]);
+      token(xv, t0 + k);
+    }
+    return;
+  }
+  const int count = (int)min((int64_t)TT, p.map.ntok - t0);
+  for (int k = 0; k < count; ++k) {
+    if (k > 0 && ((bits >> k) & 1u)) {
+      n = p.map.seq_of(t0 + k);
+      load_state_window<T, W, V, FULL>(p, n, c, left, win);
+    }
+    float xv[V];
+    if (n < 0) {   // outside every sequence
+#pragma unroll
+      for (int e = 0; e < V; ++e) xv[e] = 0.f;
+      store_piece<T, V, FULL>(y + (t0 + k) * p.D + c, left, xv);
+      continue;
+    }
+    load_piece<T, V, FULL>(x + (t0 + k) * p.xs + c, left, xv);
+    token(xv, t0 + k);
+    if (fin && ((bits >> (k + 1)) & 1u)) {   // the sequence's last token: the window is its state
+#pragma unroll
+      for (int j = 0; j < W - 1; ++j)
+        store_piece<T, V, FULL>(fin + ((int64_t)n * (W - 1) + W - 2 - j) * p.D + c, left, win[j]);
+    }
+  }
+}
+
+// Workgroups past `main_wgs`: the states of sequences without tokens are copied
+// (from NULL: zeros).
+template <typename T, int W>
+__device__ __forceinline__ void copy_empty_states(const ConvParams& p, const void* from, void* to, uint32_t wg,
+                                                  uint32_t wgs) {
+  const int64_t row = (W - 1) * p.D;
+  for (int64_t n = wg; n < p.map.nseq; n += wgs) {
+    if (!p.map.empty[n]) continue;
+    for (int64_t i = threadIdx.x; i < row; i += kThreads)
+      reinterpret_cast<T*>(to)[n * row + i] = from ? reinterpret_cast<const T*>(from)[n * row + i] : from_f<T>(0.f);
+  }
+}
+
+constexpr uint32_t kEmptyWgs = 32;
+
+template <typename T, int W, int TT>
+__global__ __launch_bounds__(kThreads) void conv_fwd_kernel(ConvParams p, uint32_t pieces, uint32_t count,
+                                                            uint32_t main_wgs) {
+  constexpr int V = kPiece<T>;
+  if (blockIdx.x >= main_wgs) {
+    copy_empty_states<T, W>(p, p.state0, p.state_fin, blockIdx.x - main_wgs, kEmptyWgs);
+    return;
+  }
+  const uint32_t id = blockIdx.x * kThreads + threadIdx.x;
+  if (id >= count) return;
+  const int64_t t0 = (int64_t)(id / pieces) * TT, c = (int64_t)(id % pieces) * V;
+  const int left = (int)min(p.D - c, (int64_t)V);
+  if (left == V) conv_fwd_stretch<T, W, TT, true>(p, t0, c, left);
+  else conv_fwd_stretch<T, W, TT, false>(p, t0, c, left);
+}
+
+// Single tokens: a thread owns a piece of one sequence, loads its state before it
+// writes any (in place works).
+template <typename T, int W>
+__global__ __launch_bounds__(kThreads) void conv_decode_kernel(ConvParams p, uint32_t pieces, uint32_t count) {
+  constexpr int V = kPiece<T>;
+  const uint32_t id = blockIdx.x * kThreads + threadIdx.x;
+  if (id >= count) return;
+  const int n = (int)(id / pieces);
+  const int64_t c = (int64_t)(id % pieces) * V;
+  const int left = (int)min(p.D - c, (int64_t)V);
+  float w[V * W], bias[V], win[W - 1][V];
+  load_state_window<T, W, V, false>(p, n, c, left, win);
+  load_taps<W, V, false>(p, c, left, w, bias);
+  for (int64_t k = 0; k < p.map.T; ++k) {
+    const int64_t t = n * p.map.T + k;
+    float xv[V], o[V];
+    load_piece<T, V>(reinterpret_cast<const T*>(p.x) + t * p.xs + c, left, xv);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float s = tap_sum<W, V>(w, bias[e], e, xv[e], win);
+      o[e] = p.silu ? s * sigmoid_fast(s) : s;
+    }
+    store_piece<T, V>(reinterpret_cast<T*>(p.y) + t * p.D + c, left, o);
+#pragma unroll
+    for (int j = W - 2; j > 0; --j)
+#pragma unroll
+      for (int e = 0; e < V; ++e) win[j][e] = win[j - 1][e];
+#pragma unroll
+    for (int e = 0; e < V; ++e) win[0][e] = xv[e];
+  }
+  T* fin = reinterpret_cast<T*>(p.state_fin);
+#pragma unroll
+  for (int j = 0; j < W - 1; ++j) store_piece<T, V>(fin + ((int64_t)n * (W - 1) + W - 2 - j) * p.D + c, left, win[j]);
+}
+
+// ---------------------------------------------------------------------------
+// Backward.  dpre_t = dy_t (SiLU'(pre_t)); the row u steps before t gets
+// weight_{W-1-u} dpre_t.  A thread walks its stretch and the W - 1 tokens behind
+// it, with the last W - 1 rows and their gradients so far in registers: a row's
+// gradient is complete W - 1 tokens later, or where its sequence ends, and is
+// written once.  dweight and dbias are summed over the stretch in registers,
+// over the workgroup's stretches in LDS, and over the workgroups by
+// launch_column_sums.
+// ---------------------------------------------------------------------------
+constexpr int kBwdTokens = 32;
+
+template <typename T, int W, bool FULL>
+__device__ __forceinline__ void conv_bwd_stretch(const ConvParams& p, int64_t t0, int64_t c, int left,
+                                                 float (&dw)[kPiece<T> * W], float (&db)[kPiece<T>]) {
+  constexpr int V = kPiece<T>, TT = kBwdTokens;
+  const T* x = reinterpret_cast<const T*>(p.x);
+  const T* dy = reinterpret_cast<const T*>(p.dy);
+  T* dx = reinterpret_cast<T*>(p.dx);
+  const T* dfin = reinterpret_cast<const T*>(p.dstate_fin);
+  T* dst0 = reinterpret_cast<T*>(p.dstate0);
+  float w[V * W], bias[V], win[W - 1][V], g[W - 1][V];
+  load_taps<W, V, FULL>(p, c, left, w, bias);
+  int n = p.map.seq_of(t0);
+  const int pos0 = load_window<T, W, V, FULL>(p, x, t0, n, c, left, win);
+#pragma unroll
+  for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+    for (int e = 0; e < V; ++e) g[j][e] = 0.f;
+
+  // one token: its gradient into the rows of the window, g[W-2] then complete
+  auto token = [&](const float (&xv)[V], const float (&dyv)[V], bool own, float (&done)[V]) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      float d = dyv[e], act;
+      if (p.silu) d *= silu_grad_f(tap_sum<W, V>(w, bias[e], e, xv[e], win), act);
+      if (own) {
+        db[e] += d;
+        dw[e * W + W - 1] = __builtin_fmaf(d, xv[e], dw[e * W + W - 1]);
+      }
+#pragma unroll
+      for (int j = 0; j < W - 1; ++j) {
+        if (own) dw[e * W + W - 2 - j] = __builtin_fmaf(d, win[j][e], dw[e * W + W - 2 - j]);
+        g[j][e] = __builtin_fmaf(w[e * W + W - 2 - j], d, g[j][e]);
+      }
+      done[e] = g[W - 2][e];
+#pragma unroll
+      for (int j = W - 2; j > 0; --j) {
+        win[j][e] = win[j - 1][e];
+        g[j][e] = g[j - 1][e];
+      }
+      win[0][e] = xv[e];
+      g[0][e] = w[e * W + W - 1] * d;
+    }
+  };
+
+  const uint64_t bits = (uint64_t)p.map.start_bits(t0) |
+                        (t0 + 32 < p.map.ntok ? (uint64_t)p.map.start_bits(t0 + 32) << 32 : ~0ull << 32);
+  if (t0 + TT + W - 1 <= p.map.ntok && (bits & (((1ull << (TT + W - 2)) - 1ull) << 1)) == 0 &&
+      !((bits & 1ull) && dst0) && n >= 0) {
+    constexpr int U = 5;   // tokens loaded ahead (35 = 7 x 5 for four taps)
+    typename RowVec<T, V>::type rx[U], ry[U];
+    float xv[V], dyv[V], done[V];
+    for (int k0 = 0; k0 < TT + W - 1; k0 += U) {
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const int64_t t = t0 + min(k0 + k, TT + W - 2);
+        load_raw<T, V, FULL>(x + t * p.xs + c, left, rx[k]);
+        load_raw<T, V, FULL>(dy + t * p.dys + c, left, ry[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        if (k0 + k >= TT + W - 1) break;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          xv[e] = to_f<T>(rx[k][e]);
+          dyv[e] = to_f<T>(ry[k][e]);
+        }
+        token(xv, dyv, k0 + k < TT, done);
+        if (k0 + k >= W - 1) store_piece<T, V, FULL>(dx + (t0 + k0 + k - (W - 1)) * p.D + c, left, done);
+      }
+    }
+    return;
+  }
+
+  // any starts: `start` is the current sequence's first token (further back than the
+  // window: as good as anywhere there)
+  int64_t start = pos0 < W - 1 ? t0 - pos0 : t0 - 64;
+  const int64_t own_end = min(t0 + TT, p.map.ntok);
+  // gradient of the row `back` + 1 tokens before t (a token of the sequence, or a row of
+  // its state), if this thread's to write; at the sequence's end its final state's too
+  auto emit = [&](int64_t t, int back, float (&v)[V], bool end) {
+    const int64_t at = t - 1 - back;
+    if (end && dfin && n >= 0) {
+      float f[V];
+      load_piece<T, V, FULL>(dfin + ((int64_t)n * (W - 1) + W - 2 - back) * p.D + c, left, f);
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[e] += f[e];
+    }
+    if (at >= start) {
+      if (at >= t0 && at < own_end) store_piece<T, V, FULL>(dx + at * p.D + c, left, v);
+    } else if (dst0 && n >= 0 && start >= t0 && start < own_end) {
+      const int64_t r = W - 1 - (start - at);   // the row start - at before the start
+      store_piece<T, V, FULL>(dst0 + ((int64_t)n * (W - 1) + r) * p.D + c, left, v);
+    }
+  };
+  for (int k = 0; k <= TT + W - 2; ++k) {
+    const int64_t t = t0 + k;
+    if (k > 0 && ((bits >> k) & 1ull)) {   // the sequence ended before t (or all tokens did)
+#pragma unroll
+      for (int j = 0; j < W - 1; ++j) emit(t, j, g[j], true);
+      if (t >= own_end) return;
+      n = p.map.seq_of(t);
+      start = t;
+      load_state_window<T, W, V, FULL>(p, n, c, left, win);
+#pragma unroll
+      for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+        for (int e = 0; e < V; ++e) g[j][e] = 0.f;
+    }
+    float xv[V], dyv[V], done[V];
+    if (n >= 0) {
+      load_piece<T, V, FULL>(x + t * p.xs + c, left, xv);
+      load_piece<T, V, FULL>(dy + t * p.dys + c, left, dyv);
+      token(xv, dyv, k < TT, done);
+      emit(t + 1, W - 1, done, false);   // the row W - 1 before t
+    } else if (k < TT) {   // outside every sequence
+#pragma unroll
+      for (int e = 0; e < V; ++e) xv[e] = 0.f;
+      store_piece<T, V, FULL>(dx + t * p.D + c, left, xv);
+    }
+  }
+}
+
+// lanes: adjacent pieces (kLanes of them), then stretches
+template <typename T, int W>
+__global__ __launch_bounds__(kThreads) void conv_bwd_kernel(ConvParams p, uint32_t lanes, uint32_t groups,
+                                                            uint32_t main_wgs) {
+  constexpr int V = kPiece<T>;
+  if (blockIdx.x >= main_wgs) {
+    copy_empty_states<T, W>(p, p.dstate_fin, p.dstate0, blockIdx.x - main_wgs, kEmptyWgs);
+    return;
+  }
+  __shared__ float sums[kThreads][V * (W + 1) + 1];
+  const uint32_t row = blockIdx.x / groups, lane = threadIdx.x % lanes, sub = threadIdx.x / lanes, subs = kThreads / lanes;
+  const int64_t c = ((int64_t)(blockIdx.x % groups) * lanes + lane) * V;
+  const int64_t t0 = ((int64_t)row * subs + sub) * kBwdTokens;
+  const int left = (int)min(max(p.D - c, (int64_t)0), (int64_t)V);
+  float dw[V * W], db[V];
+#pragma unroll
+  for (int e = 0; e < V * W; ++e) dw[e] = 0.f;
+#pragma unroll
+  for (int e = 0; e < V; ++e) db[e] = 0.f;
+  if (left > 0 && t0 < p.map.ntok) {
+    if (left == V) conv_bwd_stretch<T, W, true>(p, t0, c, left, dw, db);
+    else conv_bwd_stretch<T, W, false>(p, t0, c, left, dw, db);
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) sums[threadIdx.x][i * V + e] = dw[e * W + i];
+    sums[threadIdx.x][W * V + e] = db[e];
+  }
+  __syncthreads();
+  // (tap, channel) of the workgroup's channels, over its stretches in order
+  const int width = (int)lanes * V;
+  for (int o = threadIdx.x; o < width * (W + 1); o += kThreads) {
+    const int i = o / width, cc = o % width;
+    const int64_t ch = (int64_t)(blockIdx.x % groups) * width + cc;
+    if (ch >= p.D) continue;
+    float s = 0.f;
+    for (uint32_t q = 0; q < subs; ++q) s += sums[q * lanes + cc / V][i * V + cc % V];
+    p.part[((int64_t)row * (W + 1) + i) * p.D + ch] = s;
+  }
+}
+
+struct BwdGrid {
+  uint32_t lanes, groups;
+  int64_t rows;
+};
+BwdGrid bwd_grid(int64_t ntok, int64_t D, bool bf16) {
+  const int64_t V = bf16 ? 8 : 4, pieces = (D + V - 1) / V;
+  uint32_t lanes = 1;
+  while (lanes < 64 && lanes < pieces) lanes *= 2;
+  const int64_t per = (int64_t)(kThreads / lanes) * kBwdTokens;
+  return BwdGrid{lanes, (uint32_t)((pieces + lanes - 1) / lanes), (ntok + per - 1) / per};
+}
+
+// stretches of 16 tokens, or of 4 where those would leave most of the card idle
+constexpr int64_t kFillThreads = 256 * 4 * 64 * 2;
+
+template <typename T, int W> hipError_t forward(const ConvParams& p, hipStream_t stream) {
+  constexpr int V = kPiece<T>;
+  const int64_t pieces = (p.D + V - 1) / V;
+  const bool small = (p.map.ntok + 15) / 16 * pieces < kFillThreads;
+  const int64_t tiles = small ? (p.map.ntok + 3) / 4 : (p.map.ntok + 15) / 16;
+  const int64_t count = tiles * pieces;
+  if (count > UINT32_MAX - kThreads * (kEmptyWgs + 1)) return hipErrorInvalidValue;
+  const uint32_t wgs = (uint32_t)((count + kThreads - 1) / kThreads);
+  const uint32_t extra = p.map.seq && p.state_fin ? kEmptyWgs : 0;
+  if (small)
+    hipLaunchKernelGGL((conv_fwd_kernel<T, W, 4>), dim3(wgs + extra), dim3(kThreads), 0, stream, p, (uint32_t)pieces,
+                       (uint32_t)count, wgs);
+  else
+    hipLaunchKernelGGL((conv_fwd_kernel<T, W, 16>), dim3(wgs + extra), dim3(kThreads), 0, stream, p, (uint32_t)pieces,
+                       (uint32_t)count, wgs);
+  return hipGetLastError();
+}
+
+template <typename T, int W> hipError_t decode(const ConvParams& p, hipStream_t stream) {
+  const int64_t pieces = (p.D + kPiece<T> - 1) / kPiece<T>, count = pieces * p.map.nseq;
+  if (count > UINT32_MAX - kThreads) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((conv_decode_kernel<T, W>), dim3((uint32_t)((count + kThreads - 1) / kThreads)), dim3(kThreads), 0,
+                     stream, p, (uint32_t)pieces, (uint32_t)count);
+  return hipGetLastError();
+}
+
+template <typename T, int W> hipError_t backward(const ConvParams& p, hipStream_t stream) {
+  const BwdGrid g = bwd_grid(p.map.ntok, p.D, sizeof(T) == 2);
+  const int64_t wgs = g.rows * g.groups;
+  if (wgs > INT32_MAX) return hipErrorInvalidValue;
+  const uint32_t extra = p.map.seq && p.dstate0 ? kEmptyWgs : 0;
+  hipLaunchKernelGGL((conv_bwd_kernel<T, W>), dim3((uint32_t)wgs + extra), dim3(kThreads), 0, stream, p, g.lanes,
+                     g.groups, (uint32_t)wgs);
+  return hipGetLastError();
+}
+
+#define RLA_CONV_DISPATCH(fn)                                                          \
+  if (bf16)                                                                            \
+    return p.taps == 2 ? fn<u16, 2>(p, stream) : p.taps == 3 ? fn<u16, 3>(p, stream)   \
+                                                             : fn<u16, 4>(p, stream);  \
+  return p.taps == 2 ? fn<float, 2>(p, stream) : p.taps == 3 ? fn<float, 3>(p, stream) \
+                                                             : fn<float, 4>(p, stream)
+
+hipError_t dispatch_backward(const ConvParams& p, bool bf16, hipStream_t stream) { RLA_CONV_DISPATCH(backward); }
+
+}  // namespace
+
+hipError_t launch_conv_forward(const ConvParams& p, bool bf16, hipStream_t stream) { RLA_CONV_DISPATCH(forward); }
+hipError_t launch_conv_decode(const ConvParams& p, bool bf16, hipStream_t stream) { RLA_CONV_DISPATCH(decode); }
+
+int64_t conv_backward_rows(int64_t ntok, int64_t D, bool bf16) { return bwd_grid(ntok, D, bf16).rows; }
+
+hipError_t launch_conv_backward(const ConvParams& p, bool bf16, float* dweight, float* dbias, hipStream_t stream) {
+  if (p.map.ntok > 0) {
+    const hipError_t e = dispatch_backward(p, bf16, stream);
+    if (e != hipSuccess) return e;
+  }
+  return launch_column_sums(p.part, conv_backward_rows(p.map.ntok, p.D, bf16), (int64_t)(p.taps + 1) * p.D, p.D, p.taps,
+                            dweight, dbias, stream);
+}
+
+}  // namespace rla

@@ -1,0 +1,175 @@
+// Shared by the operators around a mixing layer (conv.hip, ssm*.hip,
+// norm.hip) and their host side (layer_api.cpp): rows of any alignment, the
+// map from tokens to sequences, launch parameters.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "common.hpp"
+
+namespace rla {
+
+// ---------------------------------------------------------------------------
+// Rows.  V values of a row starting at p, of which n exist.  Activations are
+// aligned to their elements only (odd channel counts, slices of projections):
+// gfx950 loads 16 bytes from any address, so a whole piece is one access, and
+// only a row's last piece is read value by value.
+// ---------------------------------------------------------------------------
+template <typename T, int V> struct RowVec {
+  typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+};
+// (as stored: what is loaded ahead is converted where it is used)
+template <typename T, int V, bool FULL = false>
+__device__ __forceinline__ void load_raw(const T* p, int n, typename RowVec<T, V>::type& x) {
+  if (FULL || n >= V) {
+    x = *reinterpret_cast<const typename RowVec<T, V>::type*>(p);
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[e] = e < n ? p[e] : from_f<T>(0.f);
+  }
+}
+template <typename T, int V, bool FULL = false>
+__device__ __forceinline__ void load_piece(const T* p, int n, float (&x)[V]) {
+  if (FULL || n >= V) {
+    const typename RowVec<T, V>::type v = *reinterpret_cast<const typename RowVec<T, V>::type*>(p);
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[e] = to_f<T>(v[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[e] = e < n ? to_f<T>(p[e]) : 0.f;
+  }
+}
+template <typename T, int V, bool FULL = false>
+__device__ __forceinline__ void store_piece(T* p, int n, const float (&x)[V]) {
+  if (FULL || n >= V) {
+    typename RowVec<T, V>::type v;
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = from_f<T>(x[e]);
+    *reinterpret_cast<typename RowVec<T, V>::type*>(p) = v;
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (e < n) p[e] = from_f<T>(x[e]);
+  }
+}
+// values of a 16-byte piece
+template <typename T> constexpr int kPiece = 16 / (int)sizeof(T);
+
+// 1 / (1 + e^-z), the reciprocal by v_rcp_f32 (1 ulp; a rounded division is ten
+// instructions)
+__device__ __forceinline__ float sigmoid_fast(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
+// SiLU'(z), and SiLU(z)
+__device__ __forceinline__ float silu_grad_f(float z, float& silu) {
+  const float s = sigmoid_fast(z);
+  silu = z * s;
+  return s * __builtin_fmaf(z, 1.f - s, 1.f);
+}
+
+// ---------------------------------------------------------------------------
+// Tokens and sequences.  Dense: sequence t / T.  Packed: a map built per call
+// in the workspace (launch_token_map): seq[t], -1 outside every sequence;
+// starts: bit t set where token t's sequence is not token t - 1's (and for t =
+// 0), bits past the end set; empty[n]: sequence n has no token.
+// ---------------------------------------------------------------------------
+struct TokenMap {
+  int64_t ntok = 0, T = 1;           // dense: tokens per sequence (packed: unused)
+  int32_t nseq = 0;
+  const int32_t* seq = nullptr;      // packed
+  const uint32_t* starts = nullptr;
+  const int32_t* empty = nullptr;
+
+  __device__ __forceinline__ int seq_of(int64_t t) const {
+    return seq ? seq[t] : (int)((uint32_t)t / (uint32_t)T);
+  }
+  // start bits of tokens t .. t + 31
+  __device__ __forceinline__ uint32_t start_bits(int64_t t) const {
+    if (seq) {
+      const uint32_t w = (uint32_t)t >> 5, s = (uint32_t)t & 31u;
+      const uint64_t two = (uint64_t)starts[w] | ((uint64_t)starts[w + 1] << 32);
+      return (uint32_t)(two >> s);
+    }
+    const uint32_t r = (uint32_t)t % (uint32_t)T;
+    uint32_t bits = 0;
+    for (int64_t i = r == 0 ? 0 : T - r; i < 32; i += T) bits |= 1u << i;
+    const int64_t left = ntok - t;
+    return left >= 32 ? bits : bits | (~0u << (left < 0 ? 0 : left));
+  }
+};
+inline size_t token_map_bytes(int64_t ntok, int64_t nseq) {
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  return up(4 * (size_t)ntok) + up(4 * ((size_t)ntok / 32 + 3)) + up(4 * (size_t)nseq);
+}
+// Points `map` (packed) at its arrays in ws; `build`: launches what fills them.
+hipError_t launch_token_map(const int32_t* cu, int32_t nseq, int64_t ntok, unsigned char* ws, bool build,
+                            TokenMap& map, hipStream_t stream);
+
+// ---------------------------------------------------------------------------
+// Sums over the rows of part [rows][cols]: the last step of every gradient of
+// a shared parameter (fixed order).  Column i * inner + j goes to out[j * outer
+// + i] for i < outer, else to out2[j] (NULL: dropped).
+// ---------------------------------------------------------------------------
+hipError_t launch_column_sums(const float* part, int64_t rows, int64_t cols, int64_t inner, int32_t outer, float* out,
+                              float* out2, hipStream_t stream);
+
+struct ConvParams {
+  TokenMap map;
+  int64_t D = 0, xs = 0, dys = 0;
+  int32_t taps = 4, silu = 0;
+  const void* x = nullptr;
+  const float* weight = nullptr;
+  const float* bias = nullptr;
+  const void* state0 = nullptr;
+  void* y = nullptr;
+  void* state_fin = nullptr;
+  const void* dy = nullptr;
+  const void* dstate_fin = nullptr;
+  void* dx = nullptr;
+  void* dstate0 = nullptr;
+  float* part = nullptr;   // [tiles][taps + 1][D] sums of dweight, dbias
+};
+hipError_t launch_conv_forward(const ConvParams& p, bool bf16, hipStream_t stream);
+hipError_t launch_conv_decode(const ConvParams& p, bool bf16, hipStream_t stream);
+int64_t conv_backward_rows(int64_t ntok, int64_t D, bool bf16);
+hipError_t launch_conv_backward(const ConvParams& p, bool bf16, float* dweight, float* dbias, hipStream_t stream);
+
+// dst = src (NULL: zeros), `n` 16-bit words
+hipError_t launch_copy_words(const void* src, void* dst, int64_t n, hipStream_t stream);
+
+struct AddNormParams {
+  int64_t rows = 0, width = 0, xs = 0, dns = 0, wgs = 0;
+  float eps = 0.f;
+  const void* x = nullptr;
+  const void* residual = nullptr;
+  const float* weight = nullptr;
+  const float* scale = nullptr;
+  void* n = nullptr;
+  void* residual_out = nullptr;
+  const void* residual_in = nullptr;   // backward: the forward's residual_out
+  const void* dn = nullptr;
+  const void* dresidual_out = nullptr;
+  void* dx = nullptr;
+  void* dresidual = nullptr;
+  float* part = nullptr;               // [wgs][1, or 2 with scale][width]
+};
+int64_t addnorm_backward_wgs(int64_t rows, int64_t width, bool bf16);
+hipError_t launch_addnorm(const AddNormParams& p, bool bf16, bool res_bf16, bool backward, hipStream_t stream);
+
+struct GateNormParams {
+  int64_t rows = 0, heads = 1, width = 0, xs = 0, gs = 0, dos = 0, wstride = 0, groups = 0;
+  float eps = 0.f;
+  int32_t first = 0;
+  const void* x = nullptr;
+  const void* gate = nullptr;
+  const float* weight = nullptr;
+  void* o = nullptr;
+  const void* dO = nullptr;
+  void* dx = nullptr;
+  void* dgate = nullptr;
+  float* part = nullptr;
+};
+// Groups of lanes in the backward, and the rows of its partial sums.
+int64_t gatenorm_backward_groups(int64_t rows, int64_t heads, int64_t width, bool bf16, int64_t& part_rows, bool per_head);
+hipError_t launch_gatenorm(const GateNormParams& p, bool bf16, bool x_bf16, bool backward, hipStream_t stream);
+
+}  // namespace rla

@@ -1,0 +1,322 @@
+// Selective scan, forward and single tokens (layout of the work: ssm.hpp).
+//
+//   s_t = softplus(delta_t + bias);  h_t = exp(s_t A) h_{t-1} + s_t u_t B_t
+//   o_t = (C_t . h_t + skip u_t) z_t sigmoid(z_t)
+//
+// What bounds it is the vector ALU: 16 states are 16 (product, exponential, product,
+// two multiply-adds) a token and channel, against 8 bytes of bf16 activations.
+// Everything that is once per (token, channel) is kept out of the lanes that hold
+// states: a tile of 32 tokens is staged by threads that own (token, piece of
+// channels), which form the steps and s u for it and, after the scan, add the
+// skip, gate and store.  exp(s A) is v_exp_f32 of s (A log2 e).
+#include "ssm.hpp"
+
+namespace rla {
+
+namespace {
+
+// The thread's own (token, piece), as loaded, of a tile of TT tokens x kCB channels.
+template <typename T, typename SL, int TT> struct SsmTileIo {
+  static constexpr int V = TT * SL::kCB / kThreads;      // channels a thread
+  static constexpr int kPer = SL::kCB / V;               // threads a token
+  static constexpr int VB = TT * SL::NP / kThreads ? TT * SL::NP / kThreads : 1;   // values of B, C
+  static constexpr int kPerB = SL::NP / VB;
+  typename RowVec<T, V>::type u, d, z;
+  typename RowVec<T, VB>::type b, c;
+  bool in;   // the token exists and belongs to a sequence
+};
+
+template <typename T, typename SL, bool SUMMARY>
+__global__ __launch_bounds__(kThreads) void ssm_fwd_kernel(SsmParams p) {
+  constexpr int NS = SL::NS, LPC = SL::LPC, NP = SL::NP, kRow = SL::kRow, TT = kSsmTile;
+  typedef SsmTileIo<T, SL, TT> Io;
+  constexpr int V = Io::V, VB = Io::VB;
+  __shared__ __attribute__((aligned(16))) float sD[TT][kRow], sX[TT][kRow], sY[SUMMARY ? 1 : TT][kRow];
+  __shared__ __attribute__((aligned(16))) float sB[TT][NP], sC[SUMMARY ? 1 : TT][NP];
+
+  const int tid = threadIdx.x;
+  const int nblk = (int)p.G * p.bpg, chunk = (int)blockIdx.x / nblk, blk = (int)blockIdx.x - chunk * nblk;
+  const int g = blk / p.bpg;
+  const int64_t c0 = g * p.Dg + (int64_t)(blk - g * p.bpg) * SL::kCB;   // first channel
+  const int nc = (int)min((int64_t)SL::kCB, (g + 1) * p.Dg - c0);
+  int64_t t0;
+  int len;
+  chunk_range(p, chunk, t0, len);
+  int last, first;
+  chunk_starts(p, t0, len, last, first);
+  if constexpr (SUMMARY) {
+    if (blk == 0 && tid == 0) p.flags[chunk] = (last >= 0 ? kHasStart : 0) | (first <= len ? kClosed : 0);
+    if (first == len || (p.map.seq && t0 + len >= p.map.ntok)) return;   // nothing continues behind it
+    if (p.map.seq && first < len && p.map.start_bits(t0 + len) & 1u) return;
+  }
+
+  // the lane's channel and states
+  const int q = SL::q(), ch = SL::ch(), n0 = q * NS;
+  const bool live = ch < nc;
+  const int64_t c = c0 + (live ? ch : 0);
+  const int nleft = (int)p.N - n0;
+  float A2[NS], h[NS];
+  load_states<NS>(p.A + c * p.N + n0, nleft, A2);
+#pragma unroll
+  for (int n = 0; n < NS; ++n) A2[n] *= kLog2e;
+  auto start_state = [&](int seq) {
+    if (p.h0 && seq >= 0) load_states<NS>(p.h0 + ((int64_t)seq * p.D + c) * p.N + n0, nleft, h);
+    else
+#pragma unroll
+      for (int n = 0; n < NS; ++n) h[n] = 0.f;
+  };
+  auto end_state = [&](int seq) {
+    if (p.hfin && seq >= 0 && live) store_piece<float, NS>(p.hfin + ((int64_t)seq * p.D + c) * p.N + n0, nleft, h);
+  };
+
+  // the thread's token and channels in a tile
+  const int r = tid / Io::kPer, pc = tid % Io::kPer * V, pleft = nc - pc;
+  const int rb = tid / Io::kPerB, pb = tid % Io::kPerB * VB, bleft = (int)p.N - pb;
+  const T* ug = reinterpret_cast<const T*>(p.u) + c0 + pc;
+  const T* dg = reinterpret_cast<const T*>(p.delta) + c0 + pc;
+  const T* zg = reinterpret_cast<const T*>(p.z) + c0 + pc;
+  const T* bg = reinterpret_cast<const T*>(p.B) + g * p.N + pb;
+  const T* cg = reinterpret_cast<const T*>(p.C) + g * p.N + pb;
+  float bias[V], skip[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    bias[e] = p.dbias && e < pleft ? p.dbias[c0 + pc + e] : 0.f;
+    skip[e] = p.skip && e < pleft ? p.skip[c0 + pc + e] : 0.f;
+  }
+  auto load_tile = [&](int k, Io& io) {
+    const int64_t t = t0 + k + r, tb = t0 + k + rb;
+    io.in = k + r < len && (!p.map.seq || p.map.seq[t] >= 0);
+    if (k + r < len) {
+      load_raw<T, V>(ug + t * p.us, pleft, io.u);
+      load_raw<T, V>(dg + t * p.dts, pleft, io.d);
+      if (!SUMMARY && p.z) load_raw<T, V>(zg + t * p.zs, pleft, io.z);
+    }
+    if (rb < TT && k + rb < len) {
+      load_raw<T, VB>(bg + tb * p.bs, bleft, io.b);
+      if (!SUMMARY) load_raw<T, VB>(cg + tb * p.cs, bleft, io.c);
+    }
+  };
+
+  // tiles from the one of the last start on (summary), or all
+  const int k_first = SUMMARY && last > 0 ? last / TT * TT : 0;
+  int seq = p.map.seq || p.h0 || p.hfin ? p.map.seq_of(t0) : 0;
+  if (SUMMARY) {
+    if (last >= 0) seq = p.map.seq_of(t0 + last);
+    start_state(last >= 0 ? seq : -1);
+  } else if (last >= 0 && p.map.start_bits(t0) & 1u) {
+    start_state(seq);
+  } else {   // the chunks before, from the last one with a start on
+    int cc = chunk - 1;
+    while (!(p.flags[cc] & kHasStart)) --cc;
+    load_states<NS>(p.S + ((int64_t)cc * p.D + c) * NP + n0, NS, h);
+    for (++cc; cc < chunk; ++cc) {
+      float s[NS];
+      load_states<NS>(p.S + ((int64_t)cc * p.D + c) * NP + n0, NS, s);
+      const float sum = p.sumd[(int64_t)cc * p.D + c];
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        // (a state that is zero stays so: no infinity times it where A is positive)
+        const float carried = h[n] == 0.f ? 0.f : __builtin_amdgcn_exp2f(sum * A2[n]) * h[n];
+        h[n] = carried + s[n];
+      }
+    }
+  }
+  float total = 0.f;   // sum of the channel's steps (lanes q = 0)
+
+  Io cur;
+  load_tile(k_first, cur);
+  for (int k = k_first; k < len; k += TT) {
+    // ---- this tile into LDS ----
+    const bool in = cur.in;
+    const typename RowVec<T, V>::type uu = cur.u, zz = cur.z;
+    {
+      float s[V], x[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float raw = to_f<T>(cur.d[e]) + bias[e];
+        const bool use = in && e < pleft && (!SUMMARY || k + r >= last);
+        s[e] = use ? (p.softplus ? softplus_exact(raw) : raw) : 0.f;
+        x[e] = use ? s[e] * to_f<T>(cur.u[e]) : 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        sD[r][pc + e] = s[e];
+        sX[r][pc + e] = x[e];
+      }
+      if (rb < TT) {
+        const bool inb = k + rb < len && (!p.map.seq || p.map.seq[t0 + k + rb] >= 0) && (!SUMMARY || k + rb >= last);
+#pragma unroll
+        for (int e = 0; e < VB; ++e) {
+          sB[rb][pb + e] = inb && e < bleft ? to_f<T>(cur.b[e]) : 0.f;
+          if (!SUMMARY) sC[rb][pb + e] = inb && e < bleft ? to_f<T>(cur.c[e]) : 0.f;
+        }
+      }
+    }
+    __syncthreads();
+    if (k + TT < len) load_tile(k + TT, cur);
+
+    // ---- the scan ----
+    const uint32_t valid = len - k >= TT ? ~0u : (1u << (len - k)) - 1u;
+    uint32_t bits = SUMMARY ? 0u : p.map.start_bits(t0 + k) & valid;
+    if (k == 0) bits &= ~1u;   // the chunk's first token: its state is set
+#pragma unroll 1
+    for (int i = 0; i < TT; i += 4) {
+      if (!SUMMARY && p.ck && (i & (kSsmSub - 1)) == 0 && k + i < len && live) {
+        const int64_t sub = (int64_t)chunk * (p.L / kSsmSub) + (k + i) / kSsmSub;
+        store_piece<float, NS, true>(p.ck + (sub * p.D + c) * NP + n0, NS, h);
+      }
+      const float dv = sD[i + (q & 3)][ch], xv = sX[i + (q & 3)][ch];
+      float y[4];
+      if (SUMMARY) total += dv;
+      const uint32_t here = (bits >> i) & 15u;
+      auto token = [&](auto J) {
+        constexpr int j = decltype(J)::value;
+        if (!SUMMARY && here != 0 && (here >> j) & 1u) {
+          if (!(k == 0 && i + j == 0)) end_state(seq);
+          seq = p.map.seq_of(t0 + k + i + j);
+          start_state(seq);
+        }
+        const float dj = quad_lane<j>(dv), xj = quad_lane<j>(xv);
+        float b[NS], cc[NS], acc = 0.f;
+#pragma unroll
+        for (int n = 0; n < NS; ++n) b[n] = sB[i + j][n0 + n];
+        if (!SUMMARY)
+#pragma unroll
+          for (int n = 0; n < NS; ++n) cc[n] = sC[i + j][n0 + n];
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+          h[n] = __builtin_fmaf(__builtin_amdgcn_exp2f(dj * A2[n]), h[n], xj * b[n]);
+          if (!SUMMARY) acc = __builtin_fmaf(h[n], cc[n], acc);
+        }
+        y[j] = acc;
+      };
+      token(std::integral_constant<int, 0>());
+      token(std::integral_constant<int, 1>());
+      token(std::integral_constant<int, 2>());
+      token(std::integral_constant<int, 3>());
+      if (!SUMMARY) {
+        const float yt = tokens_over_lanes<LPC>(y);
+        if (q < 4) sY[i + q][ch] = yt;
+      }
+    }
+    __syncthreads();
+
+    // ---- skip, gate, store ----
+    if (!SUMMARY && p.o && k + r < len) {   // (no outputs: the backward's recomputation)
+      float y[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        y[e] = __builtin_fmaf(skip[e], to_f<T>(uu[e]), sY[r][pc + e]);
+        if (p.z) {
+          const float zf = to_f<T>(zz[e]);
+          y[e] *= zf * sigmoid_fast(zf);
+        }
+        if (!in) y[e] = 0.f;
+      }
+      store_piece<T, V>(reinterpret_cast<T*>(p.o) + (t0 + k + r) * p.D + c0 + pc, pleft, y);
+    }
+  }
+  if constexpr (SUMMARY) {
+    if (!live) return;
+    store_piece<float, NS, true>(p.S + ((int64_t)chunk * p.D + c) * NP + n0, NS, h);
+    total = group_sum<4>(total);   // the quad's lanes took a token of four each
+    if (q == 0) p.sumd[(int64_t)chunk * p.D + c] = total;
+  } else {
+    // the last sequence ends with the chunk
+    if (p.map.seq ? t0 + len >= p.map.ntok || (p.map.start_bits(t0 + len) & 1u) : (t0 + len) % p.map.T == 0)
+      end_state(seq);
+  }
+}
+
+// final (or, in the backward, initial) states of sequences without tokens
+__global__ __launch_bounds__(kThreads) void ssm_empty_kernel(const int32_t* empty, int32_t nseq, int64_t row,
+                                                             const float* from, float* to) {
+  for (int64_t n = blockIdx.x; n < nseq; n += gridDim.x) {
+    if (!empty[n]) continue;
+    for (int64_t i = threadIdx.x; i < row; i += kThreads) to[n * row + i] = from ? from[n * row + i] : 0.f;
+  }
+}
+
+// Single tokens.  A lane holds NS states of a channel through the call's tokens: the
+// states are read and written once, which is what the call costs (HBM).
+template <typename T, typename SL>
+__global__ __launch_bounds__(kThreads) void ssm_decode_kernel(SsmParams p) {
+  constexpr int NS = SL::NS, LPC = SL::LPC;
+  const int q = SL::q(), n0 = q * NS;
+  const int64_t id = (int64_t)blockIdx.x * SL::kCB + SL::ch();   // (sequence, channel)
+  if (id >= p.map.nseq * p.D) return;   // whole channels of lanes
+  const int64_t s = id / p.D, c = id - s * p.D, g = c / p.Dg;
+  const int nleft = (int)p.N - n0;
+  float A2[NS], h[NS];
+  if (p.h0) load_states<NS>(p.h0 + id * p.N + n0, nleft, h);
+  else
+#pragma unroll
+    for (int n = 0; n < NS; ++n) h[n] = 0.f;
+  load_states<NS>(p.A + c * p.N + n0, nleft, A2);
+#pragma unroll
+  for (int n = 0; n < NS; ++n) A2[n] *= kLog2e;
+  const float bias = p.dbias ? p.dbias[c] : 0.f, skip = p.skip ? p.skip[c] : 0.f;
+  for (int64_t k = 0; k < p.map.T; ++k) {
+    const int64_t t = s * p.map.T + k;
+    const float u = to_f<T>(reinterpret_cast<const T*>(p.u)[t * p.us + c]);
+    const float raw = to_f<T>(reinterpret_cast<const T*>(p.delta)[t * p.dts + c]) + bias;
+    const float z = p.z ? to_f<T>(reinterpret_cast<const T*>(p.z)[t * p.zs + c]) : 0.f;
+    float b[NS], cc[NS], y = 0.f;
+    load_piece<T, NS>(reinterpret_cast<const T*>(p.B) + t * p.bs + g * p.N + n0, nleft, b);
+    load_piece<T, NS>(reinterpret_cast<const T*>(p.C) + t * p.cs + g * p.N + n0, nleft, cc);
+    const float step = p.softplus ? softplus_exact(raw) : raw, x = step * u;
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+      h[n] = __builtin_fmaf(__builtin_amdgcn_exp2f(step * A2[n]), h[n], x * b[n]);
+      y = __builtin_fmaf(h[n], cc[n], y);
+    }
+    y = group_sum<LPC>(y);
+    y = __builtin_fmaf(skip, u, y);
+    if (p.z) y *= z * sigmoid_fast(z);
+    if (q == 0) reinterpret_cast<T*>(p.o)[t * p.D + c] = from_f<T>(y);
+  }
+  store_piece<float, NS>(p.hfin + id * p.N + n0, nleft, h);
+}
+
+template <typename T, typename SL> hipError_t forward(const SsmParams& p, hipStream_t stream) {
+  const dim3 grid((uint32_t)(p.G * p.bpg * p.nchunk));   // blocks of channels fastest: rows are contiguous
+  if (p.map.seq ? p.nchunk > 1 : p.cps > 1) {
+    hipLaunchKernelGGL((ssm_fwd_kernel<T, SL, true>), grid, dim3(kThreads), 0, stream, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((ssm_fwd_kernel<T, SL, false>), grid, dim3(kThreads), 0, stream, p);
+  return hipGetLastError();
+}
+template <typename T, typename SL> hipError_t decode(const SsmParams& p, hipStream_t stream) {
+  const int64_t wgs = (p.map.nseq * p.D + SL::kCB - 1) / SL::kCB;
+  if (wgs > INT32_MAX) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((ssm_decode_kernel<T, SL>), dim3((uint32_t)wgs), dim3(kThreads), 0, stream, p);
+  return hipGetLastError();
+}
+
+template <typename T> hipError_t dispatch(const SsmParams& p, bool single, hipStream_t stream) {
+  switch (ssm_padded(p.N)) {
+    case 8: return single ? decode<T, SsmLanes<2, 4>>(p, stream) : forward<T, SsmLanes<2, 4>>(p, stream);
+    case 16: return single ? decode<T, SsmLanes<4, 4>>(p, stream) : forward<T, SsmLanes<4, 4>>(p, stream);
+    case 32: return single ? decode<T, SsmLanes<4, 8>>(p, stream) : forward<T, SsmLanes<4, 8>>(p, stream);
+    default: return single ? decode<T, SsmLanes<4, 16>>(p, stream) : forward<T, SsmLanes<4, 16>>(p, stream);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_ssm_forward(const SsmParams& p, bool bf16, hipStream_t stream) {
+  const hipError_t e = bf16 ? dispatch<u16>(p, false, stream) : dispatch<float>(p, false, stream);
+  if (e != hipSuccess || !p.map.seq || !p.hfin) return e;
+  return launch_ssm_empty(p, p.h0, p.hfin, stream);
+}
+hipError_t launch_ssm_empty(const SsmParams& p, const float* from, float* to, hipStream_t stream) {
+  hipLaunchKernelGGL(ssm_empty_kernel, dim3(32), dim3(kThreads), 0, stream, p.map.empty, p.map.nseq, p.D * p.N, from, to);
+  return hipGetLastError();
+}
+hipError_t launch_ssm_decode(const SsmParams& p, bool bf16, hipStream_t stream) {
+  return bf16 ? dispatch<u16>(p, true, stream) : dispatch<float>(p, true, stream);
+}
+
+}  // namespace rla
