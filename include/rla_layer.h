@@ -97,12 +97,12 @@ rla_status rla_conv_decode(const rla_conv_problem *problem, const void *x,
  * ------------------------------------------------------------------------ */
 typedef struct {
   int64_t batch, seq_len;
-  int64_t channels;          /* D, a multiple of groups */
+  int64_t channels;          /* D < 2^24, a multiple of groups */
   int64_t states;            /* N_state, 1 to 64 */
   int64_t groups;            /* G >= 1 */
   int64_t num_seqs;
   const int32_t *cu_seqlens;
-  int64_t u_stride, delta_stride, z_stride, do_stride;   /* 0: D */
+  int64_t u_stride, delta_stride, z_stride, do_stride;   /* 0: D; all < 2^24 */
   int64_t b_stride, c_stride;                             /* 0: G * N_state */
   int32_t softplus;          /* 0 or 1 */
   int32_t dtype;             /* rla_dtype of u, delta, B, C, z, o and their gradients */

@@ -72,6 +72,8 @@ __device__ __forceinline__ float silu_grad_f(float z, float& silu) {
 // starts: bit t set where token t's sequence is not token t - 1's (and for t =
 // 0), bits past the end set; empty[n]: sequence n has no token.
 // ---------------------------------------------------------------------------
+// (constant while a kernel reads it: address space 4, scalar loads where t is uniform)
+template <typename T> using ConstPtr = const __attribute__((address_space(4))) T*;
 struct TokenMap {
   int64_t ntok = 0, T = 1;           // dense: tokens per sequence (packed: unused)
   int32_t nseq = 0;
@@ -80,13 +82,14 @@ struct TokenMap {
   const int32_t* empty = nullptr;
 
   __device__ __forceinline__ int seq_of(int64_t t) const {
-    return seq ? seq[t] : (int)((uint32_t)t / (uint32_t)T);
+    return seq ? ((ConstPtr<int32_t>)(uint64_t)seq)[t] : (int)((uint32_t)t / (uint32_t)T);
   }
   // start bits of tokens t .. t + 31
   __device__ __forceinline__ uint32_t start_bits(int64_t t) const {
     if (seq) {
       const uint32_t w = (uint32_t)t >> 5, s = (uint32_t)t & 31u;
-      const uint64_t two = (uint64_t)starts[w] | ((uint64_t)starts[w + 1] << 32);
+      const ConstPtr<uint32_t> words = (ConstPtr<uint32_t>)(uint64_t)starts;
+      const uint64_t two = (uint64_t)words[w] | ((uint64_t)words[w + 1] << 32);
       return (uint32_t)(two >> s);
     }
     const uint32_t r = (uint32_t)t % (uint32_t)T;

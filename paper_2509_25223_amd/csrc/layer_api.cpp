@@ -350,7 +350,7 @@ rla_status check_ssm(const rla_ssm_problem* q, SsmParams& p) {
   if (!is_type(q->dtype)) return RLA_ERR_DTYPE;
   const rla_status st = tokens(q->batch, q->seq_len, q->num_seqs, q->cu_seqlens, p.map);
   if (st != RLA_OK) return st;
-  if (q->states < 1 || q->states > 64 || q->groups < 1 || q->channels < q->groups || q->channels > (1 << 24) ||
+  if (q->states < 1 || q->states > 64 || q->groups < 1 || q->channels < q->groups || q->channels >= (1 << 24) ||
       q->channels % q->groups != 0)
     return RLA_ERR_SHAPE;
   if (q->softplus != 0 && q->softplus != 1) return RLA_ERR_VALUE;
@@ -362,8 +362,8 @@ rla_status check_ssm(const rla_ssm_problem* q, SsmParams& p) {
   if (!stride(q->u_stride, p.D, p.us) || !stride(q->delta_stride, p.D, p.dts) || !stride(q->z_stride, p.D, p.zs) ||
       !stride(q->do_stride, p.D, p.dos) || !stride(q->b_stride, p.G * p.N, p.bs) || !stride(q->c_stride, p.G * p.N, p.cs))
     return RLA_ERR_SHAPE;
-  for (int64_t s : {p.us, p.dts, p.zs, p.dos, p.bs, p.cs})
-    if (times(times(p.map.ntok, s), 4) < 0) return RLA_ERR_SHAPE;
+  for (int64_t s : {p.us, p.dts, p.zs, p.dos, p.bs, p.cs})   // (24-bit row offsets)
+    if (s >= (1 << 24) || times(times(p.map.ntok, s), 4) < 0) return RLA_ERR_SHAPE;
   if (times(times(p.map.nseq, p.D), p.N * 4) < 0) return RLA_ERR_SHAPE;
   const int64_t cb = ssm_channels(p.N);
   p.bpg = (int32_t)((p.Dg + cb - 1) / cb);

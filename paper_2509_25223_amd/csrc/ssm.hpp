@@ -85,9 +85,10 @@ __device__ __forceinline__ float softplus_exact(float x) {
   return x > 20.f ? x : s;
 }
 
-template <int NS_, int LPC_> struct SsmLanes {
+template <int NS_, int LPC_, int W_ = 4> struct SsmLanes {
   static constexpr int NS = NS_, LPC = LPC_, NP = NS * LPC;
-  static constexpr int kCW = 64 / LPC, kCB = kWaves * kCW;   // channels of a wave, of a workgroup
+  static constexpr int kW = W_, kThr = 64 * W_;           // waves, threads of a workgroup
+  static constexpr int kCW = 64 / LPC, kCB = kW * kCW;    // channels of a wave, of a workgroup
   // rows of LDS tiles [token][channel]: four rows apart on different banks
   static constexpr int kRow = kCB + kCB / 4;
   __device__ __forceinline__ static int q() { return (int)threadIdx.x % LPC; }
@@ -102,22 +103,81 @@ template <int NS> __device__ __forceinline__ void load_states(const float* p, in
   load_piece<float, NS>(p, left, h);
 }
 
+// x of another lane (every lane of the pattern exists: no value to fall back on, which
+// would cost an instruction to set)
+template <int CTRL> __device__ __forceinline__ float lane_dpp(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true));
+}
 // lane j of every quad
-template <int J> __device__ __forceinline__ float quad_lane(float x) { return dpp<J * 0x55>(x); }
+template <int J> __device__ __forceinline__ float quad_lane(float x) { return lane_dpp<J * 0x55>(x); }
+
+template <typename F> __device__ __forceinline__ void over4(const F& f) {
+  f(std::integral_constant<int, 0>());
+  f(std::integral_constant<int, 1>());
+  f(std::integral_constant<int, 2>());
+  f(std::integral_constant<int, 3>());
+}
+
+// The kernel's parameters read again from where the launch put them: a kernel with
+// some forty pointers and strides would otherwise keep them all in scalar registers
+// through its loops, and spill.  Only for kernels whose one argument is SsmParams.
+typedef ConstPtr<SsmParams> SsmArgs;
+__device__ __forceinline__ SsmArgs fresh_args() {
+  uint64_t a = (uint64_t)(__builtin_amdgcn_kernarg_segment_ptr());
+  asm volatile("" : "+s"(a));
+  return (SsmArgs)a;
+}
+
+// Loaded values have arrived here.  Without it a loop that uses values loaded in front
+// of it waits for every load at that use in each turn, the next tile's among them.
+template <int N> __device__ __forceinline__ void settle(float (&x)[N]) {
+#pragma unroll
+  for (int e = 0; e < N; ++e) asm volatile("" : "+v"(x[e]));
+}
+
+__device__ __forceinline__ TokenMap fresh_map(SsmArgs a) {
+  TokenMap m;
+  m.ntok = a->map.ntok;
+  m.T = a->map.T;
+  m.seq = a->map.seq;
+  m.starts = a->map.starts;
+  return m;
+}
+
+template <typename V> __device__ __forceinline__ V settled(V x) {
+  if constexpr (sizeof(V) == 2) {
+    u16 w = __builtin_bit_cast(u16, x);
+    asm volatile("" : "+v"(w));
+    return __builtin_bit_cast(V, w);
+  } else {
+    struct Words { uint32_t w[sizeof(V) / 4]; } t = __builtin_bit_cast(Words, x);
+#pragma unroll
+    for (int e = 0; e < (int)sizeof(V) / 4; ++e) asm volatile("" : "+v"(t.w[e]));
+    return __builtin_bit_cast(V, t);
+  }
+}
+
+// base + a lane's 32-bit offset in bytes
+template <typename T> __device__ __forceinline__ const T* at(const void* base, int64_t elems, uint32_t bytes) {
+  return reinterpret_cast<const T*>(reinterpret_cast<const char*>(reinterpret_cast<const T*>(base) + elems) + bytes);
+}
+template <typename T> __device__ __forceinline__ T* at(void* base, int64_t elems, uint32_t bytes) {
+  return reinterpret_cast<T*>(reinterpret_cast<char*>(reinterpret_cast<T*>(base) + elems) + bytes);
+}
 
 // v[j] summed over the LPC lanes of a channel; lane q keeps token q & 3's.
 template <int LPC> __device__ __forceinline__ float tokens_over_lanes(float (&v)[4]) {
   const int lane = threadIdx.x;
   if constexpr (LPC >= 16)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] += dpp<0x140>(v[j]);   // row_mirror
+    for (int j = 0; j < 4; ++j) v[j] += lane_dpp<0x140>(v[j]);   // row_mirror
   if constexpr (LPC >= 8)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] += dpp<0x141>(v[j]);   // row_half_mirror
+    for (int j = 0; j < 4; ++j) v[j] += lane_dpp<0x141>(v[j]);   // row_half_mirror
   const bool b0 = lane & 1, b1 = lane & 2;
-  const float x0 = (b0 ? v[1] : v[0]) + dpp<0xB1>(b0 ? v[0] : v[1]);
-  const float x1 = (b0 ? v[3] : v[2]) + dpp<0xB1>(b0 ? v[2] : v[3]);
-  return (b1 ? x1 : x0) + dpp<0x4E>(b1 ? x0 : x1);
+  const float x0 = (b0 ? v[1] : v[0]) + lane_dpp<0xB1>(b0 ? v[0] : v[1]);
+  const float x1 = (b0 ? v[3] : v[2]) + lane_dpp<0xB1>(b0 ? v[2] : v[3]);
+  return (b1 ? x1 : x0) + lane_dpp<0x4E>(b1 ? x0 : x1);
 }
 
 // Chunk c: first token, number of tokens.
@@ -165,5 +225,92 @@ __device__ __forceinline__ void chunk_starts(const SsmParams& p, int64_t t0, int
   last = __builtin_amdgcn_readfirstlane(last);
   first = __builtin_amdgcn_readfirstlane(first);
 }
+
+// ---------------------------------------------------------------------------
+// Staging: tiles of TT tokens x kCB channels, a thread's (token, piece of V
+// channels), and of B and C a (token, VB states).  A tile is loaded, as stored, one
+// turn ahead of its use.  No load depends on a branch of a lane's own, nor leaves an
+// older value in its register (either makes the loads behind it wait for those in
+// front): tokens past the chunk read its last one, channels past the block its last
+// one, states past the last the last, an absent gate the steps, and all of them are
+// masked where they are used.
+// ---------------------------------------------------------------------------
+constexpr int kStU = 1, kStZ = 2, kStO = 4, kStB = 8, kStC = 16;
+
+template <typename T, typename SL, int TT, int WHAT> struct SsmStage {
+  static constexpr int V = TT * SL::kCB / SL::kThr, kPer = SL::kCB / V;
+  static constexpr int VB = TT * SL::NP >= SL::kThr ? TT * SL::NP / SL::kThr : 1, kPerB = SL::NP / VB;
+  typedef typename RowVec<T, V>::type Vec;
+  typedef typename RowVec<T, VB>::type VecB;
+  Vec u, d, z, o;
+  VecB b, c;
+  int seq = 0, seqb = 0;   // of the tokens (packed)
+
+  // token and first channel; token and first state
+  __device__ __forceinline__ static int r() { return (int)threadIdx.x / kPer; }
+  __device__ __forceinline__ static int pc() { return (int)threadIdx.x % kPer * V; }
+  __device__ __forceinline__ static int rb() { return min((int)threadIdx.x / kPerB, TT - 1); }
+  __device__ __forceinline__ static int pb() { return (int)threadIdx.x % kPerB * VB; }
+  // threads that stage B and C (8 states: half of them, the others repeat the last token)
+  __device__ __forceinline__ static bool owns_b() { return TT * SL::NP >= SL::kThr || (int)threadIdx.x < TT * SL::NP; }
+  __device__ __forceinline__ bool inside(int k, int end, bool packed) const { return k + r() < end && (!packed || seq >= 0); }
+  __device__ __forceinline__ bool inside_b(int k, int end, bool packed) const { return k + rb() < end && (!packed || seqb >= 0); }
+
+  // the piece of row `row` (< 32, its stride < 2^24) from column `col` on, of `width` columns
+  template <int N>
+  __device__ __forceinline__ static typename RowVec<T, N>::type piece(const void* base, int64_t first, uint32_t row,
+                                                                      int64_t stride, int col, bool whole, int width) {
+    typedef typename RowVec<T, N>::type Out;
+    const uint32_t off = __umul24(row, (uint32_t)stride);
+    if (whole) return *at<Out>(base, first, (off + (uint32_t)col) * (uint32_t)sizeof(T));
+    Out x;
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = *at<T>(base, first, (off + (uint32_t)min(col + e, width - 1)) * (uint32_t)sizeof(T));
+    return x;
+  }
+  template <typename Q> __device__ __forceinline__ static const Q* at(const void* base, int64_t first, uint32_t bytes) {
+    return reinterpret_cast<const Q*>(reinterpret_cast<const char*>(reinterpret_cast<const T*>(base) + first) + bytes);
+  }
+
+  // tokens from t on, of which `left` >= 1 are the chunk's; nc channels from c0 on
+  __device__ __forceinline__ void load(int64_t t, int left, int64_t c0, int64_t g, int nc) {
+    const SsmArgs a = fresh_args();
+    const uint32_t rr = min(r(), left - 1), rrb = min(rb(), left - 1);
+    const int N = (int)a->N;
+    const bool all = nc == SL::kCB, states = N == SL::NP, gated = (WHAT & kStZ) && a->z != nullptr;
+    // (all of the scalar loads first, one wait for them)
+    const void *pd = a->delta, *pu = a->u, *po = a->dO, *pz = gated ? a->z : a->delta, *pb_ = a->B, *pc_ = a->C;
+    const int64_t sd = a->dts, su = a->us, so = a->dos, sz = gated ? a->zs : a->dts, sb = a->bs, sc = a->cs;
+    if (a->map.seq) {
+      seq = a->map.seq[t + rr];
+      seqb = a->map.seq[t + rrb];
+    }
+    d = piece<V>(pd, t * sd + c0, rr, sd, pc(), all, nc);
+    if constexpr (WHAT & kStU) u = piece<V>(pu, t * su + c0, rr, su, pc(), all, nc);
+    if constexpr (WHAT & kStO) o = piece<V>(po, t * so + c0, rr, so, pc(), all, nc);
+    if constexpr (WHAT & kStZ) z = piece<V>(pz, t * sz + c0, rr, sz, pc(), all, nc);
+    if constexpr (WHAT & kStB) b = piece<VB>(pb_, t * sb + g * N, rrb, sb, pb(), states, N);
+    if constexpr (WHAT & kStC) c = piece<VB>(pc_, t * sc + g * N, rrb, sc, pb(), states, N);
+  }
+  // The tile has arrived.  Memory operations are counted in order: a wait for these
+  // loads behind the stores of the tile before would be one for the stores too.
+  __device__ __forceinline__ void settle() {
+    d = settled(d);
+    if constexpr (WHAT & kStU) u = settled(u);
+    if constexpr (WHAT & kStO) o = settled(o);
+    if constexpr (WHAT & kStZ) z = settled(z);
+    if constexpr (WHAT & kStB) b = settled(b);
+    if constexpr (WHAT & kStC) c = settled(c);
+    asm volatile("" : "+v"(seq), "+v"(seqb));
+  }
+  // steps of the thread's channels
+  __device__ __forceinline__ void steps(const float (&bias)[V], bool softplus, float (&s)[V]) const {
+#pragma unroll
+    for (int e = 0; e < V; ++e) s[e] = to_f<T>(d[e]) + bias[e];
+    if (softplus)
+#pragma unroll
+      for (int e = 0; e < V; ++e) s[e] = softplus_exact(s[e]);
+  }
+};
 
 }  // namespace rla

@@ -34,7 +34,7 @@ __device__ __forceinline__ float half16(float a, float b) {
 }
 // x of lane ^ 4
 __device__ __forceinline__ float across4(float x) {
-  int y = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x104, 0xF, 0x5, false);   // row_shl:4
+  int y = __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x104, 0xF, 0xF, true);          // row_shl:4
   y = __builtin_amdgcn_update_dpp(y, __builtin_bit_cast(int, x), 0x114, 0xF, 0xA, false);       // row_shr:4
   return __builtin_bit_cast(float, y);
 }
@@ -67,7 +67,7 @@ template <typename SL> struct ChannelSums {
       float b[NS / 2];
 #pragma unroll
       for (int n = 0; n < NS / 2; ++n)
-        b[n] = (b3 ? a[n + NS / 2] : a[n]) + dpp<0x128>(b3 ? a[n] : a[n + NS / 2]);   // row_ror:8
+        b[n] = (b3 ? a[n + NS / 2] : a[n]) + lane_dpp<0x128>(b3 ? a[n] : a[n + NS / 2]);   // row_ror:8
       if constexpr (LPC == 8) {
 #pragma unroll
         for (int n = 0; n < NS / 2; ++n) out[n] = b[n];
@@ -84,12 +84,11 @@ template <typename SL> struct ChannelSums {
 // E[chunk]: the gradient of the state entering the chunk, from zero behind it (or,
 // where its sequence ends inside, from the final state's).
 template <typename T, typename SL>
-__global__ __launch_bounds__(kThreads) void ssm_rev_kernel(SsmParams p) {
+__global__ __launch_bounds__(SL::kThr) void ssm_rev_kernel(SsmParams p) {
   constexpr int NS = SL::NS, NP = SL::NP, kRow = SL::kRow, TT = kSsmTile;
-  constexpr int V = TT * SL::kCB / kThreads, kPer = SL::kCB / V;
-  constexpr int VB = TT * NP / kThreads, kPerB = NP / VB;
+  typedef SsmStage<T, SL, TT, kStO | kStZ | kStC> St;
+  constexpr int V = St::V, VB = St::VB;
   __shared__ __attribute__((aligned(16))) float sD[TT][kRow], sG[TT][kRow], sC[TT][NP];
-  const int tid = threadIdx.x;
   const int nblk = (int)p.G * p.bpg, chunk = (int)blockIdx.x / nblk, blk = (int)blockIdx.x - chunk * nblk;
   const int g = blk / p.bpg;
   const int64_t c0 = g * p.Dg + (int64_t)(blk - g * p.bpg) * SL::kCB;
@@ -116,57 +115,81 @@ __global__ __launch_bounds__(kThreads) void ssm_rev_kernel(SsmParams p) {
 #pragma unroll
     for (int n = 0; n < NS; ++n) dh[n] = 0.f;
 
-  const int r = tid / kPer, pc = tid % kPer * V, pleft = nc - pc;
-  const int rb = tid / kPerB, pb = tid % kPerB * VB, bleft = (int)p.N - pb;
-  const T* dg = reinterpret_cast<const T*>(p.delta) + c0 + pc;
-  const T* og = reinterpret_cast<const T*>(p.dO) + c0 + pc;
-  const T* zg = reinterpret_cast<const T*>(p.z) + c0 + pc;
-  const T* cg = reinterpret_cast<const T*>(p.C) + g * p.N + pb;
+  St st;
+  const int r = St::r(), pc = St::pc(), rb = St::rb(), pb = St::pb(), pleft = nc - pc, bleft = (int)p.N - pb;
   float bias[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) bias[e] = p.dbias && e < pleft ? p.dbias[c0 + pc + e] : 0.f;
-  typename RowVec<T, V>::type rd, ro, rz;
-  typename RowVec<T, VB>::type rc;
-  bool in = false, inb = false;
-  auto load_tile = [&](int k) {
-    const int64_t t = t0 + k + r, tb = t0 + k + rb;
-    in = k + r < end && (!p.map.seq || p.map.seq[t] >= 0);
-    inb = k + rb < end && (!p.map.seq || p.map.seq[tb] >= 0);
-    if (in) {
-      load_raw<T, V>(dg + t * p.dts, pleft, rd);
-      load_raw<T, V>(og + t * p.dos, pleft, ro);
-      if (p.z) load_raw<T, V>(zg + t * p.zs, pleft, rz);
-    }
-    if (inb) load_raw<T, VB>(cg + tb * p.cs, bleft, rc);
-  };
+  settle(A2);
+  settle(dh);
+  settle(bias);
   const int k_last = (end - 1) / TT * TT;
-  load_tile(k_last);
+  const bool packed = p.map.seq != nullptr, sp = p.softplus != 0, gated = p.z != nullptr;
+  st.load(t0 + k_last, end - k_last, c0, g, nc);
   for (int k = k_last; k >= 0; k -= TT) {
+    const bool in = st.inside(k, end, packed);
+    float s[V];
+    st.steps(bias, sp, s);
 #pragma unroll
     for (int e = 0; e < V; ++e) {
       const bool use = in && e < pleft;
-      const float raw = to_f<T>(rd[e]) + bias[e], z = p.z ? to_f<T>(rz[e]) : 0.f;
-      sD[r][pc + e] = use ? (p.softplus ? softplus_exact(raw) : raw) : 0.f;
-      sG[r][pc + e] = use ? to_f<T>(ro[e]) * (p.z ? z * sigmoid_fast(z) : 1.f) : 0.f;
+      float gy = to_f<T>(st.o[e]);
+      if (gated) {
+        const float z = to_f<T>(st.z[e]);
+        gy *= z * sigmoid_fast(z);
+      }
+      sD[r][pc + e] = use ? s[e] : 0.f;
+      sG[r][pc + e] = use ? gy : 0.f;
     }
+    if (st.owns_b()) {
+      const bool inb = st.inside_b(k, end, packed);
 #pragma unroll
-    for (int e = 0; e < VB; ++e) sC[rb][pb + e] = inb && e < bleft ? to_f<T>(rc[e]) : 0.f;
+      for (int e = 0; e < VB; ++e) sC[rb][pb + e] = inb && e < bleft ? to_f<T>(st.c[e]) : 0.f;
+    }
     __syncthreads();
-    if (k >= TT) load_tile(k - TT);
-#pragma unroll 1
-    for (int i = TT - 4; i >= 0; i -= 4) {
-      const float dv = sD[i + (q & 3)][ch], gv = sG[i + (q & 3)][ch];
-      auto token = [&](auto J) {
-        constexpr int j = decltype(J)::value;
-        const float dj = quad_lane<j>(dv), gj = quad_lane<j>(gv);
+    if (k >= TT) st.load(t0 + k - TT, TT, c0, g, nc);
+struct Four {
+      float d, g, c[4][NS];
+    };
+    auto fetch = [&](int i, Four& f) {
+      f.d = sD[i + (q & 3)][ch];
+      f.g = sG[i + (q & 3)][ch];
 #pragma unroll
-        for (int n = 0; n < NS; ++n)
-          dh[n] = __builtin_amdgcn_exp2f(dj * A2[n]) * __builtin_fmaf(gj, sC[i + j][n0 + n], dh[n]);
-      };
-      token(std::integral_constant<int, 3>());
-      token(std::integral_constant<int, 2>());
-      token(std::integral_constant<int, 1>());
-      token(std::integral_constant<int, 0>());
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int n = 0; n < NS; ++n) f.c[j][n] = sC[i + j][n0 + n];
+    };
+    Four f[2];
+    fetch(TT - 4, f[1]);
+#pragma unroll
+    for (int i = TT - 4; i >= 0; i -= 4) {
+      if (i > 0) fetch(i - 4, f[(i / 4 + 1) & 1]);
+      __builtin_amdgcn_sched_barrier(0);
+      const Four& now = f[(i / 4) & 1];
+      float e[4][NS], x[4][NS];
+      over4([&](auto J) {
+        constexpr int j = decltype(J)::value;
+        const float dj = quad_lane<j>(now.d);
+#pragma unroll
+        for (int n = 0; n < NS; ++n) e[j][n] = dj * A2[n];
+      });
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int n = 0; n < NS; ++n) e[j][n] = __builtin_amdgcn_exp2f(e[j][n]);
+      over4([&](auto J) {   // through the decay at once: a C dy + a dh
+        constexpr int j = decltype(J)::value;
+        const float gj = quad_lane<j>(now.g);
+#pragma unroll
+        for (int n = 0; n < NS; ++n) x[j][n] = e[j][n] * (gj * now.c[j][n]);
+      });
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 3; j >= 0; --j)
+#pragma unroll
+        for (int n = 0; n < NS; ++n) dh[n] = __builtin_fmaf(e[j][n], dh[n], x[j][n]);
+      __builtin_amdgcn_sched_barrier(0);
     }
     __syncthreads();
   }
@@ -174,15 +197,19 @@ __global__ __launch_bounds__(kThreads) void ssm_rev_kernel(SsmParams p) {
 }
 
 template <typename T, typename SL>
-__global__ __launch_bounds__(kThreads) void ssm_bwd_kernel(SsmParams p) {
+__global__ __launch_bounds__(SL::kThr, 2) void ssm_bwd_kernel(SsmParams p) {
   constexpr int NS = SL::NS, LPC = SL::LPC, NP = SL::NP, kRow = SL::kRow, TT = kSsmSub;
-  constexpr int V = TT * SL::kCB / kThreads, kPer = SL::kCB / V;   // staging: channels a thread, threads a token
-  constexpr int VB = TT * NP >= kThreads ? TT * NP / kThreads : 1, kPerB = NP / VB;
+  typedef SsmStage<T, SL, TT, kStU | kStZ | kStO | kStB | kStC> St;
+  constexpr int V = St::V, VB = St::VB;
   typedef ChannelSums<SL> CS;
   __shared__ __attribute__((aligned(16))) float sD[TT][kRow], sX[TT][kRow], sG[TT][kRow];
   __shared__ __attribute__((aligned(16))) float sI[TT][kRow], sQ[TT][kRow], sY[TT][kRow];
   __shared__ __attribute__((aligned(16))) float sB[TT][NP], sC[TT][NP];
-  __shared__ float sdB[kWaves][TT][NP], sdC[kWaves][TT][NP];
+  // each thread's own: the tile as loaded, its channels' bias and skip (registers are what
+  // this kernel is short of)
+  __shared__ __attribute__((aligned(16))) T sOwn[4][SL::kThr][V];
+  __shared__ float sBias[SL::kCB], sSkip[SL::kCB];
+  __shared__ __attribute__((aligned(16))) float sBC[SL::kW][2][TT][NP];   // a wave's sums of dB, dC
 
   const int tid = threadIdx.x, wave = tid >> 6;
   const int nblk = (int)p.G * p.bpg, chunk = (int)blockIdx.x / nblk, blk = (int)blockIdx.x - chunk * nblk;
@@ -205,10 +232,13 @@ __global__ __launch_bounds__(kThreads) void ssm_bwd_kernel(SsmParams p) {
     dA[n] = 0.f;
   }
   auto state_of = [&](const float* base, int seq, float (&h)[NS]) {
-    if (base && seq >= 0) load_states<NS>(base + ((int64_t)seq * p.D + c) * p.N + n0, nleft, h);
-    else
+    if (base && seq >= 0) {
+      load_states<NS>(base + ((int64_t)seq * p.D + c) * p.N + n0, nleft, h);
+      settle(h);   // here, and not in every tile's turn of the code that follows
+    } else {
 #pragma unroll
       for (int n = 0; n < NS; ++n) h[n] = 0.f;
+    }
   };
   // the gradient behind the chunk's last token
   int seq = p.map.seq_of(t0 + len - 1);
@@ -230,184 +260,281 @@ __global__ __launch_bounds__(kThreads) void ssm_bwd_kernel(SsmParams p) {
     }
   }
 
-  const int r = tid / kPer, pc = tid % kPer * V, pleft = nc - pc;
-  const int rb = tid / kPerB, pb = tid % kPerB * VB, bleft = (int)p.N - pb;
-  const T* ug = reinterpret_cast<const T*>(p.u) + c0 + pc;
-  const T* dg = reinterpret_cast<const T*>(p.delta) + c0 + pc;
-  const T* zg = reinterpret_cast<const T*>(p.z) + c0 + pc;
-  const T* og = reinterpret_cast<const T*>(p.dO) + c0 + pc;
-  const T* bg = reinterpret_cast<const T*>(p.B) + g * p.N + pb;
-  const T* cg = reinterpret_cast<const T*>(p.C) + g * p.N + pb;
-  float bias[V], skip[V], dskip[V], ddb[V];
+  St st;
+  const int r = St::r(), pc = St::pc(), rb = St::rb(), pb = St::pb(), pleft = nc - pc, bleft = (int)p.N - pb;
+  const uint32_t fout = (r * (uint32_t)p.D + pc) * (uint32_t)sizeof(T), fck = ((live ? ch : 0) * NP + n0) * 4;
+  float dskip[V], ddb[V];
 #pragma unroll
-  for (int e = 0; e < V; ++e) {
-    bias[e] = p.dbias && e < pleft ? p.dbias[c0 + pc + e] : 0.f;
-    skip[e] = p.skip && e < pleft ? p.skip[c0 + pc + e] : 0.f;
-    dskip[e] = ddb[e] = 0.f;
+  for (int e = 0; e < V; ++e) dskip[e] = ddb[e] = 0.f;
+  if (tid < SL::kCB) {
+    sBias[tid] = p.dbias && tid < nc ? p.dbias[c0 + tid] : 0.f;
+    sSkip[tid] = p.skip && tid < nc ? p.skip[c0 + tid] : 0.f;
   }
-  typename RowVec<T, V>::type ru, rd, rz, ro;
-  typename RowVec<T, VB>::type rB, rC;
+  __syncthreads();
   float ck[NS];
-  bool in = false, inb = false;
   auto load_tile = [&](int k) {
-    const int64_t t = t0 + k + r, tb = t0 + k + rb;
-    in = k + r < len && (!p.map.seq || p.map.seq[t] >= 0);
-    inb = rb < TT && k + rb < len && (!p.map.seq || p.map.seq[tb] >= 0);
-    if (in) {
-      load_raw<T, V>(ug + t * p.us, pleft, ru);
-      load_raw<T, V>(dg + t * p.dts, pleft, rd);
-      load_raw<T, V>(og + t * p.dos, pleft, ro);
-      if (p.z) load_raw<T, V>(zg + t * p.zs, pleft, rz);
-    }
-    if (inb) {
-      load_raw<T, VB>(bg + tb * p.bs, bleft, rB);
-      load_raw<T, VB>(cg + tb * p.cs, bleft, rC);
-    }
-    const int64_t sub = (int64_t)chunk * (p.L / kSsmSub) + k / kSsmSub;
-    load_states<NS>(p.ck + (sub * p.D + c) * NP + n0, NS, ck);
+    st.load(t0 + k, len - k, c0, g, nc);
+    const SsmArgs a = fresh_args();
+    const int64_t sub = (int64_t)chunk * (a->L / kSsmSub) + k / kSsmSub;
+    load_piece<float, NS, true>(at<float>(a->ck, (sub * a->D + c0) * NP, fck), NS, ck);
   };
+  settle(A2);
+  settle(carry);
   const int k_last = (len - 1) / TT * TT;
+  const bool packed = p.map.seq != nullptr, sp = p.softplus != 0, gated = p.z != nullptr;
   load_tile(k_last);
   for (int k = k_last; k >= 0; k -= TT) {
+    const SsmArgs a = fresh_args();
     // ---- these tokens into LDS ----
-    float s[V], u[V], gy[V], o[V], z[V], slope[V];
-    const bool here = in;
+    const uint32_t valid = len - k >= TT ? (1u << TT) - 1u : (1u << (len - k)) - 1u;
+    const uint32_t bits = fresh_map(a).start_bits(t0 + k) & valid;
+    const bool here = st.inside(k, len, packed);
+    {
+      float s[V], bias[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const bool use = here && e < pleft;
-      const float raw = (use ? to_f<T>(rd[e]) : 0.f) + bias[e];
-      u[e] = use ? to_f<T>(ru[e]) : 0.f;
-      o[e] = use ? to_f<T>(ro[e]) : 0.f;
-      z[e] = use && p.z ? to_f<T>(rz[e]) : 0.f;
-      s[e] = use ? (p.softplus ? softplus_exact(raw) : raw) : 0.f;
-      slope[e] = p.softplus ? sigmoid_fast(raw) : 1.f;
-      gy[e] = p.z ? o[e] * (z[e] * sigmoid_fast(z[e])) : o[e];
-      sD[r][pc + e] = s[e];
-      sX[r][pc + e] = s[e] * u[e];
-      sG[r][pc + e] = gy[e];
-    }
-    if (rb < TT)
-#pragma unroll
-      for (int e = 0; e < VB; ++e) {
-        sB[rb][pb + e] = inb && e < bleft ? to_f<T>(rB[e]) : 0.f;
-        sC[rb][pb + e] = inb && e < bleft ? to_f<T>(rC[e]) : 0.f;
+      for (int e = 0; e < V; ++e) {
+        bias[e] = sBias[pc + e];
+        sOwn[0][tid][e] = st.u[e];
+        sOwn[1][tid][e] = st.d[e];
+        sOwn[2][tid][e] = st.z[e];
+        sOwn[3][tid][e] = st.o[e];
       }
-    float h[NS];
+      st.steps(bias, sp, s);
 #pragma unroll
-    for (int n = 0; n < NS; ++n) h[n] = ck[n];
+      for (int e = 0; e < V; ++e) {
+        const bool use = here && e < pleft;
+        float gy = to_f<T>(st.o[e]);
+        if (gated) {
+          const float z = to_f<T>(st.z[e]);
+          gy *= z * sigmoid_fast(z);
+        }
+        sD[r][pc + e] = use ? s[e] : 0.f;
+        sX[r][pc + e] = use ? s[e] * to_f<T>(st.u[e]) : 0.f;
+        sG[r][pc + e] = use ? gy : 0.f;
+      }
+      if (st.owns_b()) {
+        const bool inb = st.inside_b(k, len, packed);
+#pragma unroll
+        for (int e = 0; e < VB; ++e) {
+          sB[rb][pb + e] = inb && e < bleft ? to_f<T>(st.b[e]) : 0.f;
+          sC[rb][pb + e] = inb && e < bleft ? to_f<T>(st.c[e]) : 0.f;
+        }
+      }
+    }
+    float h[NS], hck[NS];
+#pragma unroll
+    for (int n = 0; n < NS; ++n) hck[n] = ck[n];
     __syncthreads();
     if (k >= TT) load_tile(k - TT);
 
-    // ---- the states again ----
-    const uint32_t valid = len - k >= TT ? (1u << TT) - 1u : (1u << (len - k)) - 1u;
-    const uint32_t bits = p.map.start_bits(t0 + k) & valid;
-    float a[TT][NS], ah[TT][NS];   // decays; decayed states a h_{t-1}
+    // ---- the states again, then the reverse recurrence ----
+    // one stretch [lo, hi) of a sequence at a time, from the last; nearly always all 16
+    auto stretch = [&](auto WHOLE, int lo, int hi) {
+      constexpr bool whole = decltype(WHOLE)::value;
+      auto inside = [&](int t) { return whole || (t >= lo && t < hi); };
+      float decay[TT][NS], hg[TT / 4][NS];   // decays; states before every 4 tokens
+      // as in the forward, passes over four tokens' states of independent instructions
 #pragma unroll
-    for (int i = 0; i < TT; i += 4) {
-      const float dv = sD[i + (q & 3)][ch], xv = sX[i + (q & 3)][ch];
-      float y[4];
-      auto token = [&](auto J) {
-        constexpr int j = decltype(J)::value;
-        if ((bits >> (i + j)) & 1u) state_of(p.h0, p.map.seq_of(t0 + k + i + j), h);
-        const float dj = quad_lane<j>(dv), xj = quad_lane<j>(xv);
-        float acc = 0.f;
+      for (int i = 0; i < TT; i += 4) {
+        const float dv = sD[i + (q & 3)][ch], xv = sX[i + (q & 3)][ch];
+        float x[4][NS], c4[4][NS];
 #pragma unroll
-        for (int n = 0; n < NS; ++n) {
-          a[i + j][n] = __builtin_amdgcn_exp2f(dj * A2[n]);
-          ah[i + j][n] = a[i + j][n] * h[n];
-          h[n] = __builtin_fmaf(xj, sB[i + j][n0 + n], ah[i + j][n]);
-          acc = __builtin_fmaf(h[n], sC[i + j][n0 + n], acc);
-        }
-        y[j] = acc;
-      };
-      token(std::integral_constant<int, 0>());
-      token(std::integral_constant<int, 1>());
-      token(std::integral_constant<int, 2>());
-      token(std::integral_constant<int, 3>());
-      if (p.z) {
-        const float yt = tokens_over_lanes<LPC>(y);
-        if (q < 4) sY[i + q][ch] = yt;
-      }
-    }
-
-    // ---- the reverse recurrence ----
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-    for (int i = TT - 4; i >= 0; i -= 4) {
-      const float dv = sD[i + (q & 3)][ch], xv = sX[i + (q & 3)][ch], gv = sG[i + (q & 3)][ch];
-      float into[4], qa[4], vB[4][NS], vC[4][NS];
-      auto token = [&](auto J) {
-        constexpr int j = decltype(J)::value;
-        const float dj = quad_lane<j>(dv), xj = quad_lane<j>(xv), gj = quad_lane<j>(gv);
-        float acc = 0.f, acq = 0.f;
-#pragma unroll
-        for (int n = 0; n < NS; ++n) {
-          const float b = sB[i + j][n0 + n], cc = sC[i + j][n0 + n];
-          const float dh = __builtin_fmaf(gj, cc, carry[n]);
-          const float qn = dh * ah[i + j][n];
-          vC[j][n] = gj * __builtin_fmaf(xj, b, ah[i + j][n]);
-          vB[j][n] = dh * xj;
-          acc = __builtin_fmaf(dh, b, acc);
-          acq = __builtin_fmaf(A2[n], qn, acq);
-          dA[n] = __builtin_fmaf(dj, qn, dA[n]);
-          carry[n] = dh * a[i + j][n];
-        }
-        into[j] = acc;
-        qa[j] = acq;
-        if ((bits >> (i + j)) & 1u) {   // a sequence's first token: what flows out is its initial state's
-          const int64_t t = t0 + k + i + j;
-          if (p.dh0 && live) {
-            const int sq = p.map.seq_of(t);
-            if (sq >= 0) store_piece<float, NS>(p.dh0 + ((int64_t)sq * p.D + c) * p.N + n0, nleft, carry);
+          for (int n = 0; n < NS; ++n) {
+            x[j][n] = sB[i + j][n0 + n];
+            c4[j][n] = sC[i + j][n0 + n];
           }
-          state_of(p.dhfin, k + i + j > 0 ? p.map.seq_of(t - 1) : -1, carry);
-        }
-      };
-      token(std::integral_constant<int, 3>());
-      token(std::integral_constant<int, 2>());
-      token(std::integral_constant<int, 1>());
-      token(std::integral_constant<int, 0>());
-      const float it = tokens_over_lanes<LPC>(into), qt = tokens_over_lanes<LPC>(qa);
-      if (q < 4) {
-        sI[i + q][ch] = it;
-        sQ[i + q][ch] = qt;
-      }
-      float oB[CS::kKeep], oC[CS::kKeep];
-      CS::run(vB, oB);
-      CS::run(vC, oC);
+        over4([&](auto J) {
+          constexpr int j = decltype(J)::value;
+          const float dj = quad_lane<j>(dv), xj = quad_lane<j>(xv);
 #pragma unroll
-      for (int n = 0; n < CS::kKeep; ++n) {
-        sdB[wave][i + CS::tok()][n0 + CS::st() + n] = oB[n];
-        sdC[wave][i + CS::tok()][n0 + CS::st() + n] = oC[n];
+          for (int n = 0; n < NS; ++n) {
+            decay[i + j][n] = dj * A2[n];
+            x[j][n] *= xj;
+          }
+        });
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int n = 0; n < NS; ++n) decay[i + j][n] = __builtin_amdgcn_exp2f(decay[i + j][n]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < NS; ++n) hg[i / 4][n] = h[n];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (inside(i + j))
+#pragma unroll
+            for (int n = 0; n < NS; ++n) x[j][n] = h[n] = __builtin_fmaf(decay[i + j][n], h[n], x[j][n]);
+        if (gated) {
+          float y[4];
+#pragma unroll
+          for (int n = 0; n < NS; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[j] = n == 0 ? x[j][n] * c4[j][n] : __builtin_fmaf(x[j][n], c4[j][n], y[j]);
+          const float yt = tokens_over_lanes<LPC>(y);
+          if (q < 4 && inside(i + q)) sY[i + q][ch] = yt;
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
+#pragma unroll
+      for (int i = TT - 4; i >= 0; i -= 4) {
+        const float dv = sD[i + (q & 3)][ch], xv = sX[i + (q & 3)][ch], gv = sG[i + (q & 3)][ch];
+        float x[4][NS], ah[4][NS], v[4][NS];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int n = 0; n < NS; ++n) x[j][n] = sB[i + j][n0 + n];
+        over4([&](auto J) {
+          constexpr int j = decltype(J)::value;
+          const float xj = quad_lane<j>(xv);
+#pragma unroll
+          for (int n = 0; n < NS; ++n) x[j][n] *= xj;
+        });
+        // the states again, from the decays; dy h for dC
+        float ht[NS];
+#pragma unroll
+        for (int n = 0; n < NS; ++n) ht[n] = hg[i / 4][n];
+        over4([&](auto J) {
+          constexpr int j = decltype(J)::value;
+          const float gj = quad_lane<j>(gv);
+          if (inside(i + j))
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
+              ah[j][n] = decay[i + j][n] * ht[n];
+              ht[n] = ah[j][n] + x[j][n];
+            }
+#pragma unroll
+          for (int n = 0; n < NS; ++n) v[j][n] = inside(i + j) ? gj * ht[n] : 0.f;
+        });
+        float oB[CS::kKeep], oC[CS::kKeep];
+        CS::run(v, oC);
+        __builtin_amdgcn_sched_barrier(0);
+        // dh: what reaches each token from behind, x[j] = C dy first
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int n = 0; n < NS; ++n) x[j][n] = sC[i + j][n0 + n];
+        over4([&](auto J) {
+          constexpr int j = decltype(J)::value;
+          const float gj = quad_lane<j>(gv);
+#pragma unroll
+          for (int n = 0; n < NS; ++n) x[j][n] *= gj;
+        });
+#pragma unroll
+        for (int j = 3; j >= 0; --j)
+          if (inside(i + j))
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
+              x[j][n] += carry[n];
+              carry[n] = x[j][n] * decay[i + j][n];
+            }
+        __builtin_amdgcn_sched_barrier(0);
+        float into[4], qa[4];
+        over4([&](auto J) {
+          constexpr int j = decltype(J)::value;
+          const float dj = quad_lane<j>(dv), xj = quad_lane<j>(xv);
+          if (inside(i + j)) {
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
+              const float qn = x[j][n] * ah[j][n], b = sB[i + j][n0 + n];
+              v[j][n] = x[j][n] * xj;
+              into[j] = n == 0 ? x[j][n] * b : __builtin_fmaf(x[j][n], b, into[j]);
+              qa[j] = n == 0 ? A2[n] * qn : __builtin_fmaf(A2[n], qn, qa[j]);
+              dA[n] = __builtin_fmaf(dj, qn, dA[n]);
+            }
+          } else {
+            into[j] = qa[j] = 0.f;
+#pragma unroll
+            for (int n = 0; n < NS; ++n) v[j][n] = 0.f;
+          }
+        });
+        const float it = tokens_over_lanes<LPC>(into), qt = tokens_over_lanes<LPC>(qa);
+        if (q < 4 && inside(i + q)) {
+          sI[i + q][ch] = it;
+          sQ[i + q][ch] = qt;
+        }
+        CS::run(v, oB);
+        if (inside(i + CS::tok())) {
+#pragma unroll
+          for (int n = 0; n < CS::kKeep; ++n) {
+            sBC[wave][0][i + CS::tok()][n0 + CS::st() + n] = oB[n];
+            sBC[wave][1][i + CS::tok()][n0 + CS::st() + n] = oC[n];
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    for (int hi = TT; hi > 0;) {
+      const uint32_t below = bits & ((1u << hi) - 1u);
+      const int lo = below ? 31 - __clz(below) : 0;
+      const bool starts = below != 0;
+      const int64_t t = t0 + k + lo;
+      if (starts) {
+        state_of(a->h0, p.map.seq_of(t), h);
+      } else {
+#pragma unroll
+        for (int n = 0; n < NS; ++n) h[n] = hck[n];
+      }
+      if (lo == 0 && hi == TT) stretch(std::true_type(), lo, hi);
+      else stretch(std::false_type(), lo, hi);
+      if (starts) {   // what flows out is the initial state's; in front, another sequence ends
+        const int sq = p.map.seq_of(t);
+        if (a->dh0 && live && sq >= 0) store_piece<float, NS>(a->dh0 + ((int64_t)sq * a->D + c) * a->N + n0, nleft, carry);
+        state_of(a->dhfin, k + lo > 0 ? p.map.seq_of(t - 1) : -1, carry);
+      }
+      hi = lo;
     }
+    st.settle();
+    settle(ck);
     __syncthreads();
 
-    // ---- gradients of the activations ----
-    if (k + r < len) {
+    // ---- gradients of the activations (the thread's own places of the tiles) ----
+    // no branches among the values: a wait for one would be for the stores in front too
+    {
       float du[V], dd[V], dz[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const float into = sI[r][pc + e], ds = __builtin_fmaf(u[e], into, kLn2 * sQ[r][pc + e]);
-        du[e] = __builtin_fmaf(s[e], into, skip[e] * gy[e]);
-        dd[e] = ds * slope[e];
+        const bool use = here && e < pleft;   // else outside every sequence, or past the chunk: zeros
+        const float u = to_f<T>(sOwn[0][tid][e]), skip = sSkip[pc + e], gy = sG[r][pc + e], into = sI[r][pc + e];
+        const float slope = sp ? sigmoid_fast(to_f<T>(sOwn[1][tid][e]) + sBias[pc + e]) : 1.f;
         float act;
-        dz[e] = p.z ? o[e] * __builtin_fmaf(skip[e], u[e], sY[r][pc + e]) * silu_grad_f(z[e], act) : 0.f;
-        if (!here) du[e] = dd[e] = dz[e] = 0.f;   // outside every sequence
-        dskip[e] = __builtin_fmaf(gy[e], u[e], dskip[e]);
+        const float zs = silu_grad_f(to_f<T>(sOwn[2][tid][e]), act);
+        du[e] = use ? __builtin_fmaf(sD[r][pc + e], into, skip * gy) : 0.f;
+        dd[e] = use ? __builtin_fmaf(u, into, kLn2 * sQ[r][pc + e]) * slope : 0.f;
+        dz[e] = use ? to_f<T>(sOwn[3][tid][e]) * __builtin_fmaf(skip, u, sY[r][pc + e]) * zs : 0.f;
+        dskip[e] += use ? gy * u : 0.f;
         ddb[e] += dd[e];
       }
-      const int64_t at = (t0 + k + r) * p.D + c0 + pc;
-      store_piece<T, V>(reinterpret_cast<T*>(p.du) + at, pleft, du);
-      store_piece<T, V>(reinterpret_cast<T*>(p.ddelta) + at, pleft, dd);
-      if (p.z) store_piece<T, V>(reinterpret_cast<T*>(p.dz) + at, pleft, dz);
-    }
-    for (int i = tid; i < TT * 2 * NP; i += kThreads) {
-      const int t = i / (2 * NP), w = i / NP & 1, n = i % NP;
-      if (k + t >= len || n >= p.N) continue;
-      float v = 0.f;
+      // a thread's values of the sums over the waves: (token, dB or dC, states)
+      constexpr int E = TT * 2 * NP / SL::kThr, kPerT = 2 * NP / E;
+      const int et = tid / kPerT, w = tid % kPerT * E / NP, n1 = tid % kPerT * E % NP;
+      float v[E];
 #pragma unroll
-      for (int m = 0; m < kWaves; ++m) v += w ? sdC[m][t][n] : sdB[m][t][n];
-      p.pBC[(((int64_t)blk * p.map.ntok + t0 + k + t) * 2 + w) * p.N + n] = v;
+      for (int e = 0; e < E; ++e) {
+        const float* from = &sBC[0][w][et][n1 + e];
+        v[e] = from[0];
+#pragma unroll
+        for (int m = 1; m < SL::kW; ++m) v[e] += from[m * 2 * TT * NP];
+      }
+      const int64_t first = (t0 + k) * a->D + c0, N = a->N;
+      float* part = a->pBC + (((int64_t)blk * a->map.ntok + t0 + k) * 2) * N;
+      T *pu = at<T>(a->du, first, fout), *pd = at<T>(a->ddelta, first, fout), *pz = at<T>(a->dz, first, fout);
+      if (k + r < len) {
+        if (nc == SL::kCB) {
+          store_piece<T, V, true>(pu, V, du);
+          store_piece<T, V, true>(pd, V, dd);
+          if (gated) store_piece<T, V, true>(pz, V, dz);
+        } else {
+          store_piece<T, V>(pu, pleft, du);
+          store_piece<T, V>(pd, pleft, dd);
+          if (gated) store_piece<T, V>(pz, pleft, dz);
+        }
+      }
+      if (k + et < len) {
+        if (N == NP) store_piece<float, E, true>(part + (et * 2 + w) * NP + n1, E, v);
+        else store_piece<float, E>(part + (et * 2 + w) * N + n1, (int)N - n1, v);
+      }
     }
   }
   if (live) store_piece<float, NS>(p.pA + ((int64_t)chunk * p.D + c) * p.N + n0, nleft, dA);
@@ -419,7 +546,7 @@ __global__ __launch_bounds__(kThreads) void ssm_bwd_kernel(SsmParams p) {
     sX[r][pc + e] = ddb[e];
   }
   __syncthreads();
-  for (int i = tid; i < 2 * nc; i += kThreads) {
+  for (int i = tid; i < 2 * nc; i += SL::kThr) {
     const int w = i / nc, cc = i % nc;
     float v = 0.f;
 #pragma unroll
@@ -446,11 +573,11 @@ __global__ __launch_bounds__(kThreads) void ssm_bc_kernel(SsmParams p) {
 template <typename T, typename SL> hipError_t backward(const SsmParams& p, hipStream_t stream) {
   const dim3 grid((uint32_t)(p.G * p.bpg * p.nchunk));
   if (p.map.seq ? p.nchunk > 1 : p.cps > 1) {
-    hipLaunchKernelGGL((ssm_rev_kernel<T, SL>), grid, dim3(kThreads), 0, stream, p);
+    hipLaunchKernelGGL((ssm_rev_kernel<T, SL>), grid, dim3(SL::kThr), 0, stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((ssm_bwd_kernel<T, SL>), grid, dim3(kThreads), 0, stream, p);
+  hipLaunchKernelGGL((ssm_bwd_kernel<T, SL>), grid, dim3(SL::kThr), 0, stream, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t per = p.map.ntok * 2 * p.N;

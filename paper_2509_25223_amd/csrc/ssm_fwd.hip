@@ -15,22 +15,11 @@ namespace rla {
 
 namespace {
 
-// The thread's own (token, piece), as loaded, of a tile of TT tokens x kCB channels.
-template <typename T, typename SL, int TT> struct SsmTileIo {
-  static constexpr int V = TT * SL::kCB / kThreads;      // channels a thread
-  static constexpr int kPer = SL::kCB / V;               // threads a token
-  static constexpr int VB = TT * SL::NP / kThreads ? TT * SL::NP / kThreads : 1;   // values of B, C
-  static constexpr int kPerB = SL::NP / VB;
-  typename RowVec<T, V>::type u, d, z;
-  typename RowVec<T, VB>::type b, c;
-  bool in;   // the token exists and belongs to a sequence
-};
-
 template <typename T, typename SL, bool SUMMARY>
-__global__ __launch_bounds__(kThreads) void ssm_fwd_kernel(SsmParams p) {
+__global__ __launch_bounds__(SL::kThr) void ssm_fwd_kernel(SsmParams p) {
   constexpr int NS = SL::NS, LPC = SL::LPC, NP = SL::NP, kRow = SL::kRow, TT = kSsmTile;
-  typedef SsmTileIo<T, SL, TT> Io;
-  constexpr int V = Io::V, VB = Io::VB;
+  typedef SsmStage<T, SL, TT, SUMMARY ? kStU | kStB : kStU | kStZ | kStB | kStC> St;
+  constexpr int V = St::V, VB = St::VB;
   __shared__ __attribute__((aligned(16))) float sD[TT][kRow], sX[TT][kRow], sY[SUMMARY ? 1 : TT][kRow];
   __shared__ __attribute__((aligned(16))) float sB[TT][NP], sC[SUMMARY ? 1 : TT][NP];
 
@@ -60,43 +49,27 @@ __global__ __launch_bounds__(kThreads) void ssm_fwd_kernel(SsmParams p) {
 #pragma unroll
   for (int n = 0; n < NS; ++n) A2[n] *= kLog2e;
   auto start_state = [&](int seq) {
-    if (p.h0 && seq >= 0) load_states<NS>(p.h0 + ((int64_t)seq * p.D + c) * p.N + n0, nleft, h);
-    else
+    if (p.h0 && seq >= 0) {
+      load_states<NS>(p.h0 + ((int64_t)seq * p.D + c) * p.N + n0, nleft, h);
+      settle(h);   // here, and not in every tile's turn of the code that follows
+    } else {
 #pragma unroll
       for (int n = 0; n < NS; ++n) h[n] = 0.f;
+    }
   };
   auto end_state = [&](int seq) {
     if (p.hfin && seq >= 0 && live) store_piece<float, NS>(p.hfin + ((int64_t)seq * p.D + c) * p.N + n0, nleft, h);
   };
 
-  // the thread's token and channels in a tile
-  const int r = tid / Io::kPer, pc = tid % Io::kPer * V, pleft = nc - pc;
-  const int rb = tid / Io::kPerB, pb = tid % Io::kPerB * VB, bleft = (int)p.N - pb;
-  const T* ug = reinterpret_cast<const T*>(p.u) + c0 + pc;
-  const T* dg = reinterpret_cast<const T*>(p.delta) + c0 + pc;
-  const T* zg = reinterpret_cast<const T*>(p.z) + c0 + pc;
-  const T* bg = reinterpret_cast<const T*>(p.B) + g * p.N + pb;
-  const T* cg = reinterpret_cast<const T*>(p.C) + g * p.N + pb;
+  St st;
+  const int r = St::r(), pc = St::pc(), rb = St::rb(), pb = St::pb(), pleft = nc - pc, bleft = (int)p.N - pb;
+  const uint32_t fout = (r * (uint32_t)p.D + pc) * (uint32_t)sizeof(T);
   float bias[V], skip[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) {
     bias[e] = p.dbias && e < pleft ? p.dbias[c0 + pc + e] : 0.f;
     skip[e] = p.skip && e < pleft ? p.skip[c0 + pc + e] : 0.f;
   }
-  auto load_tile = [&](int k, Io& io) {
-    const int64_t t = t0 + k + r, tb = t0 + k + rb;
-    io.in = k + r < len && (!p.map.seq || p.map.seq[t] >= 0);
-    if (k + r < len) {
-      load_raw<T, V>(ug + t * p.us, pleft, io.u);
-      load_raw<T, V>(dg + t * p.dts, pleft, io.d);
-      if (!SUMMARY && p.z) load_raw<T, V>(zg + t * p.zs, pleft, io.z);
-    }
-    if (rb < TT && k + rb < len) {
-      load_raw<T, VB>(bg + tb * p.bs, bleft, io.b);
-      if (!SUMMARY) load_raw<T, VB>(cg + tb * p.cs, bleft, io.c);
-    }
-  };
-
   // tiles from the one of the last start on (summary), or all
   const int k_first = SUMMARY && last > 0 ? last / TT * TT : 0;
   int seq = p.map.seq || p.h0 || p.hfin ? p.map.seq_of(t0) : 0;
@@ -121,99 +94,140 @@ __global__ __launch_bounds__(kThreads) void ssm_fwd_kernel(SsmParams p) {
       }
     }
   }
-  float total = 0.f;   // sum of the channel's steps (lanes q = 0)
+  float total = 0.f;   // sum of the channel's steps
+  float* const ck = p.ck;
 
-  Io cur;
-  load_tile(k_first, cur);
+  settle(A2);
+  settle(h);
+  settle(bias);
+  settle(skip);
+  const bool packed = p.map.seq != nullptr, sp = p.softplus != 0;
+  st.load(t0 + k_first, len - k_first, c0, g, nc);
   for (int k = k_first; k < len; k += TT) {
     // ---- this tile into LDS ----
-    const bool in = cur.in;
-    const typename RowVec<T, V>::type uu = cur.u, zz = cur.z;
+    const uint32_t valid = len - k >= TT ? ~0u : (1u << (len - k)) - 1u;
+    uint32_t bits = SUMMARY ? 0u : fresh_map(fresh_args()).start_bits(t0 + k) & valid;
+    if (k == 0) bits &= ~1u;   // the chunk's first token: its state is set
+    const bool in = st.inside(k, len, packed);
+    const typename St::Vec uu = st.u, zz = st.z;
     {
-      float s[V], x[V];
+      float s[V];
+      st.steps(bias, sp, s);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const float raw = to_f<T>(cur.d[e]) + bias[e];
         const bool use = in && e < pleft && (!SUMMARY || k + r >= last);
-        s[e] = use ? (p.softplus ? softplus_exact(raw) : raw) : 0.f;
-        x[e] = use ? s[e] * to_f<T>(cur.u[e]) : 0.f;
+        sD[r][pc + e] = use ? s[e] : 0.f;
+        sX[r][pc + e] = use ? s[e] * to_f<T>(st.u[e]) : 0.f;
       }
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        sD[r][pc + e] = s[e];
-        sX[r][pc + e] = x[e];
-      }
-      if (rb < TT) {
-        const bool inb = k + rb < len && (!p.map.seq || p.map.seq[t0 + k + rb] >= 0) && (!SUMMARY || k + rb >= last);
+      if (st.owns_b()) {
+        const bool inb = st.inside_b(k, len, packed) && (!SUMMARY || k + rb >= last);
 #pragma unroll
         for (int e = 0; e < VB; ++e) {
-          sB[rb][pb + e] = inb && e < bleft ? to_f<T>(cur.b[e]) : 0.f;
-          if (!SUMMARY) sC[rb][pb + e] = inb && e < bleft ? to_f<T>(cur.c[e]) : 0.f;
+          sB[rb][pb + e] = inb && e < bleft ? to_f<T>(st.b[e]) : 0.f;
+          if (!SUMMARY) sC[rb][pb + e] = inb && e < bleft ? to_f<T>(st.c[e]) : 0.f;
         }
       }
     }
     __syncthreads();
-    if (k + TT < len) load_tile(k + TT, cur);
+    if (k + TT < len) st.load(t0 + k + TT, len - k - TT, c0, g, nc);
 
-    // ---- the scan ----
-    const uint32_t valid = len - k >= TT ? ~0u : (1u << (len - k)) - 1u;
-    uint32_t bits = SUMMARY ? 0u : p.map.start_bits(t0 + k) & valid;
-    if (k == 0) bits &= ~1u;   // the chunk's first token: its state is set
-#pragma unroll 1
-    for (int i = 0; i < TT; i += 4) {
-      if (!SUMMARY && p.ck && (i & (kSsmSub - 1)) == 0 && k + i < len && live) {
-        const int64_t sub = (int64_t)chunk * (p.L / kSsmSub) + (k + i) / kSsmSub;
-        store_piece<float, NS, true>(p.ck + (sub * p.D + c) * NP + n0, NS, h);
+    // ---- the scan: four tokens at a time, the next four's values on their way ----
+    struct Four {
+      float d, x, b[4][NS], c[4][NS];
+    };
+    auto fetch = [&](int i, Four& f) {
+      f.d = sD[i + (q & 3)][ch];
+      f.x = sX[i + (q & 3)][ch];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+          f.b[j][n] = sB[i + j][n0 + n];
+          if (!SUMMARY) f.c[j][n] = sC[i + j][n0 + n];
+        }
+    };
+    auto scan4 = [&](auto STARTS, int i, const Four& f) {
+      if (!SUMMARY && ck && (i & (kSsmSub - 1)) == 0 && k + i < len && live) {
+        const int64_t sub = (int64_t)chunk * (fresh_args()->L / kSsmSub) + (k + i) / kSsmSub;
+        store_piece<float, NS, true>(ck + (sub * p.D + c) * NP + n0, NS, h);
       }
-      const float dv = sD[i + (q & 3)][ch], xv = sX[i + (q & 3)][ch];
-      float y[4];
-      if (SUMMARY) total += dv;
-      const uint32_t here = (bits >> i) & 15u;
-      auto token = [&](auto J) {
+      if (SUMMARY) total += f.d;
+      // in passes over the four tokens' states, each of independent instructions: one
+      // wave then keeps the ALU busy through their latencies
+      float e[4][NS], x[4][NS], y[4];
+      over4([&](auto J) {
         constexpr int j = decltype(J)::value;
-        if (!SUMMARY && here != 0 && (here >> j) & 1u) {
-          if (!(k == 0 && i + j == 0)) end_state(seq);
+        const float dj = quad_lane<j>(f.d);
+#pragma unroll
+        for (int n = 0; n < NS; ++n) e[j][n] = dj * A2[n];
+      });
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int n = 0; n < NS; ++n) e[j][n] = __builtin_amdgcn_exp2f(e[j][n]);
+      over4([&](auto J) {
+        constexpr int j = decltype(J)::value;
+        const float xj = quad_lane<j>(f.x);
+#pragma unroll
+        for (int n = 0; n < NS; ++n) x[j][n] = xj * f.b[j][n];
+      });
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (decltype(STARTS)::value && ((bits >> (i + j)) & 1u)) {
+          end_state(seq);
           seq = p.map.seq_of(t0 + k + i + j);
           start_state(seq);
         }
-        const float dj = quad_lane<j>(dv), xj = quad_lane<j>(xv);
-        float b[NS], cc[NS], acc = 0.f;
 #pragma unroll
-        for (int n = 0; n < NS; ++n) b[n] = sB[i + j][n0 + n];
-        if (!SUMMARY)
-#pragma unroll
-          for (int n = 0; n < NS; ++n) cc[n] = sC[i + j][n0 + n];
-#pragma unroll
-        for (int n = 0; n < NS; ++n) {
-          h[n] = __builtin_fmaf(__builtin_amdgcn_exp2f(dj * A2[n]), h[n], xj * b[n]);
-          if (!SUMMARY) acc = __builtin_fmaf(h[n], cc[n], acc);
-        }
-        y[j] = acc;
-      };
-      token(std::integral_constant<int, 0>());
-      token(std::integral_constant<int, 1>());
-      token(std::integral_constant<int, 2>());
-      token(std::integral_constant<int, 3>());
+        for (int n = 0; n < NS; ++n) x[j][n] = h[n] = __builtin_fmaf(e[j][n], h[n], x[j][n]);
+      }
       if (!SUMMARY) {
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[j] = n == 0 ? x[j][n] * f.c[j][n] : __builtin_fmaf(x[j][n], f.c[j][n], y[j]);
         const float yt = tokens_over_lanes<LPC>(y);
         if (q < 4) sY[i + q][ch] = yt;
       }
+    };
+    if (bits == 0) {
+      Four f[2];
+      fetch(0, f[0]);
+#pragma unroll
+      for (int i = 0; i < TT; i += 4) {
+        if (i + 4 < TT) fetch(i + 4, f[(i / 4 + 1) & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+        scan4(std::false_type(), i, f[(i / 4) & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < TT; i += 4) {
+        Four f;
+        fetch(i, f);
+        scan4(std::true_type(), i, f);
+      }
     }
+    st.settle();
     __syncthreads();
 
     // ---- skip, gate, store ----
     if (!SUMMARY && p.o && k + r < len) {   // (no outputs: the backward's recomputation)
+      const SsmArgs a = fresh_args();
+      const bool gated = a->z != nullptr;
       float y[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         y[e] = __builtin_fmaf(skip[e], to_f<T>(uu[e]), sY[r][pc + e]);
-        if (p.z) {
+        if (gated) {
           const float zf = to_f<T>(zz[e]);
           y[e] *= zf * sigmoid_fast(zf);
         }
         if (!in) y[e] = 0.f;
       }
-      store_piece<T, V>(reinterpret_cast<T*>(p.o) + (t0 + k + r) * p.D + c0 + pc, pleft, y);
+      store_piece<T, V>(at<T>(a->o, (t0 + k) * a->D + c0, fout), pleft, y);
     }
   }
   if constexpr (SUMMARY) {
@@ -240,7 +254,7 @@ __global__ __launch_bounds__(kThreads) void ssm_empty_kernel(const int32_t* empt
 // Single tokens.  A lane holds NS states of a channel through the call's tokens: the
 // states are read and written once, which is what the call costs (HBM).
 template <typename T, typename SL>
-__global__ __launch_bounds__(kThreads) void ssm_decode_kernel(SsmParams p) {
+__global__ __launch_bounds__(SL::kThr) void ssm_decode_kernel(SsmParams p) {
   constexpr int NS = SL::NS, LPC = SL::LPC;
   const int q = SL::q(), n0 = q * NS;
   const int64_t id = (int64_t)blockIdx.x * SL::kCB + SL::ch();   // (sequence, channel)
@@ -281,17 +295,17 @@ __global__ __launch_bounds__(kThreads) void ssm_decode_kernel(SsmParams p) {
 template <typename T, typename SL> hipError_t forward(const SsmParams& p, hipStream_t stream) {
   const dim3 grid((uint32_t)(p.G * p.bpg * p.nchunk));   // blocks of channels fastest: rows are contiguous
   if (p.map.seq ? p.nchunk > 1 : p.cps > 1) {
-    hipLaunchKernelGGL((ssm_fwd_kernel<T, SL, true>), grid, dim3(kThreads), 0, stream, p);
+    hipLaunchKernelGGL((ssm_fwd_kernel<T, SL, true>), grid, dim3(SL::kThr), 0, stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((ssm_fwd_kernel<T, SL, false>), grid, dim3(kThreads), 0, stream, p);
+  hipLaunchKernelGGL((ssm_fwd_kernel<T, SL, false>), grid, dim3(SL::kThr), 0, stream, p);
   return hipGetLastError();
 }
 template <typename T, typename SL> hipError_t decode(const SsmParams& p, hipStream_t stream) {
   const int64_t wgs = (p.map.nseq * p.D + SL::kCB - 1) / SL::kCB;
   if (wgs > INT32_MAX) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((ssm_decode_kernel<T, SL>), dim3((uint32_t)wgs), dim3(kThreads), 0, stream, p);
+  hipLaunchKernelGGL((ssm_decode_kernel<T, SL>), dim3((uint32_t)wgs), dim3(SL::kThr), 0, stream, p);
   return hipGetLastError();
 }
 
