@@ -128,6 +128,18 @@ __device__ __forceinline__ SsmArgs fresh_args() {
   return (SsmArgs)a;
 }
 
+// Waves that share a SIMD are served oldest first: one would run ahead to its end and
+// leave the other alone there, with half of the ALU idle.  A priority that falls with
+// the tile, modulo 4, keeps them within a few tiles of each other.
+__device__ __forceinline__ void even_pace(int tile) {
+  switch (tile & 3) {
+    case 0: __builtin_amdgcn_s_setprio(3); break;
+    case 1: __builtin_amdgcn_s_setprio(2); break;
+    case 2: __builtin_amdgcn_s_setprio(1); break;
+    default: __builtin_amdgcn_s_setprio(0);
+  }
+}
+
 // Loaded values have arrived here.  Without it a loop that uses values loaded in front
 // of it waits for every load at that use in each turn, the next tile's among them.
 template <int N> __device__ __forceinline__ void settle(float (&x)[N]) {

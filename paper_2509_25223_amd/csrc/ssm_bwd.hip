@@ -89,7 +89,9 @@ __global__ __launch_bounds__(SL::kThr) void ssm_rev_kernel(SsmParams p) {
   typedef SsmStage<T, SL, TT, kStO | kStZ | kStC> St;
   constexpr int V = St::V, VB = St::VB;
   __shared__ __attribute__((aligned(16))) float sD[TT][kRow], sG[TT][kRow], sC[TT][NP];
-  const int nblk = (int)p.G * p.bpg, chunk = (int)blockIdx.x / nblk, blk = (int)blockIdx.x - chunk * nblk;
+  const int nblk = (int)p.G * p.bpg, turn = (int)blockIdx.x / nblk, blk = (int)blockIdx.x - turn * nblk;
+  // (dense: all but a sequence's first chunk)
+  const int chunk = p.map.seq ? turn : turn / (p.cps - 1) * p.cps + turn % (p.cps - 1) + 1;
   const int g = blk / p.bpg;
   const int64_t c0 = g * p.Dg + (int64_t)(blk - g * p.bpg) * SL::kCB;
   const int nc = (int)min((int64_t)SL::kCB, (g + 1) * p.Dg - c0);
@@ -127,6 +129,7 @@ __global__ __launch_bounds__(SL::kThr) void ssm_rev_kernel(SsmParams p) {
   const bool packed = p.map.seq != nullptr, sp = p.softplus != 0, gated = p.z != nullptr;
   st.load(t0 + k_last, end - k_last, c0, g, nc);
   for (int k = k_last; k >= 0; k -= TT) {
+    even_pace((k_last - k) / TT);
     const bool in = st.inside(k, end, packed);
     float s[V];
     st.steps(bias, sp, s);
@@ -246,7 +249,10 @@ __global__ __launch_bounds__(SL::kThr, 2) void ssm_bwd_kernel(SsmParams p) {
     state_of(p.dhfin, seq, carry);
   } else {   // the chunks behind, up to the first that closes the sequence
     int cc = chunk + 1;
-    while (!(p.flags[cc] & kClosed)) ++cc;
+    if (p.map.seq)
+      while (!(p.flags[cc] & kClosed)) ++cc;
+    else
+      cc = chunk / p.cps * p.cps + p.cps - 1;
     load_states<NS>(p.E + ((int64_t)cc * p.D + c) * NP + n0, NS, carry);
     for (--cc; cc > chunk; --cc) {
       float s[NS];
@@ -285,6 +291,7 @@ __global__ __launch_bounds__(SL::kThr, 2) void ssm_bwd_kernel(SsmParams p) {
   load_tile(k_last);
   for (int k = k_last; k >= 0; k -= TT) {
     const SsmArgs a = fresh_args();
+    even_pace((k_last - k) / TT);
     // ---- these tokens into LDS ----
     const uint32_t valid = len - k >= TT ? (1u << TT) - 1u : (1u << (len - k)) - 1u;
     const uint32_t bits = fresh_map(a).start_bits(t0 + k) & valid;
@@ -572,8 +579,9 @@ __global__ __launch_bounds__(kThreads) void ssm_bc_kernel(SsmParams p) {
 
 template <typename T, typename SL> hipError_t backward(const SsmParams& p, hipStream_t stream) {
   const dim3 grid((uint32_t)(p.G * p.bpg * p.nchunk));
-  if (p.map.seq ? p.nchunk > 1 : p.cps > 1) {
-    hipLaunchKernelGGL((ssm_rev_kernel<T, SL>), grid, dim3(SL::kThr), 0, stream, p);
+  if (p.cps > 1) {
+    const dim3 part((uint32_t)(p.G * p.bpg * (p.map.seq ? p.nchunk : p.nchunk / p.cps * (p.cps - 1))));
+    hipLaunchKernelGGL((ssm_rev_kernel<T, SL>), part, dim3(SL::kThr), 0, stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

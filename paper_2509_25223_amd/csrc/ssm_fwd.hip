@@ -24,7 +24,9 @@ __global__ __launch_bounds__(SL::kThr) void ssm_fwd_kernel(SsmParams p) {
   __shared__ __attribute__((aligned(16))) float sB[TT][NP], sC[SUMMARY ? 1 : TT][NP];
 
   const int tid = threadIdx.x;
-  const int nblk = (int)p.G * p.bpg, chunk = (int)blockIdx.x / nblk, blk = (int)blockIdx.x - chunk * nblk;
+  const int nblk = (int)p.G * p.bpg, turn = (int)blockIdx.x / nblk, blk = (int)blockIdx.x - turn * nblk;
+  // (dense summaries: all but a sequence's last chunk)
+  const int chunk = SUMMARY && !p.map.seq ? turn / (p.cps - 1) * p.cps + turn % (p.cps - 1) : turn;
   const int g = blk / p.bpg;
   const int64_t c0 = g * p.Dg + (int64_t)(blk - g * p.bpg) * SL::kCB;   // first channel
   const int nc = (int)min((int64_t)SL::kCB, (g + 1) * p.Dg - c0);
@@ -34,7 +36,7 @@ __global__ __launch_bounds__(SL::kThr) void ssm_fwd_kernel(SsmParams p) {
   int last, first;
   chunk_starts(p, t0, len, last, first);
   if constexpr (SUMMARY) {
-    if (blk == 0 && tid == 0) p.flags[chunk] = (last >= 0 ? kHasStart : 0) | (first <= len ? kClosed : 0);
+    if (blk == 0 && tid == 0 && p.map.seq) p.flags[chunk] = (last >= 0 ? kHasStart : 0) | (first <= len ? kClosed : 0);
     if (first == len || (p.map.seq && t0 + len >= p.map.ntok)) return;   // nothing continues behind it
     if (p.map.seq && first < len && p.map.start_bits(t0 + len) & 1u) return;
   }
@@ -80,7 +82,10 @@ __global__ __launch_bounds__(SL::kThr) void ssm_fwd_kernel(SsmParams p) {
     start_state(seq);
   } else {   // the chunks before, from the last one with a start on
     int cc = chunk - 1;
-    while (!(p.flags[cc] & kHasStart)) --cc;
+    if (p.map.seq)
+      while (!(p.flags[cc] & kHasStart)) --cc;
+    else
+      cc = chunk / p.cps * p.cps;
     load_states<NS>(p.S + ((int64_t)cc * p.D + c) * NP + n0, NS, h);
     for (++cc; cc < chunk; ++cc) {
       float s[NS];
@@ -104,6 +109,7 @@ __global__ __launch_bounds__(SL::kThr) void ssm_fwd_kernel(SsmParams p) {
   const bool packed = p.map.seq != nullptr, sp = p.softplus != 0;
   st.load(t0 + k_first, len - k_first, c0, g, nc);
   for (int k = k_first; k < len; k += TT) {
+    even_pace(k / TT);
     // ---- this tile into LDS ----
     const uint32_t valid = len - k >= TT ? ~0u : (1u << (len - k)) - 1u;
     uint32_t bits = SUMMARY ? 0u : fresh_map(fresh_args()).start_bits(t0 + k) & valid;
@@ -294,8 +300,9 @@ __global__ __launch_bounds__(SL::kThr) void ssm_decode_kernel(SsmParams p) {
 
 template <typename T, typename SL> hipError_t forward(const SsmParams& p, hipStream_t stream) {
   const dim3 grid((uint32_t)(p.G * p.bpg * p.nchunk));   // blocks of channels fastest: rows are contiguous
-  if (p.map.seq ? p.nchunk > 1 : p.cps > 1) {
-    hipLaunchKernelGGL((ssm_fwd_kernel<T, SL, true>), grid, dim3(SL::kThr), 0, stream, p);
+  if (p.cps > 1) {
+    const dim3 part((uint32_t)(p.G * p.bpg * (p.map.seq ? p.nchunk : p.nchunk / p.cps * (p.cps - 1))));
+    hipLaunchKernelGGL((ssm_fwd_kernel<T, SL, true>), part, dim3(SL::kThr), 0, stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
