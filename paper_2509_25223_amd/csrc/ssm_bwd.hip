@@ -236,7 +236,8 @@ __global__ __launch_bounds__(SL::kThr, 2) void ssm_bwd_kernel(SsmParams p) {
   }
   auto state_of = [&](const float* base, int seq, float (&h)[NS]) {
     if (base && seq >= 0) {
-      load_states<NS>(base + ((int64_t)seq * p.D + c) * p.N + n0, nleft, h);
+      const SsmArgs a = fresh_args();
+      load_states<NS>(base + ((int64_t)seq * a->D + c) * a->N + n0, nleft, h);
       settle(h);   // here, and not in every tile's turn of the code that follows
     } else {
 #pragma unroll
@@ -417,25 +418,21 @@ __global__ __launch_bounds__(SL::kThr, 2) void ssm_bwd_kernel(SsmParams p) {
         float oB[CS::kKeep], oC[CS::kKeep];
         CS::run(v, oC);
         __builtin_amdgcn_sched_barrier(0);
-        // dh: what reaches each token from behind, x[j] = C dy first
+        // dh of each token, from behind
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
           for (int n = 0; n < NS; ++n) x[j][n] = sC[i + j][n0 + n];
         over4([&](auto J) {
-          constexpr int j = decltype(J)::value;
+          constexpr int j = 3 - decltype(J)::value;
           const float gj = quad_lane<j>(gv);
-#pragma unroll
-          for (int n = 0; n < NS; ++n) x[j][n] *= gj;
-        });
-#pragma unroll
-        for (int j = 3; j >= 0; --j)
           if (inside(i + j))
 #pragma unroll
             for (int n = 0; n < NS; ++n) {
-              x[j][n] += carry[n];
+              x[j][n] = __builtin_fmaf(gj, x[j][n], carry[n]);
               carry[n] = x[j][n] * decay[i + j][n];
             }
+        });
         __builtin_amdgcn_sched_barrier(0);
         float into[4], qa[4];
         over4([&](auto J) {
@@ -486,9 +483,11 @@ __global__ __launch_bounds__(SL::kThr, 2) void ssm_bwd_kernel(SsmParams p) {
       if (lo == 0 && hi == TT) stretch(std::true_type(), lo, hi);
       else stretch(std::false_type(), lo, hi);
       if (starts) {   // what flows out is the initial state's; in front, another sequence ends
-        const int sq = p.map.seq_of(t);
+        const SsmArgs a = fresh_args();
+        const TokenMap map = fresh_map(a);
+        const int sq = map.seq_of(t);
         if (a->dh0 && live && sq >= 0) store_piece<float, NS>(a->dh0 + ((int64_t)sq * a->D + c) * a->N + n0, nleft, carry);
-        state_of(a->dhfin, k + lo > 0 ? p.map.seq_of(t - 1) : -1, carry);
+        state_of(a->dhfin, k + lo > 0 ? map.seq_of(t - 1) : -1, carry);
       }
       hi = lo;
     }
