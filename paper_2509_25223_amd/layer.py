@@ -13,8 +13,11 @@ and the scan's states are fp32.  Outputs and workspaces are allocated (on
 from __future__ import annotations
 
 import ctypes
+import functools
 
-from . import RLA_BF16, RLA_F32, RLA_OK, RLAError, _ptr, _stream_handle, _torch, load_library
+from . import RLA_BF16, RLA_F32, RLA_OK, RLAError, load_library
+
+torch = None   # imported with the library, on the first call
 
 RLA_SSM_FORWARD, RLA_SSM_BACKWARD = 0, 1
 
@@ -58,14 +61,17 @@ _PROBLEMS = {"conv": rla_conv_problem, "ssm": rla_ssm_problem, "addnorm": rla_ad
              "gatenorm": rla_gatenorm_problem}
 
 
-_bound = None
+_bound = _stream_of = None
 
 
 def _lib():
     """The library with this header's functions typed."""
-    global _bound
+    global _bound, torch, _stream_of
     if _bound is not None:
         return _bound
+    import torch as module
+    torch = module
+    _stream_of = torch._C._cuda_getCurrentRawStream   # of a device, without its object
     lib = load_library()
     for op, problem in _PROBLEMS.items():
         size = getattr(lib, "rla_%s_workspace_size" % op)
@@ -87,11 +93,19 @@ def _lib():
 
 
 # ---------------------------------------------------------------------------
-# checks
+# checks.  A call of a few tokens is bound by the host, so each tensor is looked at
+# once, cheaply; the checks that name what is wrong run where that look fails.
 # ---------------------------------------------------------------------------
 
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _stream_handle(stream, index):
+    return _stream_of(index) if stream is None else stream.cuda_stream
+
+
 def _code(name, dt):
-    torch = _torch()
     if dt is torch.bfloat16:
         return RLA_BF16
     if dt is torch.float32:
@@ -114,7 +128,7 @@ def _need(**given):
 
 def _check(name, t, index, shape, dtype):
     """A contiguous tensor of exactly this device, shape and type (None passes)."""
-    if t is None:
+    if t is None or (t.shape == shape and t.dtype is dtype and t.get_device() == index and t.is_contiguous()):
         return
     if t.shape != shape:
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
@@ -122,8 +136,7 @@ def _check(name, t, index, shape, dtype):
         raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
     if t.get_device() != index:
         raise ValueError("%s must be on GPU %d" % (name, index))
-    if not t.is_contiguous():
-        raise ValueError("%s must be contiguous" % name)
+    raise ValueError("%s must be contiguous" % name)
 
 
 def _rows(name, t, index, shape, lead, dtype):
@@ -132,11 +145,11 @@ def _rows(name, t, index, shape, lead, dtype):
     spaced over all tokens."""
     if t is None:
         return 0
-    if t.shape != shape:
-        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
-    if t.dtype is not dtype:
-        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
-    if t.get_device() != index:
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index:
+        if t.shape != shape:
+            raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+        if t.dtype is not dtype:
+            raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
         raise ValueError("%s must be on GPU %d" % (name, index))
     if t.is_contiguous():
         return 0
@@ -159,13 +172,20 @@ def _rows(name, t, index, shape, lead, dtype):
     return step
 
 
+# problems by their sizes (never changed after): building one costs as much as passing it
+_conv_problem = functools.lru_cache(256)(rla_conv_problem)
+_ssm_problem = functools.lru_cache(256)(rla_ssm_problem)
+_addnorm_problem = functools.lru_cache(256)(rla_addnorm_problem)
+_gatenorm_problem = functools.lru_cache(256)(rla_gatenorm_problem)
+
+
 def _cu(cu_seqlens, index, lead):
     """(pointer, N) of packed sequences."""
     if cu_seqlens is None:
         return None, 0
     if len(lead) == 2 and lead[0] != 1:
         raise ValueError("cu_seqlens requires packed tokens")
-    if cu_seqlens.dtype is not _torch().int32 or cu_seqlens.get_device() != index:
+    if cu_seqlens.dtype is not torch.int32 or cu_seqlens.get_device() != index:
         raise TypeError("cu_seqlens must be an int32 tensor on GPU %d" % index)
     if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 1 or not cu_seqlens.is_contiguous():
         raise ValueError("cu_seqlens must be contiguous [N + 1]")
@@ -183,7 +203,6 @@ def _tokens(name, t, inner):
 
 
 def _new(like, shape, dtype, stream):
-    torch = _torch()
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=like.device)
     with torch.cuda.stream(stream):   # memory of the stream that uses it
@@ -192,7 +211,7 @@ def _new(like, shape, dtype, stream):
 
 def _space(like, need, workspace, stream):
     if workspace is None:
-        workspace = _new(like, max(need, 1), _torch().uint8, stream)
+        workspace = _new(like, max(need, 1), torch.uint8, stream)
     elif workspace.get_device() != like.get_device() or not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous and on %s" % like.device)
     have = workspace.numel() * workspace.element_size()
@@ -222,8 +241,8 @@ def _gradients(grads, index, expected):
 # ---------------------------------------------------------------------------
 
 def _conv(x, weight, bias, silu, cu_seqlens, dy=None):
-    torch = _torch()
-    _need(x=x, weight=weight)
+    if x is None or weight is None:
+        _need(x=x, weight=weight)
     index = _device("x", x)
     B, T, lead = _tokens("x", x, 1)
     D = x.shape[-1]
@@ -236,13 +255,15 @@ def _conv(x, weight, bias, silu, cu_seqlens, dy=None):
     cu, n = _cu(cu_seqlens, index, lead)
     xs = _rows("x", x, index, x.shape, len(lead), x.dtype)
     ds = _rows("dy", dy, index, x.shape, len(lead), x.dtype)
-    problem = rla_conv_problem(B, T, D, n, cu, xs, ds, taps, 1 if silu else 0, dtype)
+    make = _conv_problem if cu is None else rla_conv_problem
+    problem = make(B, T, D, n, cu, xs, ds, taps, 1 if silu else 0, dtype)
     return problem, index, ((B if cu is None else n), taps - 1, D)
 
 
 def make_conv_problem(x, weight, cu_seqlens=None, silu=False) -> rla_conv_problem:
     """rla_conv_problem for x [B, T, D] / [T, D] and weight [D, taps]."""
-    return _conv(x, weight, None, silu, cu_seqlens)[0]
+    _lib()
+    return rla_conv_problem.from_buffer_copy(_conv(x, weight, None, silu, cu_seqlens)[0])
 
 
 def rla_conv_workspace_size(problem: rla_conv_problem, backward: bool = True) -> int:
@@ -269,7 +290,7 @@ def rla_conv_forward(x, weight, bias=None, silu=False, state=None, cu_seqlens=No
     if cu_seqlens is not None:
         ws, have = _space(x, lib.rla_conv_workspace_size(problem, 0), workspace, stream)
     _ok(lib.rla_conv_forward(problem, x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(state), out.data_ptr(),
-                             _ptr(state_final), _ptr(ws), have, _stream_handle(stream)), "rla_conv_forward")
+                             _ptr(state_final), _ptr(ws), have, _stream_handle(stream, index)), "rla_conv_forward")
     return out, state_final
 
 
@@ -277,7 +298,6 @@ def rla_conv_backward(x, weight, dy, bias=None, silu=False, state=None, dstate_f
                       grads=None, workspace=None, stream=None):
     """Gradients of <dy, y> + <dstate_final, state_final> for rla_conv_forward:
     a dict of dx, dweight, dbias (with a bias) and dstate (with a state)."""
-    torch = _torch()
     lib = _lib()
     problem, index, shape = _conv(x, weight, bias, silu, cu_seqlens, dy)
     if dy is None:
@@ -297,7 +317,7 @@ def rla_conv_backward(x, weight, dy, bias=None, silu=False, state=None, dstate_f
     _ok(lib.rla_conv_backward(problem, x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(state), dy.data_ptr(),
                               _ptr(dstate_final), grads["dx"].data_ptr(), grads["dweight"].data_ptr(),
                               _ptr(grads.get("dbias")), _ptr(grads.get("dstate")), ws.data_ptr(), have,
-                              _stream_handle(stream)), "rla_conv_backward")
+                              _stream_handle(stream, index)), "rla_conv_backward")
     return grads
 
 
@@ -316,7 +336,7 @@ def rla_conv_decode(x, weight, bias=None, silu=False, state=None, state_out=None
     if state_out is None:
         state_out = _new(x, shape, x.dtype, stream)
     _ok(lib.rla_conv_decode(problem, x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(state), out.data_ptr(),
-                            state_out.data_ptr(), _stream_handle(stream)), "rla_conv_decode")
+                            state_out.data_ptr(), _stream_handle(stream, index)), "rla_conv_decode")
     return out, state_out
 
 
@@ -325,8 +345,8 @@ def rla_conv_decode(x, weight, bias=None, silu=False, state=None, state_out=None
 # ---------------------------------------------------------------------------
 
 def _ssm(u, delta, A, B, C, D, z, delta_bias, softplus, cu_seqlens, dO=None):
-    torch = _torch()
-    _need(u=u, delta=delta, A=A, B=B, C=C)
+    if u is None or delta is None or A is None or B is None or C is None:
+        _need(u=u, delta=delta, A=A, B=B, C=C)
     index = _device("u", u)
     nb, T, lead = _tokens("u", u, 1)
     width, k, dt = u.shape[-1], len(lead), u.dtype
@@ -353,15 +373,16 @@ def _ssm(u, delta, A, B, C, D, z, delta_bias, softplus, cu_seqlens, dO=None):
     _check("D", D, index, (width,), torch.float32)
     _check("delta_bias", delta_bias, index, (width,), torch.float32)
     cu, n = _cu(cu_seqlens, index, lead)
-    problem = rla_ssm_problem(nb, T, width, states, groups, n, cu, us, ds, zs, os_, bs, cs, 1 if softplus else 0,
-                              dtype)
+    make = _ssm_problem if cu is None else rla_ssm_problem
+    problem = make(nb, T, width, states, groups, n, cu, us, ds, zs, os_, bs, cs, 1 if softplus else 0, dtype)
     return problem, index, ((nb if cu is None else n), width, states)
 
 
 def make_ssm_problem(u, A, B, cu_seqlens=None, softplus=True) -> rla_ssm_problem:
     """rla_ssm_problem for u [B, T, D] / [T, D], A [D, states] and B [..., groups,
     states] (sizes only: what a workspace depends on)."""
-    return _ssm(u, u, A, B, B, None, None, None, softplus, cu_seqlens)[0]
+    _lib()
+    return rla_ssm_problem.from_buffer_copy(_ssm(u, u, A, B, B, None, None, None, softplus, cu_seqlens)[0])
 
 
 def rla_ssm_workspace_size(problem: rla_ssm_problem, op: int) -> int:
@@ -377,7 +398,7 @@ def rla_ssm_forward(u, delta, A, B, C, D=None, z=None, delta_bias=None, softplus
     (of RLA_SSM_BACKWARD's size) keeps what rla_ssm_backward(use_saved=True) reads."""
     lib = _lib()
     problem, index, shape = _ssm(u, delta, A, B, C, D, z, delta_bias, softplus, cu_seqlens)
-    f32 = _torch().float32
+    f32 = torch.float32
     _check("h0", h0, index, shape, f32)
     _check("out", out, index, u.shape, u.dtype)
     _check("h_final", h_final, index, shape, f32)
@@ -391,7 +412,7 @@ def rla_ssm_forward(u, delta, A, B, C, D=None, z=None, delta_bias=None, softplus
     ws, have = _space(u, lib.rla_ssm_workspace_size(problem, op), workspace, stream)
     _ok(lib.rla_ssm_forward(problem, u.data_ptr(), delta.data_ptr(), A.data_ptr(), B.data_ptr(), C.data_ptr(),
                             _ptr(D), _ptr(z), _ptr(delta_bias), _ptr(h0), out.data_ptr(), _ptr(h_final),
-                            1 if save_for_backward else 0, ws.data_ptr(), have, _stream_handle(stream)),
+                            1 if save_for_backward else 0, ws.data_ptr(), have, _stream_handle(stream, index)),
         "rla_ssm_forward")
     return out, h_final
 
@@ -408,7 +429,7 @@ def rla_ssm_backward(u, delta, A, B, C, dO, D=None, z=None, delta_bias=None, sof
     if use_saved and workspace is None:
         raise ValueError("use_saved needs the workspace of the saving forward call")
     problem, index, shape = _ssm(u, delta, A, B, C, D, z, delta_bias, softplus, cu_seqlens, dO)
-    f32 = _torch().float32
+    f32 = torch.float32
     _check("h0", h0, index, shape, f32)
     _check("dh_final", dh_final, index, shape, f32)
     expected = {"du": (u.shape, u.dtype), "ddelta": (u.shape, u.dtype), "dA": (A.shape, f32),
@@ -431,7 +452,7 @@ def rla_ssm_backward(u, delta, A, B, C, dO, D=None, z=None, delta_bias=None, sof
                              _ptr(D), _ptr(z), _ptr(delta_bias), _ptr(h0), dO.data_ptr(), _ptr(dh_final),
                              g["du"].data_ptr(), g["ddelta"].data_ptr(), g["dA"].data_ptr(), g["dB"].data_ptr(),
                              g["dC"].data_ptr(), _ptr(g.get("dD")), _ptr(g.get("dz")), _ptr(g.get("ddelta_bias")),
-                             _ptr(g.get("dh0")), 1 if use_saved else 0, ws.data_ptr(), have, _stream_handle(stream)),
+                             _ptr(g.get("dh0")), 1 if use_saved else 0, ws.data_ptr(), have, _stream_handle(stream, index)),
         "rla_ssm_backward")
     return grads
 
@@ -444,7 +465,7 @@ def rla_ssm_decode(u, delta, A, B, C, D=None, z=None, delta_bias=None, softplus=
     if u.dim() != 3:
         raise ValueError("u must be [B, T, D]")
     problem, index, shape = _ssm(u, delta, A, B, C, D, z, delta_bias, softplus, None)
-    f32 = _torch().float32
+    f32 = torch.float32
     _check("h_in", h_in, index, shape, f32)
     _check("h_out", h_out, index, shape, f32)
     _check("out", out, index, u.shape, u.dtype)
@@ -454,7 +475,7 @@ def rla_ssm_decode(u, delta, A, B, C, D=None, z=None, delta_bias=None, softplus=
         h_out = _new(u, shape, f32, stream)
     _ok(lib.rla_ssm_decode(problem, u.data_ptr(), delta.data_ptr(), A.data_ptr(), B.data_ptr(), C.data_ptr(),
                            _ptr(D), _ptr(z), _ptr(delta_bias), _ptr(h_in), out.data_ptr(), h_out.data_ptr(),
-                           _stream_handle(stream)), "rla_ssm_decode")
+                           _stream_handle(stream, index)), "rla_ssm_decode")
     return out, h_out
 
 
@@ -464,7 +485,8 @@ def rla_ssm_decode(u, delta, A, B, C, D=None, z=None, delta_bias=None, softplus=
 
 def _addnorm(x, residual_dtype, eps, dn=None, name="x"):
     """`x`: the block's output, or (backward without a scale) its stand-in dn."""
-    _need(**{name: x})
+    if x is None:
+        raise ValueError("%s is required" % name)
     if x.dim() < 1:
         raise ValueError("%s must have rows" % name)
     index = _device(name, x)
@@ -474,12 +496,13 @@ def _addnorm(x, residual_dtype, eps, dn=None, name="x"):
     xs = _rows(name, x, index, x.shape, lead, x.dtype)
     ds = _rows("dn", dn, index, x.shape, lead, x.dtype)
     width = x.shape[-1]
-    return rla_addnorm_problem(x.numel() // width if width else 0, width, xs, ds, dtype, rd, eps), index
+    return _addnorm_problem(x.numel() // width if width else 0, width, xs, ds, dtype, rd, eps), index
 
 
 def make_addnorm_problem(x, residual_dtype, eps=1e-6) -> rla_addnorm_problem:
     """rla_addnorm_problem for x [.., D] and a residual stream of that type."""
-    return _addnorm(x, residual_dtype, eps)[0]
+    _lib()
+    return rla_addnorm_problem.from_buffer_copy(_addnorm(x, residual_dtype, eps)[0])
 
 
 def rla_addnorm_workspace_size(problem: rla_addnorm_problem) -> int:
@@ -493,13 +516,13 @@ def rla_addnorm_forward(x, weight, residual=None, scale=None, eps=1e-6, out=None
     dimension.  residual None: 0; scale [D] None: 1.  The stream is of residual's
     type (without one: residual_dtype, fp32 by default).  Returns (n, residual_out);
     residual_out=residual updates in place."""
-    torch = _torch()
     lib = _lib()
     rd = residual.dtype if residual is not None else residual_out.dtype if residual_out is not None else \
         torch.float32 if residual_dtype is None else residual_dtype
     problem, index = _addnorm(x, rd, eps)
     D = x.shape[-1]
-    _need(weight=weight)
+    if weight is None:
+        _need(weight=weight)
     _check("weight", weight, index, (D,), torch.float32)
     _check("scale", scale, index, (D,), torch.float32)
     _check("residual", residual, index, x.shape, rd)
@@ -510,7 +533,7 @@ def rla_addnorm_forward(x, weight, residual=None, scale=None, eps=1e-6, out=None
     if residual_out is None:
         residual_out = _new(x, x.shape, rd, stream)
     _ok(lib.rla_addnorm_forward(problem, x.data_ptr(), _ptr(residual), weight.data_ptr(), _ptr(scale), out.data_ptr(),
-                                residual_out.data_ptr(), _stream_handle(stream)), "rla_addnorm_forward")
+                                residual_out.data_ptr(), _stream_handle(stream, index)), "rla_addnorm_forward")
     return out, residual_out
 
 
@@ -520,7 +543,6 @@ def rla_addnorm_backward(dn, residual_out, weight, x=None, scale=None, dresidual
     from the stream that it left: a dict of dx, dresidual (of the stream's type),
     dweight, and dscale where scale is given (x is needed then).
     grads["dresidual"] may be dresidual_out."""
-    torch = _torch()
     lib = _lib()
     _need(dn=dn, residual_out=residual_out, weight=weight)
     if scale is not None and x is None:
@@ -544,13 +566,13 @@ def rla_addnorm_backward(dn, residual_out, weight, x=None, scale=None, dresidual
     _ok(lib.rla_addnorm_backward(problem, dn.data_ptr(), _ptr(dresidual_out), residual_out.data_ptr(), _ptr(x),
                                  weight.data_ptr(), _ptr(scale), grads["dx"].data_ptr(), grads["dresidual"].data_ptr(),
                                  grads["dweight"].data_ptr(), _ptr(grads.get("dscale")), ws.data_ptr(), have,
-                                 _stream_handle(stream)), "rla_addnorm_backward")
+                                 _stream_handle(stream, index)), "rla_addnorm_backward")
     return grads
 
 
 def _gatenorm(x, gate, weight, gate_first, eps, dO=None):
-    torch = _torch()
-    _need(x=x, gate=gate, weight=weight)
+    if x is None or gate is None or weight is None:
+        _need(x=x, gate=gate, weight=weight)
     if x.dim() < 2:
         raise ValueError("x must be [.., heads, width]")
     index = _device("x", x)
@@ -563,14 +585,15 @@ def _gatenorm(x, gate, weight, gate_first, eps, dO=None):
     per_head = weight.dim() == 2
     _check("weight", weight, index, (H, d) if per_head else (d,), torch.float32)
     tokens = x.numel() // (H * d) if H * d else 0
-    return rla_gatenorm_problem(tokens, H, d, xs, gs, ds, dtype, xd, 1 if gate_first else 0, 1 if per_head else 0,
-                                eps), index
+    return _gatenorm_problem(tokens, H, d, xs, gs, ds, dtype, xd, 1 if gate_first else 0, 1 if per_head else 0,
+                             eps), index
 
 
 def make_gatenorm_problem(x, gate, weight, gate_first=False, eps=1e-6) -> rla_gatenorm_problem:
     """rla_gatenorm_problem for x, gate [.., heads, width] and weight [width] or
     [heads, width]."""
-    return _gatenorm(x, gate, weight, gate_first, eps)[0]
+    _lib()
+    return rla_gatenorm_problem.from_buffer_copy(_gatenorm(x, gate, weight, gate_first, eps)[0])
 
 
 def rla_gatenorm_workspace_size(problem: rla_gatenorm_problem) -> int:
@@ -588,7 +611,7 @@ def rla_gatenorm_forward(x, gate, weight, gate_first=False, eps=1e-6, out=None, 
     if out is None:
         out = _new(x, x.shape, gate.dtype, stream)
     _ok(lib.rla_gatenorm_forward(problem, x.data_ptr(), gate.data_ptr(), weight.data_ptr(), out.data_ptr(),
-                                 _stream_handle(stream)), "rla_gatenorm_forward")
+                                 _stream_handle(stream, index)), "rla_gatenorm_forward")
     return out
 
 
@@ -607,5 +630,5 @@ def rla_gatenorm_backward(dO, x, gate, weight, gate_first=False, eps=1e-6, grads
     ws, have = _space(x, lib.rla_gatenorm_workspace_size(problem), workspace, stream)
     _ok(lib.rla_gatenorm_backward(problem, dO.data_ptr(), x.data_ptr(), gate.data_ptr(), weight.data_ptr(),
                                   grads["dx"].data_ptr(), grads["dgate"].data_ptr(), grads["dweight"].data_ptr(),
-                                  ws.data_ptr(), have, _stream_handle(stream)), "rla_gatenorm_backward")
+                                  ws.data_ptr(), have, _stream_handle(stream, index)), "rla_gatenorm_backward")
     return grads
