@@ -73,7 +73,9 @@ __device__ __forceinline__ void load_state_window(const ConvParams& p, int n, in
   for (int j = 0; j < W - 1; ++j) load_state<T, W, V, FULL>(p.state0, n, W - 2 - j, p.D, c, left, win[j]);
 }
 
-template <typename T, int W, int TT, bool FULL>
+template <bool SILU> __device__ __forceinline__ float activation(float s) { return SILU ? s * sigmoid_fast(s) : s; }
+
+template <typename T, int W, int TT, bool SILU, bool NT, bool FULL>
 __device__ __forceinline__ void conv_fwd_stretch(const ConvParams& p, int64_t t0, int64_t c, int left) {
   constexpr int V = kPiece<T>;
   const T* x = reinterpret_cast<const T*>(p.x);
@@ -88,10 +90,9 @@ __device__ __forceinline__ void conv_fwd_stretch(const ConvParams& p, int64_t t0
     float o[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      const float s = tap_sum<W, V>(w, bias[e], e, xv[e], win);
-      o[e] = p.silu ? s * sigmoid_fast(s) : s;
+      o[e] = activation<SILU>(tap_sum<W, V>(w, bias[e], e, xv[e], win));
     }
-    store_piece<T, V, FULL>(y + t * p.D + c, left, o);
+    store_piece<T, V, FULL, NT>(y + t * p.D + c, left, o);
 #pragma unroll
     for (int j = W - 2; j > 0; --j)
 #pragma unroll
@@ -99,17 +100,24 @@ __device__ __forceinline__ void conv_fwd_stretch(const ConvParams& p, int64_t t0
 #pragma unroll
     for (int e = 0; e < V; ++e) win[0][e] = xv[e];
   };
-  // no start behind the first token: one sequence, all loads ahead
+  // no start behind the first token: one sequence, loads a batch ahead of their use
   if (t0 + TT <= p.map.ntok && (bits & (((1u << TT) - 1u) << 1)) == 0 && n >= 0) {
-    typename RowVec<T, V>::type raw[TT];
+    constexpr int U = TT < 8 ? TT : 8;
+    typename RowVec<T, V>::type raw[2][U];
 #pragma unroll
-    for (int k = 0; k < TT; ++k) load_raw<T, V, FULL>(x + (t0 + k) * p.xs + c, left, raw[k]);
+    for (int k = 0; k < U; ++k) load_raw<T, V, FULL>(x + (t0 + k) * p.xs + c, left, raw[0][k]);
 #pragma unroll
-    for (int k = 0; k < TT; ++k) {
-      float xv[V];
+    for (int k0 = 0; k0 < TT; k0 += U) {
+      if (k0 + U < TT)
 #pragma unroll
-      for (int e = 0; e < V; ++e) xv[e] = to_f<T>(raw[k][e]);
-      token(xv, t0 + k);
+        for (int k = 0; k < U; ++k) load_raw<T, V, FULL>(x + (t0 + k0 + U + k) * p.xs + c, left, raw[(k0 / U + 1) & 1][k]);
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        float xv[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) xv[e] = to_f<T>(raw[k0 / U & 1][k][e]);
+        token(xv, t0 + k0 + k);
+      }
     }
     return;
   }
@@ -151,7 +159,7 @@ __device__ __forceinline__ void copy_empty_states(const ConvParams& p, const voi
 
 constexpr uint32_t kEmptyWgs = 32;
 
-template <typename T, int W, int TT>
+template <typename T, int W, int TT, bool SILU, bool NT>
 __global__ __launch_bounds__(kThreads) void conv_fwd_kernel(ConvParams p, uint32_t pieces, uint32_t count,
                                                             uint32_t main_wgs) {
   constexpr int V = kPiece<T>;
@@ -163,13 +171,15 @@ __global__ __launch_bounds__(kThreads) void conv_fwd_kernel(ConvParams p, uint32
   if (id >= count) return;
   const int64_t t0 = (int64_t)(id / pieces) * TT, c = (int64_t)(id % pieces) * V;
   const int left = (int)min(p.D - c, (int64_t)V);
-  if (left == V) conv_fwd_stretch<T, W, TT, true>(p, t0, c, left);
-  else conv_fwd_stretch<T, W, TT, false>(p, t0, c, left);
+  if (left == V) conv_fwd_stretch<T, W, TT, SILU, NT, true>(p, t0, c, left);
+  else conv_fwd_stretch<T, W, TT, SILU, NT, false>(p, t0, c, left);
 }
 
 // Single tokens: a thread owns a piece of one sequence, loads its state before it
-// writes any (in place works).
-template <typename T, int W>
+// writes any (in place works).  256 sequences x 6144 channels of bf16, four taps: 8.8 us
+// for 25 MB, of which 3.6 is what a launch with one round of loads takes; two sequences
+// a thread, whose taps come once: 8.9.
+template <typename T, int W, bool SILU>
 __global__ __launch_bounds__(kThreads) void conv_decode_kernel(ConvParams p, uint32_t pieces, uint32_t count) {
   constexpr int V = kPiece<T>;
   const uint32_t id = blockIdx.x * kThreads + threadIdx.x;
@@ -186,16 +196,12 @@ __global__ __launch_bounds__(kThreads) void conv_decode_kernel(ConvParams p, uin
     load_piece<T, V>(reinterpret_cast<const T*>(p.x) + t * p.xs + c, left, xv);
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      const float s = tap_sum<W, V>(w, bias[e], e, xv[e], win);
-      o[e] = p.silu ? s * sigmoid_fast(s) : s;
+      o[e] = activation<SILU>(tap_sum<W, V>(w, bias[e], e, xv[e], win));
+#pragma unroll
+      for (int j = W - 2; j > 0; --j) win[j][e] = win[j - 1][e];
+      win[0][e] = xv[e];
     }
     store_piece<T, V>(reinterpret_cast<T*>(p.y) + t * p.D + c, left, o);
-#pragma unroll
-    for (int j = W - 2; j > 0; --j)
-#pragma unroll
-      for (int e = 0; e < V; ++e) win[j][e] = win[j - 1][e];
-#pragma unroll
-    for (int e = 0; e < V; ++e) win[0][e] = xv[e];
   }
   T* fin = reinterpret_cast<T*>(p.state_fin);
 #pragma unroll
@@ -213,10 +219,12 @@ __global__ __launch_bounds__(kThreads) void conv_decode_kernel(ConvParams p, uin
 // ---------------------------------------------------------------------------
 constexpr int kBwdTokens = 32;
 
-template <typename T, int W, bool FULL>
-__device__ __forceinline__ void conv_bwd_stretch(const ConvParams& p, int64_t t0, int64_t c, int left,
-                                                 float (&dw)[kPiece<T> * W], float (&db)[kPiece<T>]) {
-  constexpr int V = kPiece<T>, TT = kBwdTokens;
+constexpr int kBwdV = 4;   // channels a thread: 8 spill past 2 waves a SIMD
+
+template <typename T, int W, bool SILU, bool NT, bool FULL>
+__device__ __forceinline__ void conv_bwd_stretch(const ConvParams& p, int64_t t0, int64_t c, int left, float (&dw)[kBwdV * W],
+                                                 float (&db)[kBwdV]) {
+  constexpr int V = kBwdV, TT = kBwdTokens;
   const T* x = reinterpret_cast<const T*>(p.x);
   const T* dy = reinterpret_cast<const T*>(p.dy);
   T* dx = reinterpret_cast<T*>(p.dx);
@@ -236,7 +244,7 @@ __device__ __forceinline__ void conv_bwd_stretch(const ConvParams& p, int64_t t0
 #pragma unroll
     for (int e = 0; e < V; ++e) {
       float d = dyv[e], act;
-      if (p.silu) d *= silu_grad_f(tap_sum<W, V>(w, bias[e], e, xv[e], win), act);
+      if (SILU) d *= silu_grad_f(tap_sum<W, V>(w, bias[e], e, xv[e], win), act);
       if (own) {
         db[e] += d;
         dw[e * W + W - 1] = __builtin_fmaf(d, xv[e], dw[e * W + W - 1]);
@@ -261,26 +269,31 @@ __device__ __forceinline__ void conv_bwd_stretch(const ConvParams& p, int64_t t0
                         (t0 + 32 < p.map.ntok ? (uint64_t)p.map.start_bits(t0 + 32) << 32 : ~0ull << 32);
   if (t0 + TT + W - 1 <= p.map.ntok && (bits & (((1ull << (TT + W - 2)) - 1ull) << 1)) == 0 &&
       !((bits & 1ull) && dst0) && n >= 0) {
-    constexpr int U = 5;   // tokens loaded ahead (35 = 7 x 5 for four taps)
-    typename RowVec<T, V>::type rx[U], ry[U];
-    float xv[V], dyv[V], done[V];
-    for (int k0 = 0; k0 < TT + W - 1; k0 += U) {
+    constexpr int U = 5, TE = TT + W - 1;   // tokens a batch, loaded a batch ahead (35 = 7 x 5 for four taps)
+    typename RowVec<T, V>::type rx[2][U], ry[2][U];
+    auto load = [&](int k0, int to) {
 #pragma unroll
       for (int k = 0; k < U; ++k) {
-        const int64_t t = t0 + min(k0 + k, TT + W - 2);
-        load_raw<T, V, FULL>(x + t * p.xs + c, left, rx[k]);
-        load_raw<T, V, FULL>(dy + t * p.dys + c, left, ry[k]);
+        const int64_t t = t0 + min(k0 + k, TE - 1);
+        load_raw<T, V, FULL>(x + t * p.xs + c, left, rx[to][k]);
+        load_raw<T, V, FULL>(dy + t * p.dys + c, left, ry[to][k]);
       }
+    };
+    load(0, 0);
+#pragma unroll
+    for (int k0 = 0; k0 < TE; k0 += U) {
+      if (k0 + U < TE) load(k0 + U, (k0 / U + 1) & 1);
 #pragma unroll
       for (int k = 0; k < U; ++k) {
-        if (k0 + k >= TT + W - 1) break;
+        if (k0 + k >= TE) break;
+        float xv[V], dyv[V], done[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          xv[e] = to_f<T>(rx[k][e]);
-          dyv[e] = to_f<T>(ry[k][e]);
+          xv[e] = to_f<T>(rx[k0 / U & 1][k][e]);
+          dyv[e] = to_f<T>(ry[k0 / U & 1][k][e]);
         }
         token(xv, dyv, k0 + k < TT, done);
-        if (k0 + k >= W - 1) store_piece<T, V, FULL>(dx + (t0 + k0 + k - (W - 1)) * p.D + c, left, done);
+        if (k0 + k >= W - 1) store_piece<T, V, FULL, NT>(dx + (t0 + k0 + k - (W - 1)) * p.D + c, left, done);
       }
     }
     return;
@@ -336,10 +349,12 @@ __device__ __forceinline__ void conv_bwd_stretch(const ConvParams& p, int64_t t0
 }
 
 // lanes: adjacent pieces (kLanes of them), then stretches
-template <typename T, int W>
-__global__ __launch_bounds__(kThreads) void conv_bwd_kernel(ConvParams p, uint32_t lanes, uint32_t groups,
+// (three waves a SIMD: 154 us for 16384 tokens x 6144 channels of bf16, two 162, four 268
+// with what they spill)
+template <typename T, int W, bool SILU, bool NT>
+__global__ __launch_bounds__(kThreads, 3) void conv_bwd_kernel(ConvParams p, uint32_t lanes, uint32_t groups,
                                                             uint32_t main_wgs) {
-  constexpr int V = kPiece<T>;
+  constexpr int V = kBwdV;
   if (blockIdx.x >= main_wgs) {
     copy_empty_states<T, W>(p, p.dstate_fin, p.dstate0, blockIdx.x - main_wgs, kEmptyWgs);
     return;
@@ -355,8 +370,8 @@ __global__ __launch_bounds__(kThreads) void conv_bwd_kernel(ConvParams p, uint32
 #pragma unroll
   for (int e = 0; e < V; ++e) db[e] = 0.f;
   if (left > 0 && t0 < p.map.ntok) {
-    if (left == V) conv_bwd_stretch<T, W, true>(p, t0, c, left, dw, db);
-    else conv_bwd_stretch<T, W, false>(p, t0, c, left, dw, db);
+    if (left == V) conv_bwd_stretch<T, W, SILU, NT, true>(p, t0, c, left, dw, db);
+    else conv_bwd_stretch<T, W, SILU, NT, false>(p, t0, c, left, dw, db);
   }
 #pragma unroll
   for (int e = 0; e < V; ++e) {
@@ -381,51 +396,63 @@ struct BwdGrid {
   uint32_t lanes, groups;
   int64_t rows;
 };
-BwdGrid bwd_grid(int64_t ntok, int64_t D, bool bf16) {
-  const int64_t V = bf16 ? 8 : 4, pieces = (D + V - 1) / V;
+BwdGrid bwd_grid(int64_t ntok, int64_t D) {
+  const int64_t pieces = (D + kBwdV - 1) / kBwdV;
   uint32_t lanes = 1;
   while (lanes < 64 && lanes < pieces) lanes *= 2;
   const int64_t per = (int64_t)(kThreads / lanes) * kBwdTokens;
   return BwdGrid{lanes, (uint32_t)((pieces + lanes - 1) / lanes), (ntok + per - 1) / per};
 }
 
-// stretches of 16 tokens, or of 4 where those would leave most of the card idle
+// Stretches of 16 tokens, or of 4 where those would leave most of the card idle (16:
+// 96 us for 16384 tokens x 6144 channels of bf16, 35 for 20011 x 2048; 8: 100 and 38;
+// 32: 96 and 42).
 constexpr int64_t kFillThreads = 256 * 4 * 64 * 2;
 
-template <typename T, int W> hipError_t forward(const ConvParams& p, hipStream_t stream) {
-  constexpr int V = kPiece<T>;
-  const int64_t pieces = (p.D + V - 1) / V;
-  const bool small = (p.map.ntok + 15) / 16 * pieces < kFillThreads;
-  const int64_t tiles = small ? (p.map.ntok + 3) / 4 : (p.map.ntok + 15) / 16;
-  const int64_t count = tiles * pieces;
+template <typename T, int W, int TT, bool SILU, bool NT>
+hipError_t forward_run(const ConvParams& p, hipStream_t stream) {
+  const int64_t pieces = (p.D + kPiece<T> - 1) / kPiece<T>, count = (p.map.ntok + TT - 1) / TT * pieces;
   if (count > UINT32_MAX - kThreads * (kEmptyWgs + 1)) return hipErrorInvalidValue;
   const uint32_t wgs = (uint32_t)((count + kThreads - 1) / kThreads);
   const uint32_t extra = p.map.seq && p.state_fin ? kEmptyWgs : 0;
-  if (small)
-    hipLaunchKernelGGL((conv_fwd_kernel<T, W, 4>), dim3(wgs + extra), dim3(kThreads), 0, stream, p, (uint32_t)pieces,
-                       (uint32_t)count, wgs);
-  else
-    hipLaunchKernelGGL((conv_fwd_kernel<T, W, 16>), dim3(wgs + extra), dim3(kThreads), 0, stream, p, (uint32_t)pieces,
-                       (uint32_t)count, wgs);
+  hipLaunchKernelGGL((conv_fwd_kernel<T, W, TT, SILU, NT>), dim3(wgs + extra), dim3(kThreads), 0, stream, p,
+                     (uint32_t)pieces, (uint32_t)count, wgs);
   return hipGetLastError();
+}
+template <typename T, int W, bool SILU> hipError_t forward_sized(const ConvParams& p, hipStream_t stream) {
+  const bool small = (p.map.ntok + 15) / 16 * ((p.D + kPiece<T> - 1) / kPiece<T>) < kFillThreads;
+  if (small) return forward_run<T, W, 4, SILU, false>(p, stream);
+  return p.map.ntok * p.D * (int64_t)sizeof(T) > kNtBytes ? forward_run<T, W, 16, SILU, true>(p, stream)
+                                                          : forward_run<T, W, 16, SILU, false>(p, stream);
+}
+template <typename T, int W> hipError_t forward(const ConvParams& p, hipStream_t stream) {
+  return p.silu ? forward_sized<T, W, true>(p, stream) : forward_sized<T, W, false>(p, stream);
 }
 
 template <typename T, int W> hipError_t decode(const ConvParams& p, hipStream_t stream) {
   const int64_t pieces = (p.D + kPiece<T> - 1) / kPiece<T>, count = pieces * p.map.nseq;
   if (count > UINT32_MAX - kThreads) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((conv_decode_kernel<T, W>), dim3((uint32_t)((count + kThreads - 1) / kThreads)), dim3(kThreads), 0,
-                     stream, p, (uint32_t)pieces, (uint32_t)count);
+  const dim3 grid((uint32_t)((count + kThreads - 1) / kThreads));
+  if (p.silu)
+    hipLaunchKernelGGL((conv_decode_kernel<T, W, true>), grid, dim3(kThreads), 0, stream, p, (uint32_t)pieces, (uint32_t)count);
+  else
+    hipLaunchKernelGGL((conv_decode_kernel<T, W, false>), grid, dim3(kThreads), 0, stream, p, (uint32_t)pieces, (uint32_t)count);
   return hipGetLastError();
 }
 
-template <typename T, int W> hipError_t backward(const ConvParams& p, hipStream_t stream) {
-  const BwdGrid g = bwd_grid(p.map.ntok, p.D, sizeof(T) == 2);
+template <typename T, int W, bool SILU> hipError_t backward_sized(const ConvParams& p, hipStream_t stream) {
+  const BwdGrid g = bwd_grid(p.map.ntok, p.D);
   const int64_t wgs = g.rows * g.groups;
-  if (wgs > INT32_MAX) return hipErrorInvalidValue;
-  const uint32_t extra = p.map.seq && p.dstate0 ? kEmptyWgs : 0;
-  hipLaunchKernelGGL((conv_bwd_kernel<T, W>), dim3((uint32_t)wgs + extra), dim3(kThreads), 0, stream, p, g.lanes,
-                     g.groups, (uint32_t)wgs);
+  if (wgs > INT32_MAX - kEmptyWgs) return hipErrorInvalidValue;
+  const dim3 grid((uint32_t)wgs + (p.map.seq && p.dstate0 ? kEmptyWgs : 0));
+  if (p.map.ntok * p.D * (int64_t)sizeof(T) > kNtBytes)
+    hipLaunchKernelGGL((conv_bwd_kernel<T, W, SILU, true>), grid, dim3(kThreads), 0, stream, p, g.lanes, g.groups, (uint32_t)wgs);
+  else
+    hipLaunchKernelGGL((conv_bwd_kernel<T, W, SILU, false>), grid, dim3(kThreads), 0, stream, p, g.lanes, g.groups, (uint32_t)wgs);
   return hipGetLastError();
+}
+template <typename T, int W> hipError_t backward(const ConvParams& p, hipStream_t stream) {
+  return p.silu ? backward_sized<T, W, true>(p, stream) : backward_sized<T, W, false>(p, stream);
 }
 
 #define RLA_CONV_DISPATCH(fn)                                                          \
@@ -442,14 +469,14 @@ hipError_t dispatch_backward(const ConvParams& p, bool bf16, hipStream_t stream)
 hipError_t launch_conv_forward(const ConvParams& p, bool bf16, hipStream_t stream) { RLA_CONV_DISPATCH(forward); }
 hipError_t launch_conv_decode(const ConvParams& p, bool bf16, hipStream_t stream) { RLA_CONV_DISPATCH(decode); }
 
-int64_t conv_backward_rows(int64_t ntok, int64_t D, bool bf16) { return bwd_grid(ntok, D, bf16).rows; }
+int64_t conv_backward_rows(int64_t ntok, int64_t D) { return bwd_grid(ntok, D).rows; }
 
 hipError_t launch_conv_backward(const ConvParams& p, bool bf16, float* dweight, float* dbias, hipStream_t stream) {
   if (p.map.ntok > 0) {
     const hipError_t e = dispatch_backward(p, bf16, stream);
     if (e != hipSuccess) return e;
   }
-  return launch_column_sums(p.part, conv_backward_rows(p.map.ntok, p.D, bf16), (int64_t)(p.taps + 1) * p.D, p.D, p.taps,
+  return launch_column_sums(p.part, conv_backward_rows(p.map.ntok, p.D), (int64_t)(p.taps + 1) * p.D, p.D, p.taps,
                             dweight, dbias, stream);
 }
 

@@ -82,8 +82,8 @@ rla_status check_conv(const rla_conv_problem* q, ConvParams& p) {
   return RLA_OK;
 }
 
-size_t conv_part_bytes(const rla_conv_problem* q, const ConvParams& p) {
-  return up(sizeof(float) * (size_t)conv_backward_rows(p.map.ntok, p.D, q->dtype == RLA_BF16) * (size_t)(p.taps + 1) *
+size_t conv_part_bytes(const ConvParams& p) {
+  return up(sizeof(float) * (size_t)conv_backward_rows(p.map.ntok, p.D) * (size_t)(p.taps + 1) *
             (size_t)p.D);
 }
 size_t conv_map_bytes(const rla_conv_problem* q, const ConvParams& p) {
@@ -112,7 +112,7 @@ using namespace rla;
 extern "C" size_t rla_conv_workspace_size(const rla_conv_problem* q, int backward) {
   ConvParams p;
   if (check_conv(q, p) != RLA_OK) return 0;
-  return conv_map_bytes(q, p) + (backward ? conv_part_bytes(q, p) : 0);
+  return conv_map_bytes(q, p) + (backward ? conv_part_bytes(p) : 0);
 }
 
 extern "C" rla_status rla_conv_forward(const rla_conv_problem* q, const void* x, const float* weight,
@@ -153,7 +153,7 @@ extern "C" rla_status rla_conv_backward(const rla_conv_problem* q, const void* x
       !aligned(dbias, 4) || !aligned(dstate_init, el) || overlap(dstate_final, sbytes, dstate_init, sbytes))
     return RLA_ERR_VALUE;
   const size_t map_bytes = conv_map_bytes(q, p);
-  st = check_workspace(map_bytes + conv_part_bytes(q, p), workspace, workspace_bytes);
+  st = check_workspace(map_bytes + conv_part_bytes(p), workspace, workspace_bytes);
   if (st != RLA_OK) return st;
   hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);
   unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);

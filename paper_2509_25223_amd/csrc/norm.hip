@@ -55,10 +55,10 @@ __device__ __forceinline__ void row_load(const T* row, int64_t c, int left, floa
     load_piece<T, V>(row + c, left, x);
   }
 }
-template <typename T, int V, bool FULL>
+template <typename T, int V, bool FULL, bool NT = false>
 __device__ __forceinline__ void row_store(T* row, int64_t c, int left, const float (&x)[V]) {
   if constexpr (FULL) {
-    if (left > 0) store_piece<T, V, true>(row + c, V, x);
+    if (left > 0) store_piece<T, V, true, NT>(row + c, V, x);
   } else {
     store_piece<T, V>(row + c, left, x);
   }
@@ -91,12 +91,33 @@ __device__ __forceinline__ float row_sum(float v, float* lds) {
   return v;
 }
 
+// Two sums at once; `turn` alternates, so that one barrier a call is enough.
+template <int L>
+__device__ __forceinline__ void row_sums(float& a, float& b, float (&lds)[2][kWaves][2], int turn) {
+  a = lanes_sum<(L < 64 ? L : 64)>(a);
+  b = lanes_sum<(L < 64 ? L : 64)>(b);
+  if constexpr (L > 64) {
+    const int w = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) {
+      lds[turn][w][0] = a;
+      lds[turn][w][1] = b;
+    }
+    __syncthreads();
+    a = b = 0.f;
+#pragma unroll
+    for (int i = 0; i < L / 64; ++i) {
+      a += lds[turn][i][0];
+      b += lds[turn][i][1];
+    }
+  }
+}
+
 // ---------------------------------------------------------------------------
 // Before a block.  A row is taken by a wave (up to 4 pieces a lane: 2048 bf16
 // channels) or a workgroup; wider rows (NP = 0) are read twice, their sum
 // first.
 // ---------------------------------------------------------------------------
-template <typename T, typename R, int L, int NP, bool FULL>
+template <typename T, typename R, int L, int NP, bool FULL, bool NT>
 __global__ __launch_bounds__(kThreads) void addnorm_fwd_kernel(AddNormParams p) {
   constexpr int V = kPiece<T>, N = NP ? NP : 1;
   typedef RowLanes<L, N, V> RL;
@@ -124,11 +145,11 @@ __global__ __launch_bounds__(kThreads) void addnorm_fwd_kernel(AddNormParams p) 
   };
   auto finish = [&](int64_t c, int left, const float (&r)[V], float inv) {
     float w[V];
-    row_store<R, V, FULL>(out, c, left, r);
+    row_store<R, V, FULL, NT>(out, c, left, r);
     row_load<float, V, FULL>(p.weight, c, left, w);
 #pragma unroll
     for (int e = 0; e < V; ++e) w[e] *= r[e] * inv;
-    row_store<T, V, FULL>(n, c, left, w);
+    row_store<T, V, FULL, NT>(n, c, left, w);
   };
   float ss = 0.f;
   if constexpr (NP > 0) {
@@ -162,11 +183,12 @@ __global__ __launch_bounds__(kThreads) void addnorm_fwd_kernel(AddNormParams p) 
 // Rows blockIdx.x * (kThreads / L) + ..., a grid apart.  Column sums: [workgroup][2][width]
 // (dweight, dscale), the workgroup's waves added in LDS.  NP = 0: the row in
 // two passes, and the sums kept in the workgroup's partial row itself.
-template <typename T, typename R, int L, int NP, bool FULL>
+template <typename T, typename R, int L, int NP, bool FULL, bool NT>
 __global__ __launch_bounds__(kThreads) void addnorm_bwd_kernel(AddNormParams p) {
   constexpr int V = kPiece<T>, N = NP ? NP : 1;
   typedef RowLanes<L, N, V> RL;
-  __shared__ float lds[kWaves];
+  __shared__ float lds[2][kWaves][2];
+  int turn = 0;
   constexpr int kSub = kThreads / L;
   const bool scaled = p.scale != nullptr;
   float* part = p.part + (int64_t)blockIdx.x * (scaled ? 2 : 1) * p.width;
@@ -192,7 +214,7 @@ __global__ __launch_bounds__(kThreads) void addnorm_bwd_kernel(AddNormParams p) 
       dw[e] = __builtin_fmaf(q.dn[e], q.r[e] * ng.inv, dw[e]);
       dr[e] += ng.of(q.dn[e] * q.w[e], q.r[e]);
     }
-    if (p.dresidual) row_store<R, V, FULL>(reinterpret_cast<R*>(p.dresidual) + row * p.width, c, left, dr);
+    if (p.dresidual) row_store<R, V, FULL, NT>(reinterpret_cast<R*>(p.dresidual) + row * p.width, c, left, dr);
     if (scaled) {
       row_load<T, V, FULL>(reinterpret_cast<const T*>(p.x) + row * p.xs, c, left, t);
 #pragma unroll
@@ -201,7 +223,7 @@ __global__ __launch_bounds__(kThreads) void addnorm_bwd_kernel(AddNormParams p) 
 #pragma unroll
       for (int e = 0; e < V; ++e) dr[e] *= t[e];
     }
-    row_store<T, V, FULL>(reinterpret_cast<T*>(p.dx) + row * p.width, c, left, dr);
+    row_store<T, V, FULL, NT>(reinterpret_cast<T*>(p.dx) + row * p.width, c, left, dr);
   };
 
   if constexpr (NP > 0) {
@@ -226,8 +248,9 @@ __global__ __launch_bounds__(kThreads) void addnorm_bwd_kernel(AddNormParams p) 
           ss += q[j].r[e] * q[j].r[e];
           sd += q[j].dn[e] * w[j][e] * q[j].r[e];
         }
-      const float yy = row_sum<L>(ss, lds), dy = row_sum<L>(sd, lds);
-      const NormGrad ng(yy, dy, wd, p.eps);
+      row_sums<L>(ss, sd, lds, turn);
+      turn ^= 1;
+      const NormGrad ng(ss, sd, wd, p.eps);
 #pragma unroll
       for (int j = 0; j < N; ++j) finish(row, RL::col(j), RL::left(j, p.width), q[j], ng, dw[j], ds[j]);
     }
@@ -269,8 +292,9 @@ __global__ __launch_bounds__(kThreads) void addnorm_bwd_kernel(AddNormParams p) 
           sd += q.dn[e] * q.w[e] * q.r[e];
         }
       }
-      const float yy = row_sum<L>(ss, lds), dy = row_sum<L>(sd, lds);
-      const NormGrad ng(yy, dy, wd, p.eps);
+      row_sums<L>(ss, sd, lds, turn);
+      turn ^= 1;
+      const NormGrad ng(ss, sd, wd, p.eps);
       for (int64_t c = RL::col(0); c < p.width; c += L * V) {
         const int left = (int)min(p.width - c, (int64_t)V);
         Piece q;
@@ -291,7 +315,7 @@ __global__ __launch_bounds__(kThreads) void addnorm_bwd_kernel(AddNormParams p) 
 // After a block.  A head's row is taken by L lanes, NP pieces each; rows wider than
 // that (NP = 0) are read twice.
 // ---------------------------------------------------------------------------
-template <typename T, typename X, int L, int NP, bool FULL, bool FIRST>
+template <typename T, typename X, int L, int NP, bool FULL, bool FIRST, bool NT>
 __global__ __launch_bounds__(kThreads) void gatenorm_fwd_kernel(GateNormParams p) {
   constexpr int V = kPiece<T>, N = NP ? NP : 1;
   typedef RowLanes<L, N, V> RL;
@@ -320,7 +344,7 @@ __global__ __launch_bounds__(kThreads) void gatenorm_fwd_kernel(GateNormParams p
     row_load<float, V, FULL>(weight, c, left, w);
 #pragma unroll
     for (int e = 0; e < V; ++e) w[e] *= y[e] * inv * (FIRST ? 1.f : act[e]);
-    row_store<T, V, FULL>(o, c, left, w);
+    row_store<T, V, FULL, NT>(o, c, left, w);
   };
   float ss = 0.f;
   if constexpr (NP > 0) {
@@ -351,7 +375,7 @@ __global__ __launch_bounds__(kThreads) void gatenorm_fwd_kernel(GateNormParams p
 // Groups of L lanes take rows `groups` apart, a multiple of the heads: a group
 // stays with one head.  Column sums: [group][width] for weights per head (rows of
 // [groups / heads][heads][width]), else [workgroup][width].
-template <typename T, typename X, int L, int NP, bool FULL, bool FIRST>
+template <typename T, typename X, int L, int NP, bool FULL, bool FIRST, bool NT>
 __global__ __launch_bounds__(kThreads) void gatenorm_bwd_kernel(GateNormParams p) {
   constexpr int V = kPiece<T>, N = NP ? NP : 1, kSub = kThreads / L;
   typedef RowLanes<L, N, V> RL;
@@ -392,8 +416,8 @@ __global__ __launch_bounds__(kThreads) void gatenorm_bwd_kernel(GateNormParams p
       dg[e] = (FIRST ? dy * q.x[e] : q.d[e] * hat * w[e]) * slope;
     }
     const int64_t at = (tok * p.heads + h) * p.width;
-    row_store<X, V, FULL>(reinterpret_cast<X*>(p.dx) + at, c, left, dx);
-    row_store<T, V, FULL>(reinterpret_cast<T*>(p.dgate) + at, c, left, dg);
+    row_store<X, V, FULL, NT>(reinterpret_cast<X*>(p.dx) + at, c, left, dx);
+    row_store<T, V, FULL, NT>(reinterpret_cast<T*>(p.dgate) + at, c, left, dg);
   };
 
   if constexpr (NP > 0) {
@@ -468,17 +492,20 @@ __global__ __launch_bounds__(kThreads) void gatenorm_bwd_kernel(GateNormParams p
 // ---------------------------------------------------------------------------
 // launches
 // ---------------------------------------------------------------------------
-constexpr int64_t kBwdWgs = 512;   // two workgroups a CU: the partial sums stay small
-
 struct Shape {
   int L, NP;
 };
-// addnorm: a wave a row up to 4 pieces a lane, then a workgroup, then two passes
-Shape addnorm_shape(int64_t width, int V) {
+// addnorm forward: a wave a row up to 4 pieces a lane, then a workgroup, then two passes.
+// Backward, where a lane holds its columns' sums beside the row: a wave a row of one
+// piece a lane, then a workgroup (16384 rows of 2048 bf16 values with an fp32 stream: a
+// wave with 4 pieces 195 us, one to a SIMD).
+Shape addnorm_shape(int64_t width, int V, bool backward) {
   const int64_t pieces = (width + V - 1) / V;
-  for (int L : {64, kThreads})
-    for (int NP : {1, 2, 4})
-      if (pieces <= L * NP) return Shape{L, NP};
+  if (pieces <= 64) return Shape{64, 1};
+  if (!backward && pieces <= 128) return Shape{64, 2};
+  if (!backward && pieces <= 256) return Shape{64, 4};
+  for (int NP : {1, 2, 4})
+    if (pieces <= kThreads * NP) return Shape{kThreads, NP};
   return Shape{kThreads, 0};
 }
 // gatenorm: the fewest lanes that hold a row in a piece each, then more pieces
@@ -489,76 +516,90 @@ Shape gatenorm_shape(int64_t width, int V) {
   if (pieces <= 256) return Shape{64, 4};
   return Shape{64, 0};
 }
+// Workgroups that keep sums over many rows: enough to fill the card, few enough that the
+// sums stay small beside the rows.  More where a workgroup leaves one row of sums for
+// many rows at a time (gatenorm, one weight for all heads).
+constexpr int64_t kBwdWgs = 512, kBwdRowWgs = 1024, kBwdNarrowWgs = 1024;
 
-template <typename T, typename R, int L, int NP, bool FULL>
-hipError_t addnorm_run(const AddNormParams& p, bool backward, hipStream_t stream) {
-  if (backward) {
-    hipLaunchKernelGGL((addnorm_bwd_kernel<T, R, L, NP, FULL>), dim3((uint32_t)p.wgs), dim3(kThreads), 0, stream, p);
-  } else {
-    const int64_t sub = kThreads / L;
-    hipLaunchKernelGGL((addnorm_fwd_kernel<T, R, L, NP, FULL>), dim3((uint32_t)((p.rows + sub - 1) / sub)),
-                       dim3(kThreads), 0, stream, p);
-  }
+template <typename T, typename R, int L, int NP, bool FULL, bool NT>
+hipError_t addnorm_forward(const AddNormParams& p, hipStream_t stream) {
+  const int64_t sub = kThreads / L;
+  hipLaunchKernelGGL((addnorm_fwd_kernel<T, R, L, NP, FULL, NT>), dim3((uint32_t)((p.rows + sub - 1) / sub)),
+                     dim3(kThreads), 0, stream, p);
   return hipGetLastError();
 }
-template <typename T, typename R, bool FULL>
+template <typename T, typename R, int L, int NP, bool FULL, bool NT>
+hipError_t addnorm_backward(const AddNormParams& p, hipStream_t stream) {
+  hipLaunchKernelGGL((addnorm_bwd_kernel<T, R, L, NP, FULL, NT>), dim3((uint32_t)p.wgs), dim3(kThreads), 0, stream, p);
+  return hipGetLastError();
+}
+template <typename T, typename R, bool FULL, bool NT>
 hipError_t addnorm_shaped(const AddNormParams& p, bool backward, hipStream_t stream) {
-  const Shape s = addnorm_shape(p.width, kPiece<T>);
+  const Shape s = addnorm_shape(p.width, kPiece<T>, backward);
+  if (backward) {
+    if (s.L == 64) return addnorm_backward<T, R, 64, 1, FULL, NT>(p, stream);
+    if (s.NP == 1) return addnorm_backward<T, R, kThreads, 1, FULL, NT>(p, stream);
+    if (s.NP == 2) return addnorm_backward<T, R, kThreads, 2, FULL, NT>(p, stream);
+    if (s.NP == 4) return addnorm_backward<T, R, kThreads, 4, FULL, NT>(p, stream);
+    return addnorm_backward<T, R, kThreads, 0, FULL, NT>(p, stream);
+  }
   if (s.L == 64) {
-    if (s.NP == 1) return addnorm_run<T, R, 64, 1, FULL>(p, backward, stream);
-    if (s.NP == 2) return addnorm_run<T, R, 64, 2, FULL>(p, backward, stream);
-    return addnorm_run<T, R, 64, 4, FULL>(p, backward, stream);
+    if (s.NP == 1) return addnorm_forward<T, R, 64, 1, FULL, NT>(p, stream);
+    if (s.NP == 2) return addnorm_forward<T, R, 64, 2, FULL, NT>(p, stream);
+    return addnorm_forward<T, R, 64, 4, FULL, NT>(p, stream);
   }
   // (one piece of 256 lanes is four of a wave)
-  if (s.NP == 2) return addnorm_run<T, R, kThreads, 2, FULL>(p, backward, stream);
-  if (s.NP == 4) return addnorm_run<T, R, kThreads, 4, FULL>(p, backward, stream);
-  return addnorm_run<T, R, kThreads, 0, FULL>(p, backward, stream);
+  if (s.NP == 2) return addnorm_forward<T, R, kThreads, 2, FULL, NT>(p, stream);
+  if (s.NP == 4) return addnorm_forward<T, R, kThreads, 4, FULL, NT>(p, stream);
+  return addnorm_forward<T, R, kThreads, 0, FULL, NT>(p, stream);
 }
 template <typename T, typename R> hipError_t addnorm(const AddNormParams& p, bool backward, hipStream_t stream) {
-  return p.width % kPiece<T> == 0 ? addnorm_shaped<T, R, true>(p, backward, stream)
-                                  : addnorm_shaped<T, R, false>(p, backward, stream);
+  if (p.width % kPiece<T> != 0) return addnorm_shaped<T, R, false, false>(p, backward, stream);
+  return p.rows * p.width * (int64_t)(sizeof(T) + sizeof(R)) > kNtBytes ? addnorm_shaped<T, R, true, true>(p, backward, stream)
+                                                                        : addnorm_shaped<T, R, true, false>(p, backward, stream);
 }
 
-template <typename T, typename X, int L, int NP, bool FULL>
+template <typename T, typename X, int L, int NP, bool FULL, bool NT>
 hipError_t gatenorm_run(const GateNormParams& p, bool backward, hipStream_t stream) {
   const int64_t sub = kThreads / L;
+  const dim3 grid((uint32_t)(((backward ? p.groups : p.rows) + sub - 1) / sub));
   if (backward) {
-    const dim3 grid((uint32_t)((p.groups + sub - 1) / sub));
-    if (p.first) hipLaunchKernelGGL((gatenorm_bwd_kernel<T, X, L, NP, FULL, true>), grid, dim3(kThreads), 0, stream, p);
-    else hipLaunchKernelGGL((gatenorm_bwd_kernel<T, X, L, NP, FULL, false>), grid, dim3(kThreads), 0, stream, p);
+    if (p.first) hipLaunchKernelGGL((gatenorm_bwd_kernel<T, X, L, NP, FULL, true, NT>), grid, dim3(kThreads), 0, stream, p);
+    else hipLaunchKernelGGL((gatenorm_bwd_kernel<T, X, L, NP, FULL, false, NT>), grid, dim3(kThreads), 0, stream, p);
   } else {
-    const dim3 grid((uint32_t)((p.rows + sub - 1) / sub));
-    if (p.first) hipLaunchKernelGGL((gatenorm_fwd_kernel<T, X, L, NP, FULL, true>), grid, dim3(kThreads), 0, stream, p);
-    else hipLaunchKernelGGL((gatenorm_fwd_kernel<T, X, L, NP, FULL, false>), grid, dim3(kThreads), 0, stream, p);
+    if (p.first) hipLaunchKernelGGL((gatenorm_fwd_kernel<T, X, L, NP, FULL, true, NT>), grid, dim3(kThreads), 0, stream, p);
+    else hipLaunchKernelGGL((gatenorm_fwd_kernel<T, X, L, NP, FULL, false, NT>), grid, dim3(kThreads), 0, stream, p);
   }
   return hipGetLastError();
 }
-template <typename T, typename X, bool FULL>
+template <typename T, typename X, bool FULL, bool NT>
 hipError_t gatenorm_shaped(const GateNormParams& p, bool backward, hipStream_t stream) {
   const Shape s = gatenorm_shape(p.width, kPiece<T>);
-  if (s.L == 8) return gatenorm_run<T, X, 8, 1, FULL>(p, backward, stream);
-  if (s.L == 16) return gatenorm_run<T, X, 16, 1, FULL>(p, backward, stream);
-  if (s.L == 32) return gatenorm_run<T, X, 32, 1, FULL>(p, backward, stream);
-  if (s.NP == 1) return gatenorm_run<T, X, 64, 1, FULL>(p, backward, stream);
-  if (s.NP == 4) return gatenorm_run<T, X, 64, 4, FULL>(p, backward, stream);
-  return gatenorm_run<T, X, 64, 0, FULL>(p, backward, stream);
+  if (s.L == 8) return gatenorm_run<T, X, 8, 1, FULL, NT>(p, backward, stream);
+  if (s.L == 16) return gatenorm_run<T, X, 16, 1, FULL, NT>(p, backward, stream);
+  if (s.L == 32) return gatenorm_run<T, X, 32, 1, FULL, NT>(p, backward, stream);
+  if (s.NP == 1) return gatenorm_run<T, X, 64, 1, FULL, NT>(p, backward, stream);
+  if (s.NP == 4) return gatenorm_run<T, X, 64, 4, FULL, NT>(p, backward, stream);
+  return gatenorm_run<T, X, 64, 0, FULL, NT>(p, backward, stream);
 }
 template <typename T, typename X> hipError_t gatenorm(const GateNormParams& p, bool backward, hipStream_t stream) {
-  return p.width % kPiece<T> == 0 ? gatenorm_shaped<T, X, true>(p, backward, stream)
-                                  : gatenorm_shaped<T, X, false>(p, backward, stream);
+  if (p.width % kPiece<T> != 0) return gatenorm_shaped<T, X, false, false>(p, backward, stream);
+  const int64_t written = p.rows * p.width * (int64_t)(sizeof(T) + (backward ? sizeof(X) : 0));
+  return written > kNtBytes ? gatenorm_shaped<T, X, true, true>(p, backward, stream)
+                            : gatenorm_shaped<T, X, true, false>(p, backward, stream);
 }
 
 }  // namespace
 
 int64_t addnorm_backward_wgs(int64_t rows, int64_t width, bool bf16) {
-  const int64_t sub = kThreads / addnorm_shape(width, bf16 ? 8 : 4).L;
-  return max((int64_t)1, min(kBwdWgs, (rows + sub - 1) / sub));
+  const int64_t sub = kThreads / addnorm_shape(width, bf16 ? 8 : 4, true).L;
+  return max((int64_t)1, min(sub == 1 ? kBwdRowWgs : kBwdWgs, (rows + sub - 1) / sub));
 }
 
 int64_t gatenorm_backward_groups(int64_t rows, int64_t heads, int64_t width, bool bf16, int64_t& part_rows, bool per_head) {
   const Shape s = gatenorm_shape(width, bf16 ? 8 : 4);
   const int64_t sub = kThreads / s.L;
-  int64_t groups = min(rows, kBwdWgs * sub);
+  int64_t groups = min(rows, (per_head || s.NP == 0 ? kBwdWgs : kBwdNarrowWgs) * sub);
   groups = max((int64_t)1, groups / heads) * heads;   // whole sets of heads
   part_rows = per_head || s.NP == 0 ? groups : (groups + sub - 1) / sub;
   return groups;

@@ -101,8 +101,18 @@ __global__ __launch_bounds__(64 * kSumGroups) void column_sums_kernel(const floa
   const int lane = threadIdx.x & 63, g = threadIdx.x >> 6;
   const int64_t c = (int64_t)blockIdx.x * 64 + lane;
   float sum = 0.f;
-  if (c < cols)
-    for (int64_t r = g; r < rows; r += kSumGroups) sum += part[r * cols + c];
+  if (c < cols) {
+    constexpr int kAhead = 16;   // loads in flight
+    int64_t r = g;
+    for (; r + (kAhead - 1) * kSumGroups < rows; r += kAhead * kSumGroups) {
+      float v[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) v[u] = part[(r + u * kSumGroups) * cols + c];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) sum += v[u];
+    }
+    for (; r < rows; r += kSumGroups) sum += part[r * cols + c];
+  }
   s[g][lane] = sum;
   __syncthreads();
   if (g != 0 || c >= cols) return;
