@@ -343,7 +343,7 @@ namespace rla {
 namespace {
 
 // Workgroups that fill the card: chunks are added up to this many.
-constexpr int64_t kSsmFill = 1024, kSsmMinChunk = 64, kSsmMaxChunks = 64;
+constexpr int64_t kSsmFill = 1024, kSsmMinChunk = 64;
 
 rla_status check_ssm(const rla_ssm_problem* q, SsmParams& p) {
   if (!q) return RLA_ERR_NULL_ARG;

@@ -60,6 +60,7 @@ constexpr int kSsmTile = 32;   // tokens staged at a time in the forward
 constexpr int kSsmSub = 16;    // tokens between saved states, staged at a time in the backward
 constexpr int kHasStart = 1;   // a sequence starts at one of the chunk's tokens
 constexpr int kClosed = 2;     // ... after its first one, or right behind the chunk
+constexpr int kSsmMaxChunks = 64;   // of packed tokens, or of a dense sequence
 
 // states padded, and a workgroup's channels
 inline int ssm_padded(int64_t N) { return N <= 8 ? 8 : N <= 16 ? 16 : N <= 32 ? 32 : 64; }
@@ -156,6 +157,13 @@ __device__ __forceinline__ TokenMap fresh_map(SsmArgs a) {
   return m;
 }
 
+// x, but not known to be the same in the next turn of a loop: comparisons with it stay
+// where they are used, and their masks out of the scalar registers in between.
+__device__ __forceinline__ int fresh(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 template <typename V> __device__ __forceinline__ V settled(V x) {
   if constexpr (sizeof(V) == 2) {
     u16 w = __builtin_bit_cast(u16, x);
@@ -190,6 +198,40 @@ template <int LPC> __device__ __forceinline__ float tokens_over_lanes(float (&v)
   const float x0 = (b0 ? v[1] : v[0]) + lane_dpp<0xB1>(b0 ? v[0] : v[1]);
   const float x1 = (b0 ? v[3] : v[2]) + lane_dpp<0xB1>(b0 ? v[2] : v[3]);
   return (b1 ? x1 : x0) + lane_dpp<0x4E>(b1 ? x0 : x1);
+}
+
+// A state carried through the chunks first, first + dir, .. (count of them): h = exp(A sum)
+// h + x, with each chunk's x and sum of steps; four chunks' loads at a time.
+template <typename SL>
+__device__ __forceinline__ void carry_through(const SsmParams& p, const float* x, int first, int dir, int count, int64_t c,
+                                              int n0, const float (&A2)[SL::NS], float (&h)[SL::NS]) {
+  constexpr int NS = SL::NS;
+  for (int i = 0; i < count; i += 4) {
+    float v[4][NS], sum[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t cc = first + dir * min(i + u, count - 1);
+      load_piece<float, NS, true>(x + (cc * p.D + c) * SL::NP + n0, NS, v[u]);
+      sum[u] = p.sumd[cc * p.D + c];
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i + u < count)
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+          // (a state that is zero stays so: no infinity times it where A is positive)
+          const float carried = h[n] == 0.f ? 0.f : __builtin_amdgcn_exp2f(sum[u] * A2[n]) * h[n];
+          h[n] = carried + v[u][n];
+        }
+  }
+}
+
+// Packed: the last chunk before `chunk` that has `flag`, or (ahead) the first behind it;
+// there is one.  At most kSsmMaxChunks chunks: a lane each.
+__device__ __forceinline__ int find_chunk(const SsmParams& p, int chunk, int flag, bool ahead) {
+  const int lane = threadIdx.x & 63;
+  const uint64_t got = __ballot(lane < p.nchunk && (ahead ? lane > chunk : lane < chunk) && (p.flags[lane] & flag));
+  return ahead ? __ffsll((unsigned long long)got) - 1 : 63 - __clzll((long long)got);
 }
 
 // Chunk c: first token, number of tokens.

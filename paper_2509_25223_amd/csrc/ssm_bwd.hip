@@ -118,10 +118,10 @@ __global__ __launch_bounds__(SL::kThr) void ssm_rev_kernel(SsmParams p) {
     for (int n = 0; n < NS; ++n) dh[n] = 0.f;
 
   St st;
-  const int r = St::r(), pc = St::pc(), rb = St::rb(), pb = St::pb(), pleft = nc - pc, bleft = (int)p.N - pb;
+  const int r = St::r(), pc = St::pc(), rb = St::rb(), pb = St::pb(), pleft0 = nc - pc, bleft0 = (int)p.N - pb;
   float bias[V];
 #pragma unroll
-  for (int e = 0; e < V; ++e) bias[e] = p.dbias && e < pleft ? p.dbias[c0 + pc + e] : 0.f;
+  for (int e = 0; e < V; ++e) bias[e] = p.dbias && e < pleft0 ? p.dbias[c0 + pc + e] : 0.f;
   settle(A2);
   settle(dh);
   settle(bias);
@@ -131,6 +131,7 @@ __global__ __launch_bounds__(SL::kThr) void ssm_rev_kernel(SsmParams p) {
   for (int k = k_last; k >= 0; k -= TT) {
     even_pace((k_last - k) / TT);
     const bool in = st.inside(k, end, packed);
+    const int pleft = fresh(pleft0), bleft = fresh(bleft0);
     float s[V];
     st.steps(bias, sp, s);
 #pragma unroll
@@ -249,26 +250,13 @@ __global__ __launch_bounds__(SL::kThr, 2) void ssm_bwd_kernel(SsmParams p) {
   if (p.map.seq ? t0 + len >= p.map.ntok || (p.map.start_bits(t0 + len) & 1u) : (t0 + len) % p.map.T == 0) {
     state_of(p.dhfin, seq, carry);
   } else {   // the chunks behind, up to the first that closes the sequence
-    int cc = chunk + 1;
-    if (p.map.seq)
-      while (!(p.flags[cc] & kClosed)) ++cc;
-    else
-      cc = chunk / p.cps * p.cps + p.cps - 1;
-    load_states<NS>(p.E + ((int64_t)cc * p.D + c) * NP + n0, NS, carry);
-    for (--cc; cc > chunk; --cc) {
-      float s[NS];
-      load_states<NS>(p.E + ((int64_t)cc * p.D + c) * NP + n0, NS, s);
-      const float sum = p.sumd[(int64_t)cc * p.D + c];
-#pragma unroll
-      for (int n = 0; n < NS; ++n) {
-        const float back = carry[n] == 0.f ? 0.f : __builtin_amdgcn_exp2f(sum * A2[n]) * carry[n];
-        carry[n] = back + s[n];
-      }
-    }
+    const int cc = p.map.seq ? find_chunk(p, chunk, kClosed, true) : chunk / p.cps * p.cps + p.cps - 1;
+    load_piece<float, NS, true>(p.E + ((int64_t)cc * p.D + c) * NP + n0, NS, carry);
+    carry_through<SL>(p, p.E, cc - 1, -1, cc - 1 - chunk, c, n0, A2, carry);
   }
 
   St st;
-  const int r = St::r(), pc = St::pc(), rb = St::rb(), pb = St::pb(), pleft = nc - pc, bleft = (int)p.N - pb;
+  const int r = St::r(), pc = St::pc(), rb = St::rb(), pb = St::pb(), pleft0 = nc - pc, bleft0 = (int)p.N - pb;
   const uint32_t fout = (r * (uint32_t)p.D + pc) * (uint32_t)sizeof(T), fck = ((live ? ch : 0) * NP + n0) * 4;
   float dskip[V], ddb[V];
 #pragma unroll
@@ -289,13 +277,16 @@ __global__ __launch_bounds__(SL::kThr, 2) void ssm_bwd_kernel(SsmParams p) {
   settle(carry);
   const int k_last = (len - 1) / TT * TT;
   const bool packed = p.map.seq != nullptr, sp = p.softplus != 0, gated = p.z != nullptr;
+  const bool starts_seq = t0 % p.map.T == 0;   // (dense)
   load_tile(k_last);
   for (int k = k_last; k >= 0; k -= TT) {
     const SsmArgs a = fresh_args();
     even_pace((k_last - k) / TT);
     // ---- these tokens into LDS ----
     const uint32_t valid = len - k >= TT ? (1u << TT) - 1u : (1u << (len - k)) - 1u;
-    const uint32_t bits = fresh_map(a).start_bits(t0 + k) & valid;
+    // (a dense chunk's only start is its first token)
+    const uint32_t bits = packed ? fresh_map(a).start_bits(t0 + k) & valid : k == 0 && starts_seq ? 1u : 0u;
+    const int pleft = fresh(pleft0), bleft = fresh(bleft0);
     const bool here = st.inside(k, len, packed);
     {
       float s[V], bias[V];
@@ -381,7 +372,7 @@ __global__ __launch_bounds__(SL::kThr, 2) void ssm_bwd_kernel(SsmParams p) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) y[j] = n == 0 ? x[j][n] * c4[j][n] : __builtin_fmaf(x[j][n], c4[j][n], y[j]);
           const float yt = tokens_over_lanes<LPC>(y);
-          if (q < 4 && inside(i + q)) sY[i + q][ch] = yt;
+          if ((LPC == 4 || q < 4) && inside(i + q)) sY[i + q][ch] = yt;
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -454,7 +445,7 @@ __global__ __launch_bounds__(SL::kThr, 2) void ssm_bwd_kernel(SsmParams p) {
           }
         });
         const float it = tokens_over_lanes<LPC>(into), qt = tokens_over_lanes<LPC>(qa);
-        if (q < 4 && inside(i + q)) {
+        if ((LPC == 4 || q < 4) && inside(i + q)) {
           sI[i + q][ch] = it;
           sQ[i + q][ch] = qt;
         }
@@ -514,7 +505,7 @@ __global__ __launch_bounds__(SL::kThr, 2) void ssm_bwd_kernel(SsmParams p) {
       }
       // a thread's values of the sums over the waves: (token, dB or dC, states)
       constexpr int E = TT * 2 * NP / SL::kThr, kPerT = 2 * NP / E;
-      const int et = tid / kPerT, w = tid % kPerT * E / NP, n1 = tid % kPerT * E % NP;
+      const int ft = fresh(tid), et = ft / kPerT, w = ft % kPerT * E / NP, n1 = ft % kPerT * E % NP;
       float v[E];
 #pragma unroll
       for (int e = 0; e < E; ++e) {
@@ -539,7 +530,7 @@ __global__ __launch_bounds__(SL::kThr, 2) void ssm_bwd_kernel(SsmParams p) {
       }
       if (k + et < len) {
         if (N == NP) store_piece<float, E, true>(part + (et * 2 + w) * NP + n1, E, v);
-        else store_piece<float, E>(part + (et * 2 + w) * N + n1, (int)N - n1, v);
+        else store_piece<float, E>(part + (et * 2 + w) * N + n1, fresh((int)N - n1), v);
       }
     }
   }

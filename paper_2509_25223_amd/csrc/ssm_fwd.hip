@@ -64,13 +64,13 @@ __global__ __launch_bounds__(SL::kThr) void ssm_fwd_kernel(SsmParams p) {
   };
 
   St st;
-  const int r = St::r(), pc = St::pc(), rb = St::rb(), pb = St::pb(), pleft = nc - pc, bleft = (int)p.N - pb;
+  const int r = St::r(), pc = St::pc(), rb = St::rb(), pb = St::pb(), pleft0 = nc - pc, bleft0 = (int)p.N - pb;
   const uint32_t fout = (r * (uint32_t)p.D + pc) * (uint32_t)sizeof(T);
   float bias[V], skip[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    bias[e] = p.dbias && e < pleft ? p.dbias[c0 + pc + e] : 0.f;
-    skip[e] = p.skip && e < pleft ? p.skip[c0 + pc + e] : 0.f;
+    bias[e] = p.dbias && e < pleft0 ? p.dbias[c0 + pc + e] : 0.f;
+    skip[e] = p.skip && e < pleft0 ? p.skip[c0 + pc + e] : 0.f;
   }
   // tiles from the one of the last start on (summary), or all
   const int k_first = SUMMARY && last > 0 ? last / TT * TT : 0;
@@ -81,23 +81,9 @@ __global__ __launch_bounds__(SL::kThr) void ssm_fwd_kernel(SsmParams p) {
   } else if (last >= 0 && p.map.start_bits(t0) & 1u) {
     start_state(seq);
   } else {   // the chunks before, from the last one with a start on
-    int cc = chunk - 1;
-    if (p.map.seq)
-      while (!(p.flags[cc] & kHasStart)) --cc;
-    else
-      cc = chunk / p.cps * p.cps;
-    load_states<NS>(p.S + ((int64_t)cc * p.D + c) * NP + n0, NS, h);
-    for (++cc; cc < chunk; ++cc) {
-      float s[NS];
-      load_states<NS>(p.S + ((int64_t)cc * p.D + c) * NP + n0, NS, s);
-      const float sum = p.sumd[(int64_t)cc * p.D + c];
-#pragma unroll
-      for (int n = 0; n < NS; ++n) {
-        // (a state that is zero stays so: no infinity times it where A is positive)
-        const float carried = h[n] == 0.f ? 0.f : __builtin_amdgcn_exp2f(sum * A2[n]) * h[n];
-        h[n] = carried + s[n];
-      }
-    }
+    const int cc = p.map.seq ? find_chunk(p, chunk, kHasStart, false) : chunk / p.cps * p.cps;
+    load_piece<float, NS, true>(p.S + ((int64_t)cc * p.D + c) * NP + n0, NS, h);
+    carry_through<SL>(p, p.S, cc + 1, 1, chunk - 1 - cc, c, n0, A2, h);
   }
   float total = 0.f;   // sum of the channel's steps
   float* const ck = p.ck;
@@ -112,8 +98,10 @@ __global__ __launch_bounds__(SL::kThr) void ssm_fwd_kernel(SsmParams p) {
     even_pace(k / TT);
     // ---- this tile into LDS ----
     const uint32_t valid = len - k >= TT ? ~0u : (1u << (len - k)) - 1u;
-    uint32_t bits = SUMMARY ? 0u : fresh_map(fresh_args()).start_bits(t0 + k) & valid;
-    if (k == 0) bits &= ~1u;   // the chunk's first token: its state is set
+    // (the chunk's first token, and dense chunks' only start: its state is set)
+    uint32_t bits = SUMMARY || !packed ? 0u : fresh_map(fresh_args()).start_bits(t0 + k) & valid;
+    if (k == 0) bits &= ~1u;
+    const int pleft = fresh(pleft0), bleft = fresh(bleft0);
     const bool in = st.inside(k, len, packed);
     const typename St::Vec uu = st.u, zz = st.z;
     {
@@ -195,7 +183,7 @@ __global__ __launch_bounds__(SL::kThr) void ssm_fwd_kernel(SsmParams p) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) y[j] = n == 0 ? x[j][n] * f.c[j][n] : __builtin_fmaf(x[j][n], f.c[j][n], y[j]);
         const float yt = tokens_over_lanes<LPC>(y);
-        if (q < 4) sY[i + q][ch] = yt;
+        if (LPC == 4 || q < 4) sY[i + q][ch] = yt;
       }
     };
     if (bits == 0) {
