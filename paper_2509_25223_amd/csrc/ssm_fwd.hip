@@ -245,45 +245,82 @@ __global__ __launch_bounds__(kThreads) void ssm_empty_kernel(const int32_t* empt
   }
 }
 
-// Single tokens.  A lane holds NS states of a channel through the call's tokens: the
-// states are read and written once, which is what the call costs (HBM).
-template <typename T, typename SL>
+// Single tokens.  A lane holds NS states of a channel of SEQS sequences through the
+// call's tokens: the states are read and written once, which is what the call costs
+// (HBM).  A workgroup's life is little more than one round of loads, so what is in
+// flight bounds the rate: with one sequence a lane 4 KB a workgroup, 32 KB a CU.  Two
+// sequences a lane from kPairWgs workgroups of one each: 4096 channels of 16 states,
+// bf16, n sequences, time a call in us (states cold) with one / two / four a lane
+//   n     16           32           64            128           256
+//    5.0/5.0/6.0  7.5/6.3/6.8  12.7/10.5/9.3  21.8/18.1/17.3  39.0/32.6/35.0
+// (256: 4.1 TB/s).  A call of pairs touches its states once: past the caches.
+constexpr int64_t kPairWgs = 2048;
+template <typename T, typename SL, int SEQS>
 __global__ __launch_bounds__(SL::kThr) void ssm_decode_kernel(SsmParams p) {
   constexpr int NS = SL::NS, LPC = SL::LPC;
+  typedef typename RowVec<float, NS>::type States;
   const int q = SL::q(), n0 = q * NS;
-  const int64_t id = (int64_t)blockIdx.x * SL::kCB + SL::ch();   // (sequence, channel)
-  if (id >= p.map.nseq * p.D) return;   // whole channels of lanes
-  const int64_t s = id / p.D, c = id - s * p.D, g = c / p.Dg;
+  const int64_t id = (int64_t)blockIdx.x * SL::kCB + SL::ch();   // (group of sequences, channel)
+  const int64_t groups = (p.map.nseq + SEQS - 1) / SEQS;
+  if (id >= groups * p.D) return;   // whole channels of lanes
+  const int64_t s0 = (uint32_t)id / (uint32_t)p.D, c = id - s0 * p.D, g = (uint32_t)c / (uint32_t)p.Dg;
   const int nleft = (int)p.N - n0;
-  float A2[NS], h[NS];
-  if (p.h0) load_states<NS>(p.h0 + id * p.N + n0, nleft, h);
-  else
+  auto seq = [&](int i) { return min(s0 * SEQS + i, (int64_t)p.map.nseq - 1); };   // past the last: the last, not stored
+  float A2[NS], h[SEQS][NS];
 #pragma unroll
-    for (int n = 0; n < NS; ++n) h[n] = 0.f;
+  for (int i = 0; i < SEQS; ++i) {
+    const float* from = p.h0 + (seq(i) * p.D + c) * p.N + n0;
+    if (!p.h0) {
+#pragma unroll
+      for (int n = 0; n < NS; ++n) h[i][n] = 0.f;
+    } else if (SEQS > 1 && p.N == SL::NP) {
+      const States v = __builtin_nontemporal_load(reinterpret_cast<const States*>(from));
+#pragma unroll
+      for (int n = 0; n < NS; ++n) h[i][n] = v[n];
+    } else {
+      load_states<NS>(from, nleft, h[i]);
+    }
+  }
   load_states<NS>(p.A + c * p.N + n0, nleft, A2);
 #pragma unroll
   for (int n = 0; n < NS; ++n) A2[n] *= kLog2e;
   const float bias = p.dbias ? p.dbias[c] : 0.f, skip = p.skip ? p.skip[c] : 0.f;
   for (int64_t k = 0; k < p.map.T; ++k) {
-    const int64_t t = s * p.map.T + k;
-    const float u = to_f<T>(reinterpret_cast<const T*>(p.u)[t * p.us + c]);
-    const float raw = to_f<T>(reinterpret_cast<const T*>(p.delta)[t * p.dts + c]) + bias;
-    const float z = p.z ? to_f<T>(reinterpret_cast<const T*>(p.z)[t * p.zs + c]) : 0.f;
-    float b[NS], cc[NS], y = 0.f;
-    load_piece<T, NS>(reinterpret_cast<const T*>(p.B) + t * p.bs + g * p.N + n0, nleft, b);
-    load_piece<T, NS>(reinterpret_cast<const T*>(p.C) + t * p.cs + g * p.N + n0, nleft, cc);
-    const float step = p.softplus ? softplus_exact(raw) : raw, x = step * u;
+    T u[SEQS], d[SEQS], z[SEQS];
+    typename RowVec<T, NS>::type b[SEQS], cc[SEQS];
 #pragma unroll
-    for (int n = 0; n < NS; ++n) {
-      h[n] = __builtin_fmaf(__builtin_amdgcn_exp2f(step * A2[n]), h[n], x * b[n]);
-      y = __builtin_fmaf(h[n], cc[n], y);
+    for (int i = 0; i < SEQS; ++i) {
+      const int64_t t = seq(i) * p.map.T + k;
+      u[i] = reinterpret_cast<const T*>(p.u)[t * p.us + c];
+      d[i] = reinterpret_cast<const T*>(p.delta)[t * p.dts + c];
+      z[i] = p.z ? reinterpret_cast<const T*>(p.z)[t * p.zs + c] : u[i];
+      load_raw<T, NS>(reinterpret_cast<const T*>(p.B) + t * p.bs + g * p.N + n0, nleft, b[i]);
+      load_raw<T, NS>(reinterpret_cast<const T*>(p.C) + t * p.cs + g * p.N + n0, nleft, cc[i]);
     }
-    y = group_sum<LPC>(y);
-    y = __builtin_fmaf(skip, u, y);
-    if (p.z) y *= z * sigmoid_fast(z);
-    if (q == 0) reinterpret_cast<T*>(p.o)[t * p.D + c] = from_f<T>(y);
+#pragma unroll
+    for (int i = 0; i < SEQS; ++i) {
+      const float uf = to_f<T>(u[i]), raw = to_f<T>(d[i]) + bias, zf = to_f<T>(z[i]);
+      const float step = p.softplus ? softplus_exact(raw) : raw, x = step * uf;
+      float y = 0.f;
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        h[i][n] = __builtin_fmaf(__builtin_amdgcn_exp2f(step * A2[n]), h[i][n], x * to_f<T>(b[i][n]));
+        y = __builtin_fmaf(h[i][n], to_f<T>(cc[i][n]), y);
+      }
+      y = group_sum<LPC>(y);
+      y = __builtin_fmaf(skip, uf, y);
+      if (p.z) y *= zf * sigmoid_fast(zf);
+      if (q == 0 && s0 * SEQS + i < p.map.nseq)
+        reinterpret_cast<T*>(p.o)[((s0 * SEQS + i) * p.map.T + k) * p.D + c] = from_f<T>(y);
+    }
   }
-  store_piece<float, NS>(p.hfin + id * p.N + n0, nleft, h);
+#pragma unroll
+  for (int i = 0; i < SEQS; ++i) {
+    if (s0 * SEQS + i >= p.map.nseq) break;
+    float* to = p.hfin + ((s0 * SEQS + i) * p.D + c) * p.N + n0;
+    if (SEQS > 1 && p.N == SL::NP) store_piece<float, NS, true, true>(to, NS, h[i]);
+    else store_piece<float, NS>(to, nleft, h[i]);
+  }
 }
 
 template <typename T, typename SL> hipError_t forward(const SsmParams& p, hipStream_t stream) {
@@ -297,11 +334,14 @@ template <typename T, typename SL> hipError_t forward(const SsmParams& p, hipStr
   hipLaunchKernelGGL((ssm_fwd_kernel<T, SL, false>), grid, dim3(SL::kThr), 0, stream, p);
   return hipGetLastError();
 }
-template <typename T, typename SL> hipError_t decode(const SsmParams& p, hipStream_t stream) {
-  const int64_t wgs = (p.map.nseq * p.D + SL::kCB - 1) / SL::kCB;
-  if (wgs > INT32_MAX) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((ssm_decode_kernel<T, SL>), dim3((uint32_t)wgs), dim3(SL::kThr), 0, stream, p);
+template <typename T, typename SL, int SEQS> hipError_t decode_run(const SsmParams& p, hipStream_t stream) {
+  const int64_t wgs = ((p.map.nseq + SEQS - 1) / SEQS * p.D + SL::kCB - 1) / SL::kCB;
+  if (wgs > INT32_MAX / SL::kCB) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((ssm_decode_kernel<T, SL, SEQS>), dim3((uint32_t)wgs), dim3(SL::kThr), 0, stream, p);
   return hipGetLastError();
+}
+template <typename T, typename SL> hipError_t decode(const SsmParams& p, hipStream_t stream) {
+  return p.map.nseq * p.D / SL::kCB >= kPairWgs ? decode_run<T, SL, 2>(p, stream) : decode_run<T, SL, 1>(p, stream);
 }
 
 template <typename T> hipError_t dispatch(const SsmParams& p, bool single, hipStream_t stream) {
