@@ -77,13 +77,13 @@ hipError_t launch_ssm_backward(const SsmParams& p, bool bf16, hipStream_t stream
 // ---------------------------------------------------------------------------
 constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.693147180559945f;
 
-// log(1 + e^x) to a few ulp: with w = 1 + e rounded, log(w) e / (w - 1) corrects the
-// rounding of w to first order (a plain log(1 + e) loses all digits of small steps)
+// log(1 + e^x) = max(x, 0) + log(1 + e) with e = e^-|x| <= 1.  With w = 1 + e rounded,
+// what the rounding took, e - (w - 1), is added to log(w): to first order the lost part
+// over w, and over 1 instead of w it is off by e 2^-24 (a plain log(1 + e) loses all
+// digits of small steps).
 __device__ __forceinline__ float softplus_exact(float x) {
-  const float e = __expf(x), w = 1.f + e, d = w - 1.f;
-  const float l = __builtin_amdgcn_logf(w) * kLn2;
-  const float s = d == 0.f ? e : l * e * __builtin_amdgcn_rcpf(d);
-  return x > 20.f ? x : s;
+  const float e = __builtin_amdgcn_exp2f(-kLog2e * __builtin_fabsf(x)), w = 1.f + e;
+  return fmaxf(x, 0.f) + __builtin_fmaf(__builtin_amdgcn_logf(w), kLn2, e - (w - 1.f));
 }
 
 template <int NS_, int LPC_, int W_ = 4> struct SsmLanes {

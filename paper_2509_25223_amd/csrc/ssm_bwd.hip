@@ -13,7 +13,7 @@
 // Two sums cross lanes.  Those over a channel's states are over a quad (or 8, 16
 // lanes); four tokens are reduced together and left on one lane each.  Those over
 // channels (dB, dC) are 4 tokens x NS states a lane over the wave's channels,
-// halved lane bit by lane bit (2 to 3 instructions a pair, where a sum of one value
+// halved lane bit by lane bit (two instructions a pair, where a sum of one value
 // over 16 lanes costs 4 a value); then over the waves in LDS, and over the blocks
 // of channels by a last kernel, from fp32 partial sums.  No atomics.
 #include "ssm.hpp"
@@ -38,6 +38,27 @@ __device__ __forceinline__ float across4(float x) {
   y = __builtin_amdgcn_update_dpp(y, __builtin_bit_cast(int, x), 0x114, 0xF, 0xA, false);       // row_shr:4
   return __builtin_bit_cast(float, y);
 }
+// The same halving by lane bit 3, of (a0, a2) and of (a1, a3): an add that the lanes of
+// two of a row's four banks execute, then one for the other two (selecting what to add
+// first takes three instructions, not two).  In asm, as the compiler knows no masked
+// add; a value just written may be read across lanes two instructions later.
+__device__ __forceinline__ void half8(float a0, float a1, float a2, float a3, float& b0, float& b1) {
+  asm("s_nop 1\n\t"
+      "v_add_f32_dpp %0, %2, %2 row_ror:8 row_mask:0xf bank_mask:0x3\n\t"
+      "v_add_f32_dpp %1, %3, %3 row_ror:8 row_mask:0xf bank_mask:0x3\n\t"
+      "v_add_f32_dpp %0, %4, %4 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+      "v_add_f32_dpp %1, %5, %5 row_ror:8 row_mask:0xf bank_mask:0xc"
+      : "=&v"(b0), "=&v"(b1) : "v"(a0), "v"(a1), "v"(a2), "v"(a3));
+}
+// and by lane bit 2
+__device__ __forceinline__ float half4(float b0, float b1) {
+  float c;
+  asm("s_nop 1\n\t"
+      "v_add_f32_dpp %0, %1, %1 row_shl:4 row_mask:0xf bank_mask:0x5\n\t"
+      "v_add_f32_dpp %0, %2, %2 row_shr:4 row_mask:0xf bank_mask:0xa"
+      : "=&v"(c) : "v"(b0), "v"(b1));
+  return c;
+}
 
 // v[j][n] summed over the wave's channels.  The lane keeps kKeep values, of token
 // `tok` and the states from `st` on.
@@ -52,7 +73,6 @@ template <typename SL> struct ChannelSums {
     else return (lane >> 3 & 1) * 2 + (lane >> 2 & 1);
   }
   __device__ __forceinline__ static void run(const float (&v)[4][NS], float (&out)[kKeep]) {
-    const int lane = threadIdx.x;
     float a[NS];
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
@@ -63,19 +83,20 @@ template <typename SL> struct ChannelSums {
 #pragma unroll
       for (int n = 0; n < NS; ++n) out[n] = a[n];
     } else {
-      const bool b3 = lane & 8;
       float b[NS / 2];
-#pragma unroll
-      for (int n = 0; n < NS / 2; ++n)
-        b[n] = (b3 ? a[n + NS / 2] : a[n]) + lane_dpp<0x128>(b3 ? a[n] : a[n + NS / 2]);   // row_ror:8
+      if constexpr (NS == 2) {
+        const bool b3 = threadIdx.x & 8;
+        b[0] = (b3 ? a[1] : a[0]) + lane_dpp<0x128>(b3 ? a[0] : a[1]);   // row_ror:8
+      } else {
+        half8(a[0], a[1], a[2], a[3], b[0], b[1]);
+      }
       if constexpr (LPC == 8) {
 #pragma unroll
         for (int n = 0; n < NS / 2; ++n) out[n] = b[n];
       } else if constexpr (NS == 2) {
         out[0] = b[0] + across4(b[0]);
       } else {
-        const bool b2 = lane & 4;
-        out[0] = (b2 ? b[1] : b[0]) + across4(b2 ? b[0] : b[1]);
+        out[0] = half4(b[0], b[1]);
       }
     }
   }
@@ -384,24 +405,18 @@ __global__ __launch_bounds__(SL::kThr, 2) void ssm_bwd_kernel(SsmParams p) {
         for (int j = 0; j < 4; ++j)
 #pragma unroll
           for (int n = 0; n < NS; ++n) x[j][n] = sB[i + j][n0 + n];
-        over4([&](auto J) {
-          constexpr int j = decltype(J)::value;
-          const float xj = quad_lane<j>(xv);
-#pragma unroll
-          for (int n = 0; n < NS; ++n) x[j][n] *= xj;
-        });
         // the states again, from the decays; dy h for dC
         float ht[NS];
 #pragma unroll
         for (int n = 0; n < NS; ++n) ht[n] = hg[i / 4][n];
         over4([&](auto J) {
           constexpr int j = decltype(J)::value;
-          const float gj = quad_lane<j>(gv);
+          const float gj = quad_lane<j>(gv), xj = quad_lane<j>(xv);
           if (inside(i + j))
 #pragma unroll
             for (int n = 0; n < NS; ++n) {
               ah[j][n] = decay[i + j][n] * ht[n];
-              ht[n] = ah[j][n] + x[j][n];
+              ht[n] = __builtin_fmaf(xj, x[j][n], ah[j][n]);
             }
 #pragma unroll
           for (int n = 0; n < NS; ++n) v[j][n] = inside(i + j) ? gj * ht[n] : 0.f;
