@@ -5,7 +5,13 @@
 // neighbour's last) and written once.  A thread owns the 16-byte piece of a
 // row (8 bf16 or 4 fp32 channels) and walks a stretch of tokens with the last
 // W - 1 rows in registers, so the taps cost no loads; the lanes of a wave take
-// adjacent pieces of one row.
+// adjacent pieces of one row, so that every access of a wave is 1 KB of adjacent bytes.
+// bf16, four taps, bias and SiLU, us (and of the 5.4 TB/s of a large copy's traffic):
+//   forward, 16384 x 6144 (403 MB)             82.5   4.9 TB/s
+//   forward, 20011 x 2048 packed, of wider rows 36.4   4.5 TB/s
+//   gradients, 16384 x 6144 (604 MB)            136   4.4 TB/s
+// The forward has its loads in flight a batch of 8 rows ahead of their use; in the
+// gradients, SiLU' is some 25 instructions a value and shares the time with the loads.
 //
 // Rows before a sequence's start are its state's, [W-1][D] with the oldest first:
 // the row m before the start is state row W-2-m.
@@ -219,7 +225,7 @@ __global__ __launch_bounds__(kThreads) void conv_decode_kernel(ConvParams p, uin
 // ---------------------------------------------------------------------------
 constexpr int kBwdTokens = 32;
 
-constexpr int kBwdV = 4;   // channels a thread: 8 spill past 2 waves a SIMD
+constexpr int kBwdV = 4;   // channels a thread (8: registers for two waves a SIMD only)
 
 template <typename T, int W, bool SILU, bool NT, bool FULL>
 __device__ __forceinline__ void conv_bwd_stretch(const ConvParams& p, int64_t t0, int64_t c, int left, float (&dw)[kBwdV * W],
@@ -349,8 +355,8 @@ __device__ __forceinline__ void conv_bwd_stretch(const ConvParams& p, int64_t t0
 }
 
 // lanes: adjacent pieces (kLanes of them), then stretches
-// (three waves a SIMD: 154 us for 16384 tokens x 6144 channels of bf16, two 162, four 268
-// with what they spill)
+// (three waves a SIMD: two took 1.05 times as long for 16384 tokens x 6144 channels of
+// bf16, four, which spill, 1.74 times)
 template <typename T, int W, bool SILU, bool NT>
 __global__ __launch_bounds__(kThreads, 3) void conv_bwd_kernel(ConvParams p, uint32_t lanes, uint32_t groups,
                                                             uint32_t main_wgs) {
@@ -404,9 +410,9 @@ BwdGrid bwd_grid(int64_t ntok, int64_t D) {
   return BwdGrid{lanes, (uint32_t)((pieces + lanes - 1) / lanes), (ntok + per - 1) / per};
 }
 
-// Stretches of 16 tokens, or of 4 where those would leave most of the card idle (16:
-// 96 us for 16384 tokens x 6144 channels of bf16, 35 for 20011 x 2048; 8: 100 and 38;
-// 32: 96 and 42).
+// Stretches of 16 tokens, or of 4 where those would leave most of the card idle.  With
+// ordinary stores, 16: 96 us for 16384 tokens x 6144 channels of bf16, 35 for 20011 x
+// 2048; 8: 100 and 38; 32: 96 and 42.
 constexpr int64_t kFillThreads = 256 * 4 * 64 * 2;
 
 template <typename T, int W, int TT, bool SILU, bool NT>

@@ -11,6 +11,12 @@
 // first (NormGrad).  Weight
 // gradients: a lane keeps the sums of its columns over all its rows, written
 // once per workgroup (or group of lanes) and summed by launch_column_sums.
+//
+// bf16, rows of 2048 with an fp32 stream (16384 of them) and of 128 (262144), us:
+//   addnorm forward 86 (403 MB, 4.7 TB/s), gradients 109 (470 MB, 4.3 TB/s)
+//   gatenorm forward 32 (201 MB, 6.3 TB/s: a part from the 256 MB last-level cache),
+//   gradients 59 (336 MB, 5.7 TB/s)
+// Of a few rows, 4.4 to 6 us: a launch and two dependent round trips to memory.
 #include "layer.hpp"
 
 namespace rla {

@@ -11,6 +11,12 @@
 // chunk's end state from a zero start and the sum of its steps s; since the decay
 // over a chunk is exp(A sum s), the second pass folds the chunks before its own
 // into its start state by itself.
+//
+// Four lanes of four states with as many chunks as fill the card, against eight lanes of
+// two states, which fill it without chunks: 16384 tokens in 4 sequences x 4096 channels
+// x 16 states, bf16, forward 161 + 347 against 490 us, gradients 200 + 1161 against 1547
+// (the sums over a channel's lanes and what is once per channel double with the lanes).
+// Eight waves a workgroup instead of four: forward 527, gradients 1660.
 #pragma once
 
 #include "layer.hpp"
