@@ -13,7 +13,7 @@
 // once per workgroup (or group of lanes) and summed by launch_column_sums.
 //
 // bf16, rows of 2048 with an fp32 stream (16384 of them) and of 128 (262144), us:
-//   addnorm forward 86 (403 MB, 4.7 TB/s), gradients 109 (470 MB, 4.3 TB/s)
+//   addnorm forward 86 (403 MB, 4.7 TB/s), gradients 109 (604 MB, 5.5 TB/s)
 //   gatenorm forward 32 (201 MB, 6.3 TB/s: a part from the 256 MB last-level cache),
 //   gradients 59 (336 MB, 5.7 TB/s)
 // Of a few rows, 4.4 to 6 us: a launch and two dependent round trips to memory.
@@ -504,7 +504,7 @@ struct Shape {
 // addnorm forward: a wave a row up to 4 pieces a lane, then a workgroup, then two passes.
 // Backward, where a lane holds its columns' sums beside the row: a wave a row of one
 // piece a lane, then a workgroup (16384 rows of 2048 bf16 values with an fp32 stream: a
-// wave with 4 pieces 195 us, one to a SIMD).
+// wave with 4 pieces 195 us, one to a SIMD; a workgroup 109).
 Shape addnorm_shape(int64_t width, int V, bool backward) {
   const int64_t pieces = (width + V - 1) / V;
   if (pieces <= 64) return Shape{64, 1};
