@@ -51,19 +51,72 @@ __device__ __forceinline__ float tap_sum(const float (&w)[V * W], float bias, in
   return __builtin_fmaf(w[e * W + W - 1], x, s);
 }
 
+// Packed sequences without a map (few of them): offset i, the running maximum being the
+// caller's.  The same value in every lane, loaded as scalars.
+__device__ __forceinline__ int32_t offset(const ConvParams& p, int i) {
+  const int32_t v = ((ConstPtr<int32_t>)(uint64_t)p.cu)[min(i, p.map.nseq)];
+  return min(max(v, 0), (int32_t)p.map.ntok);
+}
+__device__ __forceinline__ int seq_of(const ConvParams& p, int64_t t) {
+  if (!p.cu) return p.map.seq_of(t);
+  int32_t m = 0, below = 0;   // offsets up to t
+  for (int i = 0; i <= p.map.nseq; ++i) {
+    m = max(m, offset(p, i));
+    below += m <= (int32_t)t ? 1 : 0;
+  }
+  return below > p.map.nseq ? -1 : below - 1;
+}
+__device__ __forceinline__ bool is_empty(const ConvParams& p, int n) {
+  if (!p.cu) return p.map.empty[n];
+  int32_t m = 0;
+  for (int i = 0; i <= n; ++i) m = max(m, offset(p, i));
+  return offset(p, n + 1) <= m;
+}
+
+// Tokens t and around: bit i of `before`: token t - i starts a sequence (i < 3); bit i of
+// `bits`: token t + i does (i < 32, with WIDE 64; set past the end); t's sequence.
+template <bool WIDE>
+__device__ __forceinline__ void tokens_around(const ConvParams& p, int64_t t, bool want, uint32_t& before, uint64_t& bits,
+                                              int& n) {
+  if (p.cu) {
+    uint64_t b = t < 3 ? 7ull >> t : 0ull;   // bit i: token t - 2 + i; token 0 and those in front
+    int32_t m = 0, below = 0;
+    constexpr int U = 8;
+    for (int i0 = 0; i0 <= p.map.nseq; i0 += U) {
+      int32_t v[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) v[i] = offset(p, i0 + i);   // (past the last: the last again)
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        m = max(m, v[i]);
+        const uint32_t d = (uint32_t)(m - (int32_t)t + 2);
+        b |= d < 64 ? 1ull << d : 0ull;
+        below += i0 + i <= p.map.nseq && m <= (int32_t)t ? 1 : 0;
+      }
+    }
+    const int64_t left = p.map.ntok - t + 2;
+    if (left < 64) b |= ~0ull << left;
+    before = (uint32_t)((b >> 2 & 1) | (b & 2) | (b << 2 & 4));
+    bits = b >> 2;
+    n = below > p.map.nseq ? -1 : below - 1;
+    return;
+  }
+  bits = p.map.start_bits(t);
+  before = (uint32_t)bits & 1u;
+  const int64_t t1 = t > 2 ? t - 2 : 0;
+  const uint32_t near = p.map.start_bits(t1);
+#pragma unroll
+  for (int i = 1; i < 3; ++i) before |= (t - i < 0 ? 1u : (near >> (t - i - t1)) & 1u) << i;
+  if constexpr (WIDE) bits |= t + 32 < p.map.ntok ? (uint64_t)p.map.start_bits(t + 32) << 32 : ~0ull << 32;
+  n = want ? p.map.seq_of(t) : 0;
+}
+
 // win[j] = the row before token t by j + 1, from x or the state; returns how many
 // tokens of t's sequence lie before t (W - 1 for that many or more)
 template <typename T, int W, int V, bool FULL>
-__device__ __forceinline__ int load_window(const ConvParams& p, const T* x, int64_t t, int n, int64_t c, int left,
-                                           float (&win)[W - 1][V]) {
+__device__ __forceinline__ int load_window(const ConvParams& p, const T* x, int64_t t, uint32_t before, int n, int64_t c,
+                                           int left, float (&win)[W - 1][V]) {
   int pos = 0;
-  uint32_t before = p.map.start_bits(t) & 1u;   // bit i: token t - i is a start
-  if constexpr (W > 2) {
-    const int64_t t1 = t > W - 2 ? t - (W - 2) : 0;
-    const uint32_t bits = p.map.start_bits(t1);
-#pragma unroll
-    for (int i = 1; i < W - 1; ++i) before |= (t - i < 0 ? 1u : (bits >> (t - i - t1)) & 1u) << i;
-  }
   while (pos < W - 1 && !((before >> pos) & 1u)) ++pos;
 #pragma unroll
   for (int j = 0; j < W - 1; ++j) {
@@ -89,9 +142,12 @@ __device__ __forceinline__ void conv_fwd_stretch(const ConvParams& p, int64_t t0
   T* fin = reinterpret_cast<T*>(p.state_fin);
   float w[V * W], bias[V], win[W - 1][V];
   load_taps<W, V, FULL>(p, c, left, w, bias);
-  const uint32_t bits = p.map.start_bits(t0);
-  int n = p.map.seq || p.state0 || fin ? p.map.seq_of(t0) : 0;
-  load_window<T, W, V, FULL>(p, x, t0, n, c, left, win);
+  uint32_t before;
+  uint64_t around;
+  int n;
+  tokens_around<false>(p, t0, p.map.seq || p.state0 || fin, before, around, n);
+  const uint32_t bits = (uint32_t)around;
+  load_window<T, W, V, FULL>(p, x, t0, before, n, c, left, win);
   auto token = [&](const float (&xv)[V], int64_t t) {
     float o[V];
 #pragma unroll
@@ -130,7 +186,7 @@ __device__ __forceinline__ void conv_fwd_stretch(const ConvParams& p, int64_t t0
   const int count = (int)min((int64_t)TT, p.map.ntok - t0);
   for (int k = 0; k < count; ++k) {
     if (k > 0 && ((bits >> k) & 1u)) {
-      n = p.map.seq_of(t0 + k);
+      n = seq_of(p, t0 + k);
       load_state_window<T, W, V, FULL>(p, n, c, left, win);
     }
     float xv[V];
@@ -157,7 +213,7 @@ __device__ __forceinline__ void copy_empty_states(const ConvParams& p, const voi
                                                   uint32_t wgs) {
   const int64_t row = (W - 1) * p.D;
   for (int64_t n = wg; n < p.map.nseq; n += wgs) {
-    if (!p.map.empty[n]) continue;
+    if (!is_empty(p, (int)n)) continue;
     for (int64_t i = threadIdx.x; i < row; i += kThreads)
       reinterpret_cast<T*>(to)[n * row + i] = from ? reinterpret_cast<const T*>(from)[n * row + i] : from_f<T>(0.f);
   }
@@ -238,8 +294,11 @@ __device__ __forceinline__ void conv_bwd_stretch(const ConvParams& p, int64_t t0
   T* dst0 = reinterpret_cast<T*>(p.dstate0);
   float w[V * W], bias[V], win[W - 1][V], g[W - 1][V];
   load_taps<W, V, FULL>(p, c, left, w, bias);
-  int n = p.map.seq_of(t0);
-  const int pos0 = load_window<T, W, V, FULL>(p, x, t0, n, c, left, win);
+  uint32_t before;
+  uint64_t bits;
+  int n;
+  tokens_around<true>(p, t0, true, before, bits, n);
+  const int pos0 = load_window<T, W, V, FULL>(p, x, t0, before, n, c, left, win);
 #pragma unroll
   for (int j = 0; j < W - 1; ++j)
 #pragma unroll
@@ -271,8 +330,6 @@ __device__ __forceinline__ void conv_bwd_stretch(const ConvParams& p, int64_t t0
     }
   };
 
-  const uint64_t bits = (uint64_t)p.map.start_bits(t0) |
-                        (t0 + 32 < p.map.ntok ? (uint64_t)p.map.start_bits(t0 + 32) << 32 : ~0ull << 32);
   if (t0 + TT + W - 1 <= p.map.ntok && (bits & (((1ull << (TT + W - 2)) - 1ull) << 1)) == 0 &&
       !((bits & 1ull) && dst0) && n >= 0) {
     constexpr int U = 5, TE = TT + W - 1;   // tokens a batch, loaded a batch ahead (35 = 7 x 5 for four taps)
@@ -326,13 +383,23 @@ __device__ __forceinline__ void conv_bwd_stretch(const ConvParams& p, int64_t t0
       store_piece<T, V, FULL>(dst0 + ((int64_t)n * (W - 1) + r) * p.D + c, left, v);
     }
   };
+  // rows kAhead tokens ahead of their use (whose they are shows when they are used)
+  constexpr int kAhead = 4;
+  typename RowVec<T, V>::type ax[kAhead], ay[kAhead];
+  auto ahead = [&](int64_t t, int to) {
+    t = min(t, p.map.ntok - 1);
+    load_raw<T, V, FULL>(x + t * p.xs + c, left, ax[to]);
+    load_raw<T, V, FULL>(dy + t * p.dys + c, left, ay[to]);
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) ahead(t0 + i, i);
   for (int k = 0; k <= TT + W - 2; ++k) {
     const int64_t t = t0 + k;
     if (k > 0 && ((bits >> k) & 1ull)) {   // the sequence ended before t (or all tokens did)
 #pragma unroll
       for (int j = 0; j < W - 1; ++j) emit(t, j, g[j], true);
       if (t >= own_end) return;
-      n = p.map.seq_of(t);
+      n = seq_of(p, t);
       start = t;
       load_state_window<T, W, V, FULL>(p, n, c, left, win);
 #pragma unroll
@@ -341,9 +408,18 @@ __device__ __forceinline__ void conv_bwd_stretch(const ConvParams& p, int64_t t0
         for (int e = 0; e < V; ++e) g[j][e] = 0.f;
     }
     float xv[V], dyv[V], done[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      xv[e] = to_f<T>(ax[0][e]);
+      dyv[e] = to_f<T>(ay[0][e]);
+    }
+#pragma unroll
+    for (int i = 1; i < kAhead; ++i) {
+      ax[i - 1] = ax[i];
+      ay[i - 1] = ay[i];
+    }
+    ahead(t + kAhead, kAhead - 1);
     if (n >= 0) {
-      load_piece<T, V, FULL>(x + t * p.xs + c, left, xv);
-      load_piece<T, V, FULL>(dy + t * p.dys + c, left, dyv);
       token(xv, dyv, k < TT, done);
       emit(t + 1, W - 1, done, false);   // the row W - 1 before t
     } else if (k < TT) {   // outside every sequence
@@ -420,7 +496,7 @@ hipError_t forward_run(const ConvParams& p, hipStream_t stream) {
   const int64_t pieces = (p.D + kPiece<T> - 1) / kPiece<T>, count = (p.map.ntok + TT - 1) / TT * pieces;
   if (count > UINT32_MAX - kThreads * (kEmptyWgs + 1)) return hipErrorInvalidValue;
   const uint32_t wgs = (uint32_t)((count + kThreads - 1) / kThreads);
-  const uint32_t extra = p.map.seq && p.state_fin ? kEmptyWgs : 0;
+  const uint32_t extra = (p.map.seq || p.cu) && p.state_fin ? kEmptyWgs : 0;
   hipLaunchKernelGGL((conv_fwd_kernel<T, W, TT, SILU, NT>), dim3(wgs + extra), dim3(kThreads), 0, stream, p,
                      (uint32_t)pieces, (uint32_t)count, wgs);
   return hipGetLastError();
@@ -450,7 +526,7 @@ template <typename T, int W, bool SILU> hipError_t backward_sized(const ConvPara
   const BwdGrid g = bwd_grid(p.map.ntok, p.D);
   const int64_t wgs = g.rows * g.groups;
   if (wgs > INT32_MAX - kEmptyWgs) return hipErrorInvalidValue;
-  const dim3 grid((uint32_t)wgs + (p.map.seq && p.dstate0 ? kEmptyWgs : 0));
+  const dim3 grid((uint32_t)wgs + ((p.map.seq || p.cu) && p.dstate0 ? kEmptyWgs : 0));
   if (p.map.ntok * p.D * (int64_t)sizeof(T) > kNtBytes)
     hipLaunchKernelGGL((conv_bwd_kernel<T, W, SILU, true>), grid, dim3(kThreads), 0, stream, p, g.lanes, g.groups, (uint32_t)wgs);
   else

@@ -90,6 +90,14 @@ size_t conv_map_bytes(const rla_conv_problem* q, const ConvParams& p) {
   return q->cu_seqlens ? token_map_bytes(p.map.ntok, p.map.nseq) : 0;
 }
 
+// Packed: where sequences lie, looked up in place or by a map in ws.
+hipError_t conv_sequences(const rla_conv_problem* q, unsigned char* ws, ConvParams& p, hipStream_t stream) {
+  if (p.map.nseq > kConvInPlace)
+    return launch_token_map(q->cu_seqlens, p.map.nseq, p.map.ntok, ws, true, p.map, stream);
+  p.cu = q->cu_seqlens;
+  return hipSuccess;
+}
+
 rla_status conv_pointers(const rla_conv_problem* q, const ConvParams& p, const void* x, const float* weight,
                          const float* bias, const void* s0) {
   if (!weight || (p.map.ntok > 0 && !x)) return RLA_ERR_NULL_ARG;
@@ -132,9 +140,7 @@ extern "C" rla_status rla_conv_forward(const rla_conv_problem* q, const void* x,
   if (p.map.ntok == 0) return to_status(copy_states(state_init, state_final, sbytes, stream));
   p.x = x; p.weight = weight; p.bias = bias; p.state0 = state_init; p.y = y; p.state_fin = state_final;
   hipError_t e = hipSuccess;
-  if (q->cu_seqlens)
-    e = launch_token_map(q->cu_seqlens, p.map.nseq, p.map.ntok, reinterpret_cast<unsigned char*>(workspace), true,
-                         p.map, stream);
+  if (q->cu_seqlens) e = conv_sequences(q, reinterpret_cast<unsigned char*>(workspace), p, stream);
   if (e == hipSuccess) e = launch_conv_forward(p, q->dtype == RLA_BF16, stream);
   return to_status(e);
 }
@@ -162,7 +168,7 @@ extern "C" rla_status rla_conv_backward(const rla_conv_problem* q, const void* x
   p.part = reinterpret_cast<float*>(ws + map_bytes);
   hipError_t e = hipSuccess;
   if (p.map.ntok == 0) e = copy_states(dstate_final, dstate_init, sbytes, stream);
-  else if (q->cu_seqlens) e = launch_token_map(q->cu_seqlens, p.map.nseq, p.map.ntok, ws, true, p.map, stream);
+  else if (q->cu_seqlens) e = conv_sequences(q, ws, p, stream);
   if (e == hipSuccess) e = launch_conv_backward(p, q->dtype == RLA_BF16, dweight, dbias, stream);
   return to_status(e);
 }
