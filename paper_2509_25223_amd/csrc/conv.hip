@@ -9,7 +9,7 @@
 // bf16, four taps, bias and SiLU, us (and of the 5.4 TB/s of a large copy's traffic):
 //   forward, 16384 x 6144 (403 MB)             82.5   4.9 TB/s
 //   forward, 20011 x 2048 packed, of wider rows 36.4   4.5 TB/s
-//   gradients, 16384 x 6144 (604 MB)            136   4.4 TB/s
+//   gradients, 16384 x 6144 (604 MB)            126   4.8 TB/s
 // The forward has its loads in flight a batch of 8 rows ahead of their use; in the
 // gradients, SiLU' is some 25 instructions a value and shares the time with the loads.
 //
