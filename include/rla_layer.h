@@ -93,7 +93,10 @@ rla_status rla_conv_decode(const rla_conv_problem *problem, const void *x,
  * B and C are shared by the channels of a group: channel c reads group
  * c / (D / groups).  skip (NULL: none), z (NULL: no gate), delta_bias (NULL:
  * none) are optional.  A is used as given (negative in a model that decays).
- * Decays below 2^-126 are zero.
+ * Decays below 2^-126 are zero.  Sizes: channels come in blocks (64 of up to 16
+ * states, 32 of up to 32, 16 of more; a group's last one in part), and a forward or
+ * backward takes fewer than 2^24 (block, sequence) pairs, rla_ssm_decode some
+ * 2^25; more are RLA_ERR_SHAPE.
  * ------------------------------------------------------------------------ */
 typedef struct {
   int64_t batch, seq_len;

@@ -10,6 +10,9 @@
 
 namespace rla {
 
+// Workgroups of kThreads that a launch can have: a HIP grid holds fewer than 2^32 threads.
+constexpr int64_t kMaxWgs = UINT32_MAX / kThreads;
+
 // ---------------------------------------------------------------------------
 // Rows.  V values of a row starting at p, of which n exist.  Activations are
 // aligned to their elements only (odd channel counts, slices of projections):

@@ -389,6 +389,12 @@ rla_status check_ssm(const rla_ssm_problem* q, SsmParams& p) {
   return RLA_OK;
 }
 
+// A forward or a backward: also few enough workgroups for a launch.
+rla_status check_ssm_scan(const rla_ssm_problem* q, SsmParams& p) {
+  const rla_status st = check_ssm(q, p);
+  return st == RLA_OK && ssm_wgs(p) > kMaxWgs ? RLA_ERR_SHAPE : st;
+}
+
 struct SsmPlan {
   size_t map = 0, flags = 0, S = 0, sumd = 0, ck = 0, E = 0, pBC = 0, pA = 0, pD = 0, total = 0;
 };
@@ -449,7 +455,7 @@ size_t ssm_state_bytes(const SsmParams& p) { return (size_t)p.map.nseq * (size_t
 
 extern "C" size_t rla_ssm_workspace_size(const rla_ssm_problem* q, int op) {
   SsmParams p;
-  if (check_ssm(q, p) != RLA_OK || (op != RLA_SSM_FORWARD && op != RLA_SSM_BACKWARD)) return 0;
+  if (check_ssm_scan(q, p) != RLA_OK || (op != RLA_SSM_FORWARD && op != RLA_SSM_BACKWARD)) return 0;
   return plan_ssm(q, p, op == RLA_SSM_BACKWARD).total;
 }
 
@@ -458,7 +464,7 @@ extern "C" rla_status rla_ssm_forward(const rla_ssm_problem* q, const void* u, c
                                       const float* delta_bias, const float* h_init, void* o, float* h_final, int save,
                                       void* workspace, size_t workspace_bytes, void* stream_) {
   SsmParams p;
-  rla_status st = check_ssm(q, p);
+  rla_status st = check_ssm_scan(q, p);
   if (st == RLA_OK) st = ssm_inputs(q, p, u, delta, A, B, C, skip, z, delta_bias, h_init);
   if (st != RLA_OK) return st;
   if (p.map.ntok > 0 && !o) return RLA_ERR_NULL_ARG;
@@ -487,7 +493,7 @@ extern "C" rla_status rla_ssm_backward(const rla_ssm_problem* q, const void* u, 
                                        float* dskip, void* dz, float* ddelta_bias, float* dh_init, int use_saved,
                                        void* workspace, size_t workspace_bytes, void* stream_) {
   SsmParams p;
-  rla_status st = check_ssm(q, p);
+  rla_status st = check_ssm_scan(q, p);
   if (st == RLA_OK) st = ssm_inputs(q, p, u, delta, A, B, C, skip, z, delta_bias, h_init);
   if (st != RLA_OK) return st;
   if (!dA || (skip && !dskip) || (delta_bias && !ddelta_bias)) return RLA_ERR_NULL_ARG;
@@ -530,6 +536,7 @@ extern "C" rla_status rla_ssm_decode(const rla_ssm_problem* q, const void* u, co
   if (st != RLA_OK) return st;
   if (q->cu_seqlens) return RLA_ERR_UNSUPPORTED;
   if (p.map.nseq == 0) return RLA_OK;
+  if (ssm_decode_wgs(p) > kMaxWgs) return RLA_ERR_SHAPE;
   st = ssm_inputs(q, p, u, delta, A, B, C, skip, z, delta_bias, h_in);
   if (st != RLA_OK) return st;
   if (!h_out || (p.map.ntok > 0 && !o)) return RLA_ERR_NULL_ARG;

@@ -74,6 +74,9 @@ inline int ssm_channels(int64_t N) { return N <= 16 ? 64 : N <= 32 ? 32 : 16; }
 
 hipError_t launch_ssm_forward(const SsmParams& p, bool bf16, hipStream_t stream);
 hipError_t launch_ssm_decode(const SsmParams& p, bool bf16, hipStream_t stream);
+// workgroups of a forward or a backward, of single tokens (at most kMaxWgs of them can run)
+inline int64_t ssm_wgs(const SsmParams& p) { return p.G * p.bpg * p.nchunk; }
+int64_t ssm_decode_wgs(const SsmParams& p);
 // Packed: the states of sequences without tokens, `to` = `from` (NULL: zeros).
 hipError_t launch_ssm_empty(const SsmParams& p, const float* from, float* to, hipStream_t stream);
 hipError_t launch_ssm_backward(const SsmParams& p, bool bf16, hipStream_t stream);
@@ -95,6 +98,7 @@ __device__ __forceinline__ float softplus_exact(float x) {
 template <int NS_, int LPC_, int W_ = 4> struct SsmLanes {
   static constexpr int NS = NS_, LPC = LPC_, NP = NS * LPC;
   static constexpr int kW = W_, kThr = 64 * W_;           // waves, threads of a workgroup
+  static_assert(kThr <= kThreads, "kMaxWgs");
   static constexpr int kCW = 64 / LPC, kCB = kW * kCW;    // channels of a wave, of a workgroup
   // rows of LDS tiles [token][channel]: four rows apart on different banks
   static constexpr int kRow = kCB + kCB / 4;

@@ -588,7 +588,7 @@ __global__ __launch_bounds__(kThreads) void ssm_bc_kernel(SsmParams p) {
 }
 
 template <typename T, typename SL> hipError_t backward(const SsmParams& p, hipStream_t stream) {
-  const dim3 grid((uint32_t)(p.G * p.bpg * p.nchunk));
+  const dim3 grid((uint32_t)ssm_wgs(p));
   if (p.cps > 1) {
     const dim3 part((uint32_t)(p.G * p.bpg * (p.map.seq ? p.nchunk : p.nchunk / p.cps * (p.cps - 1))));
     hipLaunchKernelGGL((ssm_rev_kernel<T, SL>), part, dim3(SL::kThr), 0, stream, p);

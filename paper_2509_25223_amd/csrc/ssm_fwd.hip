@@ -328,7 +328,7 @@ __global__ __launch_bounds__(SL::kThr) void ssm_decode_kernel(SsmParams p) {
 }
 
 template <typename T, typename SL> hipError_t forward(const SsmParams& p, hipStream_t stream) {
-  const dim3 grid((uint32_t)(p.G * p.bpg * p.nchunk));   // blocks of channels fastest: rows are contiguous
+  const dim3 grid((uint32_t)ssm_wgs(p));   // blocks of channels fastest: rows are contiguous
   if (p.cps > 1) {
     const dim3 part((uint32_t)(p.G * p.bpg * (p.map.seq ? p.nchunk : p.nchunk / p.cps * (p.cps - 1))));
     hipLaunchKernelGGL((ssm_fwd_kernel<T, SL, true>), part, dim3(SL::kThr), 0, stream, p);
@@ -339,13 +339,12 @@ template <typename T, typename SL> hipError_t forward(const SsmParams& p, hipStr
   return hipGetLastError();
 }
 template <typename T, typename SL, int SEQS> hipError_t decode_run(const SsmParams& p, hipStream_t stream) {
-  const int64_t wgs = ((p.map.nseq + SEQS - 1) / SEQS * p.D + SL::kCB - 1) / SL::kCB;
-  if (wgs > INT32_MAX / SL::kCB) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((ssm_decode_kernel<T, SL, SEQS>), dim3((uint32_t)wgs), dim3(SL::kThr), 0, stream, p);
+  hipLaunchKernelGGL((ssm_decode_kernel<T, SL, SEQS>), dim3((uint32_t)ssm_decode_wgs(p)), dim3(SL::kThr), 0, stream, p);
   return hipGetLastError();
 }
+int decode_seqs(const SsmParams& p) { return p.map.nseq * p.D / ssm_channels(p.N) >= kPairWgs ? 2 : 1; }
 template <typename T, typename SL> hipError_t decode(const SsmParams& p, hipStream_t stream) {
-  return p.map.nseq * p.D / SL::kCB >= kPairWgs ? decode_run<T, SL, 2>(p, stream) : decode_run<T, SL, 1>(p, stream);
+  return decode_seqs(p) == 2 ? decode_run<T, SL, 2>(p, stream) : decode_run<T, SL, 1>(p, stream);
 }
 
 template <typename T> hipError_t dispatch(const SsmParams& p, bool single, hipStream_t stream) {
@@ -359,6 +358,10 @@ template <typename T> hipError_t dispatch(const SsmParams& p, bool single, hipSt
 
 }  // namespace
 
+int64_t ssm_decode_wgs(const SsmParams& p) {
+  const int64_t seqs = decode_seqs(p), cb = ssm_channels(p.N);
+  return ((p.map.nseq + seqs - 1) / seqs * p.D + cb - 1) / cb;
+}
 hipError_t launch_ssm_forward(const SsmParams& p, bool bf16, hipStream_t stream) {
   const hipError_t e = bf16 ? dispatch<u16>(p, false, stream) : dispatch<float>(p, false, stream);
   if (e != hipSuccess || !p.map.seq || !p.hfin) return e;
