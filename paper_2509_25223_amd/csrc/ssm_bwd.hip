@@ -572,18 +572,20 @@ __global__ __launch_bounds__(SL::kThr, 2) void ssm_bwd_kernel(SsmParams p) {
   }
 }
 
-// dB, dC [tokens][G][N] from the blocks' sums (in their order)
+// dB, dC [tokens][G][N] from the blocks' sums (in their order); a value a thread, or
+// several where there are more values than a launch has threads
 template <typename T>
 __global__ __launch_bounds__(kThreads) void ssm_bc_kernel(SsmParams p) {
-  const int64_t per = p.map.ntok * 2 * p.N, i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= per) return;
-  const int64_t t = i / (2 * p.N);
-  const int w = (int)(i / p.N & 1), n = (int)(i % p.N);
-  T* out = reinterpret_cast<T*>(w ? p.dC : p.dB);
-  for (int g = 0; g < p.G; ++g) {
-    float v = 0.f;
-    for (int b = 0; b < p.bpg; ++b) v += p.pBC[((int64_t)g * p.bpg + b) * per + i];
-    out[(t * p.G + g) * p.N + n] = from_f<T>(v);
+  const int64_t per = p.map.ntok * 2 * p.N;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < per; i += (int64_t)gridDim.x * kThreads) {
+    const int64_t t = i / (2 * p.N);
+    const int w = (int)(i / p.N & 1), n = (int)(i % p.N);
+    T* out = reinterpret_cast<T*>(w ? p.dC : p.dB);
+    for (int g = 0; g < p.G; ++g) {
+      float v = 0.f;
+      for (int b = 0; b < p.bpg; ++b) v += p.pBC[((int64_t)g * p.bpg + b) * per + i];
+      out[(t * p.G + g) * p.N + n] = from_f<T>(v);
+    }
   }
 }
 
@@ -599,7 +601,7 @@ template <typename T, typename SL> hipError_t backward(const SsmParams& p, hipSt
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t per = p.map.ntok * 2 * p.N;
-  hipLaunchKernelGGL(ssm_bc_kernel<T>, dim3((uint32_t)((per + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, p);
+  hipLaunchKernelGGL(ssm_bc_kernel<T>, dim3((uint32_t)min((per + kThreads - 1) / kThreads, kMaxWgs)), dim3(kThreads), 0, stream, p);
   return hipGetLastError();
 }
 

@@ -1,0 +1,33 @@
+"""The operators around a mixing layer with more values than a launch holds threads
+(2^32)."""
+import pytest
+import torch
+
+import paper_2509_25223_amd as rla
+from tests import layer_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def test_scan_gradients(device):
+    """dB and dC of 2^25 tokens of 64 states: 2^32 values and more, all written, those of
+    the last sequences right."""
+    B, T, N = (1 << 19) + 3, 64, 64
+    g = torch.Generator(device).manual_seed(0)
+    rnd = lambda *s, dt=torch.bfloat16: torch.randn(*s, dtype=dt, device=device, generator=g)   # noqa: E731
+    u, delta, dO, Bm, C = rnd(B, T, 1), rnd(B, T, 1), rnd(B, T, 1), rnd(B, T, N), rnd(B, T, N)
+    A = -4 * torch.rand(1, N, device=device, generator=g)
+    like = dict(du=u, ddelta=delta, dA=A, dB=Bm, dC=C)
+    grads = {n: torch.full_like(t, float("nan")) for n, t in like.items()}
+    rla.rla_ssm_backward(u, delta, A, Bm, C, dO, grads=grads)
+    torch.cuda.synchronize()
+    for n, t in grads.items():
+        assert not torch.isnan(t).any(), n
+    last = 3
+    v = {n: ref.wide(t[-last:]) for n, t in dict(u=u, delta=delta, B=Bm, C=C).items()}
+    rows = {n: t.reshape(last * T, -1) for n, t in v.items()}
+    o, _ = ref.ssm(rows["u"], rows["delta"], ref.wide(A, False), rows["B"][:, None], rows["C"][:, None], None, None, None,
+                   True, None, [(i * T, (i + 1) * T) for i in range(last)])
+    want = ref.gradients([o], [dO[-last:].cpu().double().reshape(last * T, 1)], v)
+    for n in ("u", "delta", "B", "C"):
+        ref.check("d" + n, grads["d" + n][-last:], want[n], 8 * N + T)
