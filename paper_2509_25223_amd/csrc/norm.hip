@@ -529,10 +529,21 @@ constexpr int64_t kBwdWgs = 512, kBwdRowWgs = 1024, kBwdNarrowWgs = 1024;
 
 template <typename T, typename R, int L, int NP, bool FULL, bool NT>
 hipError_t addnorm_forward(const AddNormParams& p, hipStream_t stream) {
-  const int64_t sub = kThreads / L;
-  hipLaunchKernelGGL((addnorm_fwd_kernel<T, R, L, NP, FULL, NT>), dim3((uint32_t)((p.rows + sub - 1) / sub)),
-                     dim3(kThreads), 0, stream, p);
-  return hipGetLastError();
+  // (more rows than a launch holds: several)
+  constexpr int64_t sub = kThreads / L, most = kMaxWgs * sub;
+  AddNormParams part = p;
+  for (int64_t row = 0; row < p.rows; row += most) {
+    part.rows = min(p.rows - row, most);
+    part.x = reinterpret_cast<const T*>(p.x) + row * p.xs;
+    if (p.residual) part.residual = reinterpret_cast<const R*>(p.residual) + row * p.width;
+    part.n = reinterpret_cast<T*>(p.n) + row * p.width;
+    part.residual_out = reinterpret_cast<R*>(p.residual_out) + row * p.width;
+    hipLaunchKernelGGL((addnorm_fwd_kernel<T, R, L, NP, FULL, NT>), dim3((uint32_t)((part.rows + sub - 1) / sub)),
+                       dim3(kThreads), 0, stream, part);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 template <typename T, typename R, int L, int NP, bool FULL, bool NT>
 hipError_t addnorm_backward(const AddNormParams& p, hipStream_t stream) {

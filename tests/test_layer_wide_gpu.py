@@ -31,3 +31,22 @@ def test_scan_gradients(device):
     want = ref.gradients([o], [dO[-last:].cpu().double().reshape(last * T, 1)], v)
     for n in ("u", "delta", "B", "C"):
         ref.check("d" + n, grads["d" + n][-last:], want[n], 8 * N + T)
+
+
+def test_addnorm(device):
+    """Rows of two values, a wave each: more of them than one launch takes."""
+    rows, D = (1 << 26) + 77, 2
+    g = torch.Generator(device).manual_seed(1)
+    x = torch.randn(rows, D, dtype=torch.bfloat16, device=device, generator=g)
+    res = torch.randn(rows, D, device=device, generator=g)
+    weight, scale = torch.tensor([0.9, 1.3], device=device), torch.tensor([0.5, -2.0], device=device)
+    n, r = torch.full_like(x, float("nan")), torch.full_like(res, float("nan"))
+    rla.rla_addnorm_forward(x, weight, residual=res, scale=scale, out=n, residual_out=r)
+    for at in range(0, rows, 1 << 24):   # (all of them, some at a time)
+        part = slice(at, at + (1 << 24))
+        want_n, want_r = ref.addnorm(x[part].double(), res[part].double(), weight.double(), scale.double())
+        ref.check("n", n[part], want_n.cpu(), 4)
+        ref.check("residual", r[part], want_r.cpu())
+    same = res.clone()
+    n2, _ = rla.rla_addnorm_forward(x, weight, residual=same, scale=scale, residual_out=same)
+    assert torch.equal(n, n2) and torch.equal(r, same)
