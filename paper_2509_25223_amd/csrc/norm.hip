@@ -578,16 +578,28 @@ template <typename T, typename R> hipError_t addnorm(const AddNormParams& p, boo
 
 template <typename T, typename X, int L, int NP, bool FULL, bool NT>
 hipError_t gatenorm_run(const GateNormParams& p, bool backward, hipStream_t stream) {
-  const int64_t sub = kThreads / L;
-  const dim3 grid((uint32_t)(((backward ? p.groups : p.rows) + sub - 1) / sub));
+  constexpr int64_t sub = kThreads / L;
   if (backward) {
+    const dim3 grid((uint32_t)((p.groups + sub - 1) / sub));
     if (p.first) hipLaunchKernelGGL((gatenorm_bwd_kernel<T, X, L, NP, FULL, true, NT>), grid, dim3(kThreads), 0, stream, p);
     else hipLaunchKernelGGL((gatenorm_bwd_kernel<T, X, L, NP, FULL, false, NT>), grid, dim3(kThreads), 0, stream, p);
-  } else {
-    if (p.first) hipLaunchKernelGGL((gatenorm_fwd_kernel<T, X, L, NP, FULL, true, NT>), grid, dim3(kThreads), 0, stream, p);
-    else hipLaunchKernelGGL((gatenorm_fwd_kernel<T, X, L, NP, FULL, false, NT>), grid, dim3(kThreads), 0, stream, p);
+    return hipGetLastError();
   }
-  return hipGetLastError();
+  // (more rows than a launch holds: several, of whole tokens each)
+  const int64_t tokens = p.rows / p.heads, most = kMaxWgs * sub / p.heads;
+  GateNormParams part = p;
+  for (int64_t tok = 0; tok < tokens; tok += most) {
+    part.rows = min(tokens - tok, most) * p.heads;
+    part.x = reinterpret_cast<const X*>(p.x) + tok * p.xs;
+    part.gate = reinterpret_cast<const T*>(p.gate) + tok * p.gs;
+    part.o = reinterpret_cast<T*>(p.o) + tok * p.heads * p.width;
+    const dim3 grid((uint32_t)((part.rows + sub - 1) / sub));
+    if (p.first) hipLaunchKernelGGL((gatenorm_fwd_kernel<T, X, L, NP, FULL, true, NT>), grid, dim3(kThreads), 0, stream, part);
+    else hipLaunchKernelGGL((gatenorm_fwd_kernel<T, X, L, NP, FULL, false, NT>), grid, dim3(kThreads), 0, stream, part);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 template <typename T, typename X, bool FULL, bool NT>
 hipError_t gatenorm_shaped(const GateNormParams& p, bool backward, hipStream_t stream) {

@@ -50,3 +50,19 @@ def test_addnorm(device):
     same = res.clone()
     n2, _ = rla.rla_addnorm_forward(x, weight, residual=same, scale=scale, residual_out=same)
     assert torch.equal(n, n2) and torch.equal(r, same)
+
+
+@pytest.mark.parametrize("first", [False, True])
+def test_gatenorm(device, first):
+    """Heads of one value, 8 lanes each: more of them than one launch takes."""
+    T, H = (1 << 29) // 3 + 50, 3
+    g = torch.Generator(device).manual_seed(2)
+    x = torch.randn(T, H, 1, dtype=torch.bfloat16, device=device, generator=g)
+    gate = torch.randn(T, H, 1, dtype=torch.bfloat16, device=device, generator=g)
+    weight = torch.tensor([[0.9], [1.3], [-2.0]], device=device)
+    o = torch.full_like(x, float("nan"))
+    rla.rla_gatenorm_forward(x, gate, weight, gate_first=first, out=o)
+    for part in (slice(0, 1 << 20), slice(T // 2, T // 2 + 10007), slice(T - (1 << 20), T)):
+        want = ref.gatenorm(x[part].double(), gate[part].double(), weight.double(), first)
+        ref.check("o", o[part], want.cpu(), 4)
+    assert not torch.isnan(o).any()
