@@ -92,14 +92,15 @@ __global__ __launch_bounds__(kThreads) void token_map_kernel(const int32_t* cu, 
   }
 }
 
-// 64 columns a workgroup, 16 groups of rows: a group's rows in order, then the groups.
+// 64 columns a workgroup, from `first` on, 16 groups of rows: a group's rows in order,
+// then the groups.
 constexpr int kSumGroups = 16;
-__global__ __launch_bounds__(64 * kSumGroups) void column_sums_kernel(const float* part, int64_t rows, int64_t cols,
-                                                                      int64_t inner, int32_t outer, float* out,
-                                                                      float* out2) {
+__global__ __launch_bounds__(64 * kSumGroups) void column_sums_kernel(const float* part, int64_t rows, int64_t first,
+                                                                      int64_t cols, int64_t inner, int32_t outer,
+                                                                      float* out, float* out2) {
   __shared__ float s[kSumGroups][64];
   const int lane = threadIdx.x & 63, g = threadIdx.x >> 6;
-  const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+  const int64_t c = first + (int64_t)blockIdx.x * 64 + lane;
   float sum = 0.f;
   if (c < cols) {
     constexpr int kAhead = 16;   // loads in flight
@@ -158,9 +159,16 @@ hipError_t launch_token_map(const int32_t* cu, int32_t nseq, int64_t ntok, unsig
 
 hipError_t launch_column_sums(const float* part, int64_t rows, int64_t cols, int64_t inner, int32_t outer, float* out,
                               float* out2, hipStream_t stream) {
-  hipLaunchKernelGGL(column_sums_kernel, dim3((uint32_t)((cols + 63) / 64)), dim3(64 * kSumGroups), 0, stream, part,
-                     rows, cols, inner, outer, out, out2);
-  return hipGetLastError();
+  // (more columns than a launch holds: several)
+  constexpr int64_t most = UINT32_MAX / (64 * kSumGroups) * 64;
+  for (int64_t c = 0; c < cols; c += most) {
+    const int64_t wgs = (min(cols - c, most) + 63) / 64;
+    hipLaunchKernelGGL(column_sums_kernel, dim3((uint32_t)wgs), dim3(64 * kSumGroups), 0, stream, part, rows, c, cols,
+                       inner, outer, out, out2);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace rla

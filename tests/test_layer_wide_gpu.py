@@ -66,3 +66,19 @@ def test_gatenorm(device, first):
         want = ref.gatenorm(x[part].double(), gate[part].double(), weight.double(), first)
         ref.check("o", o[part], want.cpu(), 4)
     assert not torch.isnan(o).any()
+
+
+def test_gatenorm_weights(device):
+    """A gradient of more than 2^28 weights per head, from one token."""
+    H, d = 1 << 20, 260
+    g = torch.Generator(device).manual_seed(3)
+    x, gate, dO = (torch.randn(1, H, d, dtype=torch.bfloat16, device=device, generator=g) for _ in range(3))
+    weight = 1 + 0.1 * torch.randn(H, d, device=device, generator=g)
+    grads = dict(dx=torch.full_like(x, float("nan")), dgate=torch.full_like(x, float("nan")),
+                 dweight=torch.full_like(weight, float("nan")))
+    rla.rla_gatenorm_backward(dO, x, gate, weight, grads=grads)
+    for part in (slice(0, 2000), slice(H // 2, H // 2 + 2000), slice(H - 30000, H)):
+        # the sum over one token: its gradient times the normalised, gated value
+        want = dO[0, part].double() * ref.rms(x[0, part].double()) * ref.silu(gate[0, part].double())
+        ref.check("dweight", grads["dweight"][part], want.cpu(), 8)
+    assert not any(torch.isnan(t).any() for t in grads.values())
