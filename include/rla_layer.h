@@ -45,6 +45,8 @@ extern "C" {
  * x before a sequence's start is its initial state, zero without one.  A
  * state holds a sequence's last taps - 1 inputs, oldest first, in x's type
  * (exact copies).
+ * Sizes: calls of more than a launch can hold (some 2^38 values, 2^34 of single
+ * tokens) are RLA_ERR_SHAPE.
  * ------------------------------------------------------------------------ */
 typedef struct {
   int64_t batch, seq_len;    /* B, T (packed: 1, all tokens) */

@@ -491,10 +491,11 @@ BwdGrid bwd_grid(int64_t ntok, int64_t D) {
 // 2048; 8: 100 and 38; 32: 96 and 42.
 constexpr int64_t kFillThreads = 256 * 4 * 64 * 2;
 
+int64_t forward_threads(int64_t ntok, int64_t D, int64_t V) { return (ntok + 15) / 16 * ((D + V - 1) / V); }
+
 template <typename T, int W, int TT, bool SILU, bool NT>
 hipError_t forward_run(const ConvParams& p, hipStream_t stream) {
   const int64_t pieces = (p.D + kPiece<T> - 1) / kPiece<T>, count = (p.map.ntok + TT - 1) / TT * pieces;
-  if (count > UINT32_MAX - kThreads * (kEmptyWgs + 1)) return hipErrorInvalidValue;
   const uint32_t wgs = (uint32_t)((count + kThreads - 1) / kThreads);
   const uint32_t extra = (p.map.seq || p.cu) && p.state_fin ? kEmptyWgs : 0;
   hipLaunchKernelGGL((conv_fwd_kernel<T, W, TT, SILU, NT>), dim3(wgs + extra), dim3(kThreads), 0, stream, p,
@@ -502,7 +503,7 @@ hipError_t forward_run(const ConvParams& p, hipStream_t stream) {
   return hipGetLastError();
 }
 template <typename T, int W, bool SILU> hipError_t forward_sized(const ConvParams& p, hipStream_t stream) {
-  const bool small = (p.map.ntok + 15) / 16 * ((p.D + kPiece<T> - 1) / kPiece<T>) < kFillThreads;
+  const bool small = forward_threads(p.map.ntok, p.D, kPiece<T>) < kFillThreads;
   if (small) return forward_run<T, W, 4, SILU, false>(p, stream);
   return p.map.ntok * p.D * (int64_t)sizeof(T) > kNtBytes ? forward_run<T, W, 16, SILU, true>(p, stream)
                                                           : forward_run<T, W, 16, SILU, false>(p, stream);
@@ -513,7 +514,6 @@ template <typename T, int W> hipError_t forward(const ConvParams& p, hipStream_t
 
 template <typename T, int W> hipError_t decode(const ConvParams& p, hipStream_t stream) {
   const int64_t pieces = (p.D + kPiece<T> - 1) / kPiece<T>, count = pieces * p.map.nseq;
-  if (count > UINT32_MAX - kThreads) return hipErrorInvalidValue;
   const dim3 grid((uint32_t)((count + kThreads - 1) / kThreads));
   if (p.silu)
     hipLaunchKernelGGL((conv_decode_kernel<T, W, true>), grid, dim3(kThreads), 0, stream, p, (uint32_t)pieces, (uint32_t)count);
@@ -525,7 +525,6 @@ template <typename T, int W> hipError_t decode(const ConvParams& p, hipStream_t 
 template <typename T, int W, bool SILU> hipError_t backward_sized(const ConvParams& p, hipStream_t stream) {
   const BwdGrid g = bwd_grid(p.map.ntok, p.D);
   const int64_t wgs = g.rows * g.groups;
-  if (wgs > INT32_MAX - kEmptyWgs) return hipErrorInvalidValue;
   const dim3 grid((uint32_t)wgs + ((p.map.seq || p.cu) && p.dstate0 ? kEmptyWgs : 0));
   if (p.map.ntok * p.D * (int64_t)sizeof(T) > kNtBytes)
     hipLaunchKernelGGL((conv_bwd_kernel<T, W, SILU, true>), grid, dim3(kThreads), 0, stream, p, g.lanes, g.groups, (uint32_t)wgs);
@@ -552,6 +551,19 @@ hipError_t launch_conv_forward(const ConvParams& p, bool bf16, hipStream_t strea
 hipError_t launch_conv_decode(const ConvParams& p, bool bf16, hipStream_t stream) { RLA_CONV_DISPATCH(decode); }
 
 int64_t conv_backward_rows(int64_t ntok, int64_t D) { return bwd_grid(ntok, D).rows; }
+
+// (with a workgroup to spare for the last threads, and those of empty sequences)
+bool conv_forward_fits(const ConvParams& p, bool bf16) {
+  return forward_threads(p.map.ntok, p.D, bf16 ? 8 : 4) <= (kMaxWgs - 1 - kEmptyWgs) * kThreads;
+}
+bool conv_backward_fits(const ConvParams& p) {
+  const BwdGrid g = bwd_grid(p.map.ntok, p.D);
+  return g.rows * g.groups <= kMaxWgs - kEmptyWgs;
+}
+bool conv_decode_fits(const ConvParams& p, bool bf16) {
+  const int64_t V = bf16 ? 8 : 4;
+  return (p.D + V - 1) / V * p.map.nseq <= (kMaxWgs - 1) * kThreads;
+}
 
 hipError_t launch_conv_backward(const ConvParams& p, bool bf16, float* dweight, float* dbias, hipStream_t stream) {
   if (p.map.ntok > 0) {

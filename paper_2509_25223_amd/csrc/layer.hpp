@@ -150,6 +150,10 @@ constexpr int32_t kConvInPlace = 24;
 hipError_t launch_conv_forward(const ConvParams& p, bool bf16, hipStream_t stream);
 hipError_t launch_conv_decode(const ConvParams& p, bool bf16, hipStream_t stream);
 int64_t conv_backward_rows(int64_t ntok, int64_t D);
+// few enough workgroups for a launch
+bool conv_forward_fits(const ConvParams& p, bool bf16);
+bool conv_backward_fits(const ConvParams& p);
+bool conv_decode_fits(const ConvParams& p, bool bf16);
 hipError_t launch_conv_backward(const ConvParams& p, bool bf16, float* dweight, float* dbias, hipStream_t stream);
 
 // dst = src (NULL: zeros), `n` 16-bit words

@@ -119,7 +119,8 @@ using namespace rla;
 
 extern "C" size_t rla_conv_workspace_size(const rla_conv_problem* q, int backward) {
   ConvParams p;
-  if (check_conv(q, p) != RLA_OK) return 0;
+  if (check_conv(q, p) != RLA_OK || !(backward ? conv_backward_fits(p) : conv_forward_fits(p, q->dtype == RLA_BF16)))
+    return 0;
   return conv_map_bytes(q, p) + (backward ? conv_part_bytes(p) : 0);
 }
 
@@ -128,6 +129,7 @@ extern "C" rla_status rla_conv_forward(const rla_conv_problem* q, const void* x,
                                        void* workspace, size_t workspace_bytes, void* stream_) {
   ConvParams p;
   rla_status st = check_conv(q, p);
+  if (st == RLA_OK && !conv_forward_fits(p, q->dtype == RLA_BF16)) st = RLA_ERR_SHAPE;
   if (st == RLA_OK) st = conv_pointers(q, p, x, weight, bias, state_init);
   if (st != RLA_OK) return st;
   if (p.map.ntok > 0 && !y) return RLA_ERR_NULL_ARG;
@@ -151,6 +153,7 @@ extern "C" rla_status rla_conv_backward(const rla_conv_problem* q, const void* x
                                         void* dstate_init, void* workspace, size_t workspace_bytes, void* stream_) {
   ConvParams p;
   rla_status st = check_conv(q, p);
+  if (st == RLA_OK && !conv_backward_fits(p)) st = RLA_ERR_SHAPE;
   if (st == RLA_OK) st = conv_pointers(q, p, x, weight, bias, state_init);
   if (st != RLA_OK) return st;
   if (!dweight || (p.map.ntok > 0 && (!dy || !dx))) return RLA_ERR_NULL_ARG;
@@ -181,6 +184,7 @@ extern "C" rla_status rla_conv_decode(const rla_conv_problem* q, const void* x, 
   if (st != RLA_OK) return st;
   if (q->cu_seqlens) return RLA_ERR_UNSUPPORTED;
   if (p.map.nseq == 0) return RLA_OK;
+  if (!conv_decode_fits(p, q->dtype == RLA_BF16)) return RLA_ERR_SHAPE;
   st = conv_pointers(q, p, x, weight, bias, state_in);
   if (st != RLA_OK) return st;
   if (!state_out || (p.map.ntok > 0 && !y)) return RLA_ERR_NULL_ARG;

@@ -8,7 +8,7 @@ import paper_2509_25223_amd as rla
 from paper_2509_25223_amd import layer
 
 FAKE = 0x7f0000000000
-OK, SHAPE, WORKSPACE = 0, 2, 5
+NULL, SHAPE, WORKSPACE = 1, 2, 5
 
 
 @pytest.fixture(scope="module")
@@ -48,3 +48,34 @@ def test_scan(lib, size):
                                   dict(batch=1 << 26, channels=80, states=64)])
 def test_scan_of_single_tokens(lib, size):
     assert lib.rla_ssm_decode(ssm(**size), FAKE, FAKE, FAKE, FAKE, FAKE, None, None, None, FAKE, FAKE, FAKE, None) == SHAPE
+
+
+def conv(**kw):
+    f = dict(batch=1, seq_len=1, channels=4096, taps=4, silu=1, dtype=rla.RLA_BF16)
+    f.update(kw)
+    return rla.rla_conv_problem(**f)
+
+
+@pytest.mark.parametrize("size", [dict(batch=1 << 17, seq_len=1 << 10), dict(seq_len=1 << 27), dict(seq_len=1 << 26, dtype=rla.RLA_F32),
+                                  dict(seq_len=1 << 27, cu_seqlens=FAKE, num_seqs=100)])
+def test_convolution(lib, size):
+    p = conv(**size)
+    assert rla.rla_conv_workspace_size(p, False) == 0
+    assert lib.rla_conv_forward(p, FAKE, FAKE, None, None, FAKE, None, FAKE, 1 << 50, None) == SHAPE
+    # a 32nd less fits: past the shapes, what is missing is the workspace or an output
+    p = conv(**dict(size, seq_len=size["seq_len"] * 31 // 32))
+    want = WORKSPACE if p.cu_seqlens else NULL
+    assert lib.rla_conv_forward(p, FAKE, FAKE, None, None, FAKE if p.cu_seqlens else None, None, None, 0, None) == want
+
+
+@pytest.mark.parametrize("dtype", [rla.RLA_BF16, rla.RLA_F32])
+def test_convolution_gradients(lib, dtype):
+    for seq_len, want in ((1 << 27, SHAPE), ((1 << 27) - (1 << 14), WORKSPACE)):
+        p = conv(seq_len=seq_len, dtype=dtype)
+        assert (rla.rla_conv_workspace_size(p, True) == 0) == (want == SHAPE)
+        assert lib.rla_conv_backward(p, FAKE, FAKE, None, None, FAKE, None, FAKE, FAKE, None, None, None, 0, None) == want
+
+
+def test_convolution_of_single_tokens(lib):
+    for batch, want in ((1 << 23, SHAPE), ((1 << 23) - 1, NULL)):
+        assert lib.rla_conv_decode(conv(batch=batch), FAKE, FAKE, None, FAKE, None, FAKE, None) == want
