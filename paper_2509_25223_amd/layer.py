@@ -8,7 +8,8 @@ Activations are bf16 or fp32, [B, T, ...] or packed [T, ...] with cu_seqlens (in
 [N + 1], device); their rows may lie further apart than they are wide (slices
 of a projection), every other tensor is contiguous.  Parameters, their gradients
 and the scan's states are fp32.  Outputs and workspaces are allocated (on
-`stream`, if given) unless passed in.
+`stream`, if given) unless passed in.  A call runs on its tensors' GPU, whichever
+is the current one; a stream has to be that GPU's.
 """
 from __future__ import annotations
 
@@ -61,17 +62,18 @@ _PROBLEMS = {"conv": rla_conv_problem, "ssm": rla_ssm_problem, "addnorm": rla_ad
              "gatenorm": rla_gatenorm_problem}
 
 
-_bound = _stream_of = None
+_bound = _stream_of = _current = None
 
 
 def _lib():
     """The library with this header's functions typed."""
-    global _bound, torch, _stream_of
+    global _bound, torch, _stream_of, _current
     if _bound is not None:
         return _bound
     import torch as module
     torch = module
     _stream_of = torch._C._cuda_getCurrentRawStream   # of a device, without its object
+    _current = torch._C._cuda_getDevice
     lib = load_library()
     for op, problem in _PROBLEMS.items():
         size = getattr(lib, "rla_%s_workspace_size" % op)
@@ -102,7 +104,21 @@ def _ptr(t):
 
 
 def _stream_handle(stream, index):
-    return _stream_of(index) if stream is None else stream.cuda_stream
+    if stream is None:
+        return _stream_of(index)
+    if stream.device_index != index:
+        raise ValueError("stream must be on GPU %d" % index)
+    return stream.cuda_stream
+
+
+def _elsewhere(call, index):
+    """`call` with GPU `index` the current one, as it has to be where its tensors are
+    there: kernels run on the current device, and a default stream's handle (0) is
+    that device's."""
+    def on_it(*args):
+        with torch.cuda.device(index):
+            return call(*args)
+    return on_it
 
 
 def _code(name, dt):
@@ -289,8 +305,9 @@ def rla_conv_forward(x, weight, bias=None, silu=False, state=None, cu_seqlens=No
     ws, have = None, 0
     if cu_seqlens is not None:
         ws, have = _space(x, lib.rla_conv_workspace_size(problem, 0), workspace, stream)
-    _ok(lib.rla_conv_forward(problem, x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(state), out.data_ptr(),
-                             _ptr(state_final), _ptr(ws), have, _stream_handle(stream, index)), "rla_conv_forward")
+    call = lib.rla_conv_forward if _current() == index else _elsewhere(lib.rla_conv_forward, index)
+    _ok(call(problem, x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(state), out.data_ptr(), _ptr(state_final),
+             _ptr(ws), have, _stream_handle(stream, index)), "rla_conv_forward")
     return out, state_final
 
 
@@ -314,10 +331,10 @@ def rla_conv_backward(x, weight, dy, bias=None, silu=False, state=None, dstate_f
     else:
         _gradients(grads, index, expected)
     ws, have = _space(x, lib.rla_conv_workspace_size(problem, 1), workspace, stream)
-    _ok(lib.rla_conv_backward(problem, x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(state), dy.data_ptr(),
-                              _ptr(dstate_final), grads["dx"].data_ptr(), grads["dweight"].data_ptr(),
-                              _ptr(grads.get("dbias")), _ptr(grads.get("dstate")), ws.data_ptr(), have,
-                              _stream_handle(stream, index)), "rla_conv_backward")
+    call = lib.rla_conv_backward if _current() == index else _elsewhere(lib.rla_conv_backward, index)
+    _ok(call(problem, x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(state), dy.data_ptr(), _ptr(dstate_final),
+             grads["dx"].data_ptr(), grads["dweight"].data_ptr(), _ptr(grads.get("dbias")), _ptr(grads.get("dstate")),
+             ws.data_ptr(), have, _stream_handle(stream, index)), "rla_conv_backward")
     return grads
 
 
@@ -335,8 +352,9 @@ def rla_conv_decode(x, weight, bias=None, silu=False, state=None, state_out=None
         out = _new(x, x.shape, x.dtype, stream)
     if state_out is None:
         state_out = _new(x, shape, x.dtype, stream)
-    _ok(lib.rla_conv_decode(problem, x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(state), out.data_ptr(),
-                            state_out.data_ptr(), _stream_handle(stream, index)), "rla_conv_decode")
+    call = lib.rla_conv_decode if _current() == index else _elsewhere(lib.rla_conv_decode, index)
+    _ok(call(problem, x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(state), out.data_ptr(), state_out.data_ptr(),
+             _stream_handle(stream, index)), "rla_conv_decode")
     return out, state_out
 
 
@@ -410,10 +428,10 @@ def rla_ssm_forward(u, delta, A, B, C, D=None, z=None, delta_bias=None, softplus
         h_final = _new(u, shape, f32, stream)
     op = RLA_SSM_BACKWARD if save_for_backward else RLA_SSM_FORWARD
     ws, have = _space(u, lib.rla_ssm_workspace_size(problem, op), workspace, stream)
-    _ok(lib.rla_ssm_forward(problem, u.data_ptr(), delta.data_ptr(), A.data_ptr(), B.data_ptr(), C.data_ptr(),
-                            _ptr(D), _ptr(z), _ptr(delta_bias), _ptr(h0), out.data_ptr(), _ptr(h_final),
-                            1 if save_for_backward else 0, ws.data_ptr(), have, _stream_handle(stream, index)),
-        "rla_ssm_forward")
+    call = lib.rla_ssm_forward if _current() == index else _elsewhere(lib.rla_ssm_forward, index)
+    _ok(call(problem, u.data_ptr(), delta.data_ptr(), A.data_ptr(), B.data_ptr(), C.data_ptr(), _ptr(D), _ptr(z),
+             _ptr(delta_bias), _ptr(h0), out.data_ptr(), _ptr(h_final), 1 if save_for_backward else 0, ws.data_ptr(),
+             have, _stream_handle(stream, index)), "rla_ssm_forward")
     return out, h_final
 
 
@@ -448,12 +466,12 @@ def rla_ssm_backward(u, delta, A, B, C, dO, D=None, z=None, delta_bias=None, sof
         _gradients(grads, index, expected)
     ws, have = _space(u, lib.rla_ssm_workspace_size(problem, RLA_SSM_BACKWARD), workspace, stream)
     g = grads
-    _ok(lib.rla_ssm_backward(problem, u.data_ptr(), delta.data_ptr(), A.data_ptr(), B.data_ptr(), C.data_ptr(),
-                             _ptr(D), _ptr(z), _ptr(delta_bias), _ptr(h0), dO.data_ptr(), _ptr(dh_final),
-                             g["du"].data_ptr(), g["ddelta"].data_ptr(), g["dA"].data_ptr(), g["dB"].data_ptr(),
-                             g["dC"].data_ptr(), _ptr(g.get("dD")), _ptr(g.get("dz")), _ptr(g.get("ddelta_bias")),
-                             _ptr(g.get("dh0")), 1 if use_saved else 0, ws.data_ptr(), have, _stream_handle(stream, index)),
-        "rla_ssm_backward")
+    call = lib.rla_ssm_backward if _current() == index else _elsewhere(lib.rla_ssm_backward, index)
+    _ok(call(problem, u.data_ptr(), delta.data_ptr(), A.data_ptr(), B.data_ptr(), C.data_ptr(), _ptr(D), _ptr(z),
+             _ptr(delta_bias), _ptr(h0), dO.data_ptr(), _ptr(dh_final), g["du"].data_ptr(), g["ddelta"].data_ptr(),
+             g["dA"].data_ptr(), g["dB"].data_ptr(), g["dC"].data_ptr(), _ptr(g.get("dD")), _ptr(g.get("dz")),
+             _ptr(g.get("ddelta_bias")), _ptr(g.get("dh0")), 1 if use_saved else 0, ws.data_ptr(), have,
+             _stream_handle(stream, index)), "rla_ssm_backward")
     return grads
 
 
@@ -473,9 +491,10 @@ def rla_ssm_decode(u, delta, A, B, C, D=None, z=None, delta_bias=None, softplus=
         out = _new(u, u.shape, u.dtype, stream)
     if h_out is None:
         h_out = _new(u, shape, f32, stream)
-    _ok(lib.rla_ssm_decode(problem, u.data_ptr(), delta.data_ptr(), A.data_ptr(), B.data_ptr(), C.data_ptr(),
-                           _ptr(D), _ptr(z), _ptr(delta_bias), _ptr(h_in), out.data_ptr(), h_out.data_ptr(),
-                           _stream_handle(stream, index)), "rla_ssm_decode")
+    call = lib.rla_ssm_decode if _current() == index else _elsewhere(lib.rla_ssm_decode, index)
+    _ok(call(problem, u.data_ptr(), delta.data_ptr(), A.data_ptr(), B.data_ptr(), C.data_ptr(), _ptr(D), _ptr(z),
+             _ptr(delta_bias), _ptr(h_in), out.data_ptr(), h_out.data_ptr(), _stream_handle(stream, index)),
+        "rla_ssm_decode")
     return out, h_out
 
 
@@ -532,8 +551,9 @@ def rla_addnorm_forward(x, weight, residual=None, scale=None, eps=1e-6, out=None
         out = _new(x, x.shape, x.dtype, stream)
     if residual_out is None:
         residual_out = _new(x, x.shape, rd, stream)
-    _ok(lib.rla_addnorm_forward(problem, x.data_ptr(), _ptr(residual), weight.data_ptr(), _ptr(scale), out.data_ptr(),
-                                residual_out.data_ptr(), _stream_handle(stream, index)), "rla_addnorm_forward")
+    call = lib.rla_addnorm_forward if _current() == index else _elsewhere(lib.rla_addnorm_forward, index)
+    _ok(call(problem, x.data_ptr(), _ptr(residual), weight.data_ptr(), _ptr(scale), out.data_ptr(),
+             residual_out.data_ptr(), _stream_handle(stream, index)), "rla_addnorm_forward")
     return out, residual_out
 
 
@@ -563,10 +583,10 @@ def rla_addnorm_backward(dn, residual_out, weight, x=None, scale=None, dresidual
     else:
         _gradients(grads, index, expected)
     ws, have = _space(dn, lib.rla_addnorm_workspace_size(problem), workspace, stream)
-    _ok(lib.rla_addnorm_backward(problem, dn.data_ptr(), _ptr(dresidual_out), residual_out.data_ptr(), _ptr(x),
-                                 weight.data_ptr(), _ptr(scale), grads["dx"].data_ptr(), grads["dresidual"].data_ptr(),
-                                 grads["dweight"].data_ptr(), _ptr(grads.get("dscale")), ws.data_ptr(), have,
-                                 _stream_handle(stream, index)), "rla_addnorm_backward")
+    call = lib.rla_addnorm_backward if _current() == index else _elsewhere(lib.rla_addnorm_backward, index)
+    _ok(call(problem, dn.data_ptr(), _ptr(dresidual_out), residual_out.data_ptr(), _ptr(x), weight.data_ptr(),
+             _ptr(scale), grads["dx"].data_ptr(), grads["dresidual"].data_ptr(), grads["dweight"].data_ptr(),
+             _ptr(grads.get("dscale")), ws.data_ptr(), have, _stream_handle(stream, index)), "rla_addnorm_backward")
     return grads
 
 
@@ -610,8 +630,9 @@ def rla_gatenorm_forward(x, gate, weight, gate_first=False, eps=1e-6, out=None, 
     _check("out", out, index, x.shape, gate.dtype)
     if out is None:
         out = _new(x, x.shape, gate.dtype, stream)
-    _ok(lib.rla_gatenorm_forward(problem, x.data_ptr(), gate.data_ptr(), weight.data_ptr(), out.data_ptr(),
-                                 _stream_handle(stream, index)), "rla_gatenorm_forward")
+    call = lib.rla_gatenorm_forward if _current() == index else _elsewhere(lib.rla_gatenorm_forward, index)
+    _ok(call(problem, x.data_ptr(), gate.data_ptr(), weight.data_ptr(), out.data_ptr(), _stream_handle(stream, index)),
+        "rla_gatenorm_forward")
     return out
 
 
@@ -628,7 +649,8 @@ def rla_gatenorm_backward(dO, x, gate, weight, gate_first=False, eps=1e-6, grads
     else:
         _gradients(grads, index, expected)
     ws, have = _space(x, lib.rla_gatenorm_workspace_size(problem), workspace, stream)
-    _ok(lib.rla_gatenorm_backward(problem, dO.data_ptr(), x.data_ptr(), gate.data_ptr(), weight.data_ptr(),
-                                  grads["dx"].data_ptr(), grads["dgate"].data_ptr(), grads["dweight"].data_ptr(),
-                                  ws.data_ptr(), have, _stream_handle(stream, index)), "rla_gatenorm_backward")
+    call = lib.rla_gatenorm_backward if _current() == index else _elsewhere(lib.rla_gatenorm_backward, index)
+    _ok(call(problem, dO.data_ptr(), x.data_ptr(), gate.data_ptr(), weight.data_ptr(), grads["dx"].data_ptr(),
+             grads["dgate"].data_ptr(), grads["dweight"].data_ptr(), ws.data_ptr(), have,
+             _stream_handle(stream, index)), "rla_gatenorm_backward")
     return grads
