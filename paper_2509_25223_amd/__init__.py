@@ -136,11 +136,28 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-def _stream_handle(stream):
-    if stream is not None:
-        return ctypes.c_void_p(stream.cuda_stream)
-    torch = _torch()   # the handle of torch.cuda.current_stream(), without its object
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+def _stream_handle(stream, index):
+    """The handle of `stream`, which has to be GPU `index`'s, or of that GPU's current one."""
+    if stream is None:   # (without its object)
+        return _torch()._C._cuda_getCurrentRawStream(index)
+    if stream.device_index != index:
+        raise ValueError("stream must be on GPU %d" % index)
+    return ctypes.c_void_p(stream.cuda_stream)
+
+
+def _on(call, index):
+    """`call` with GPU `index`, where its tensors are, the current one: kernels run on
+    that, and a default stream's handle (0) stands for the current device's."""
+    if index < 0:
+        raise ValueError("tensors must be on a GPU")
+    torch = _torch()
+    if torch._C._cuda_getDevice() == index:
+        return call
+
+    def on_it(*args):
+        with torch.cuda.device(index):
+            return call(*args)
+    return on_it
 
 
 def _dtype_code(dt):
@@ -302,9 +319,10 @@ def _forward(name, op, q, k, v, alpha_s, beta, alpha_r, gamma, clip, S0, R0, cu_
         Sf = torch.empty(shape, dtype=torch.float32, device=dev)
         Rf = torch.empty(shape, dtype=torch.float32, device=dev)
     ws, ws_bytes = _workspace(problem, op, dev, workspace)
-    st = getattr(lib, name)(ctypes.byref(problem), _ptr(q), _ptr(k), _ptr(v), _ptr(alpha_s),
-                            _ptr(beta), _ptr(alpha_r), _ptr(gamma), _ptr(S0), _ptr(R0), _ptr(o),
-                            _ptr(Sf), _ptr(Rf), _ptr(ws), ws_bytes, _stream_handle(stream))
+    index = q.get_device()
+    st = _on(getattr(lib, name), index)(
+        ctypes.byref(problem), _ptr(q), _ptr(k), _ptr(v), _ptr(alpha_s), _ptr(beta), _ptr(alpha_r), _ptr(gamma),
+        _ptr(S0), _ptr(R0), _ptr(o), _ptr(Sf), _ptr(Rf), _ptr(ws), ws_bytes, _stream_handle(stream, index))
     if st != RLA_OK:
         raise RLAError(st, name)
     return o, Sf, Rf
@@ -357,9 +375,10 @@ def rdn_forward_noalloc(q, k, v, alpha_s, beta, alpha_r, gamma, clip: float = 1.
     shape = _state_shape(problem)
     Sf = torch.empty(shape, dtype=torch.float32, device=dev) if S_final is None else S_final
     Rf = torch.empty(shape, dtype=torch.float32, device=dev) if R_final is None else R_final
-    st = lib.rdn_forward_noalloc(ctypes.byref(problem), _ptr(q), _ptr(k), _ptr(v), _ptr(alpha_s),
-                                 _ptr(beta), _ptr(alpha_r), _ptr(gamma), _ptr(S0), _ptr(R0),
-                                 _ptr(o), _ptr(Sf), _ptr(Rf), _stream_handle(stream))
+    index = q.get_device()
+    st = _on(lib.rdn_forward_noalloc, index)(
+        ctypes.byref(problem), _ptr(q), _ptr(k), _ptr(v), _ptr(alpha_s), _ptr(beta), _ptr(alpha_r), _ptr(gamma),
+        _ptr(S0), _ptr(R0), _ptr(o), _ptr(Sf), _ptr(Rf), _stream_handle(stream, index))
     if st != RLA_OK:
         raise RLAError(st, "rdn_forward_noalloc")
     return o, Sf, Rf
@@ -418,12 +437,12 @@ def _backward(name, op, q, k, v, alpha_s, beta, alpha_r, gamma, dO, clip: float 
         grads["ddecay_param"] = ddp
     ws, ws_bytes = _workspace(problem, op, dev, workspace)
     g = grads
-    st = getattr(lib, name)(ctypes.byref(problem), _ptr(q), _ptr(k), _ptr(v), _ptr(alpha_s),
-                          _ptr(beta), _ptr(alpha_r), _ptr(gamma), _ptr(S0), _ptr(R0), _ptr(dO),
-                          _ptr(dS_final), _ptr(dR_final), _ptr(g["dq"]), _ptr(g["dk"]),
-                          _ptr(g["dv"]), _ptr(g["dalpha_s"]), _ptr(g["dbeta"]),
-                          _ptr(g["dalpha_r"]), _ptr(g["dgamma"]), _ptr(g.get("dS0")),
-                          _ptr(g.get("dR0")), _ptr(ws), ws_bytes, _stream_handle(stream))
+    index = q.get_device()
+    st = _on(getattr(lib, name), index)(
+        ctypes.byref(problem), _ptr(q), _ptr(k), _ptr(v), _ptr(alpha_s), _ptr(beta), _ptr(alpha_r), _ptr(gamma),
+        _ptr(S0), _ptr(R0), _ptr(dO), _ptr(dS_final), _ptr(dR_final), _ptr(g["dq"]), _ptr(g["dk"]), _ptr(g["dv"]),
+        _ptr(g["dalpha_s"]), _ptr(g["dbeta"]), _ptr(g["dalpha_r"]), _ptr(g["dgamma"]), _ptr(g.get("dS0")),
+        _ptr(g.get("dR0")), _ptr(ws), ws_bytes, _stream_handle(stream, index))
     if st != RLA_OK:
         raise RLAError(st, name)
     return g
@@ -478,9 +497,10 @@ def _decode(name, q, k, v, alpha_s, beta, alpha_r, gamma, clip, S_in, R_in, S_ou
     if R_out is None:
         R_out = torch.empty(shape, dtype=f32, device=q.device)
     o = torch.empty(v.shape, dtype=odt, device=q.device) if out is None else out
-    st = getattr(lib, name)(problem, q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha_s.data_ptr(),
-                            beta.data_ptr(), alpha_r.data_ptr(), gamma.data_ptr(), _ptr(S_in), _ptr(R_in),
-                            o.data_ptr(), S_out.data_ptr(), R_out.data_ptr(), _stream_handle(stream))
+    st = _on(getattr(lib, name), index)(
+        problem, q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha_s.data_ptr(), beta.data_ptr(), alpha_r.data_ptr(),
+        gamma.data_ptr(), _ptr(S_in), _ptr(R_in), o.data_ptr(), S_out.data_ptr(), R_out.data_ptr(),
+        _stream_handle(stream, index))
     if st != RLA_OK:
         raise RLAError(st, name)
     return o, S_out, R_out
