@@ -86,8 +86,11 @@ size_t conv_part_bytes(const ConvParams& p) {
   return up(sizeof(float) * (size_t)conv_backward_rows(p.map.ntok, p.D) * (size_t)(p.taps + 1) *
             (size_t)p.D);
 }
+// (sequences looked up in place need none; packed calls take a workspace all the same, so
+// that callers need not know how many those are)
 size_t conv_map_bytes(const rla_conv_problem* q, const ConvParams& p) {
-  return q->cu_seqlens ? token_map_bytes(p.map.ntok, p.map.nseq) : 0;
+  if (!q->cu_seqlens) return 0;
+  return p.map.nseq > kConvInPlace ? token_map_bytes(p.map.ntok, p.map.nseq) : kWsAlign;
 }
 
 // Packed: where sequences lie, looked up in place or by a map in ws.

@@ -79,3 +79,17 @@ def test_convolution_gradients(lib, dtype):
 def test_convolution_of_single_tokens(lib):
     for batch, want in ((1 << 23, SHAPE), ((1 << 23) - 1, NULL)):
         assert lib.rla_conv_decode(conv(batch=batch), FAKE, FAKE, None, FAKE, None, FAKE, None) == want
+
+
+def test_workspace_of_few_sequences(lib):
+    """Few packed sequences are looked up in place: what the call asks for does not grow with
+    the tokens, as the map of many sequences does."""
+    def size(n, tokens, backward=False):
+        return rla.rla_conv_workspace_size(conv(seq_len=tokens, channels=64, cu_seqlens=FAKE, num_seqs=n), backward)
+
+    assert 0 < size(3, 100) == size(3, 1 << 20) == size(1, 1 << 26)
+    assert size(200, 1 << 20) > 4 << 20
+    dense = rla.rla_conv_workspace_size(conv(seq_len=1 << 20, channels=64), True)
+    assert size(3, 1 << 20, True) - size(3, 1 << 20) == dense
+    assert lib.rla_conv_forward(conv(seq_len=100, cu_seqlens=FAKE, num_seqs=3), FAKE, FAKE, None, None, FAKE, None, None,
+                                0, None) == WORKSPACE
