@@ -342,7 +342,7 @@ def rla_conv_decode(x, weight, bias=None, silu=False, state=None, state_out=None
     """A few new tokens x [B, T, D] onto the sequences' states [B, taps - 1, D]
     (None: zeros).  Returns (y, state_out); state_out=state updates in place."""
     lib = _lib()
-    if x.dim() != 3:
+    if x is not None and x.dim() != 3:
         raise ValueError("x must be [B, T, D]")
     problem, index, shape = _conv(x, weight, bias, silu, None)
     _check("state", state, index, shape, x.dtype)
@@ -480,7 +480,7 @@ def rla_ssm_decode(u, delta, A, B, C, D=None, z=None, delta_bias=None, softplus=
     """A few new tokens u [B, T, D] onto the states h_in [B, D, states] (None:
     zeros).  Returns (o, h_out); h_out=h_in updates in place."""
     lib = _lib()
-    if u.dim() != 3:
+    if u is not None and u.dim() != 3:
         raise ValueError("u must be [B, T, D]")
     problem, index, shape = _ssm(u, delta, A, B, C, D, z, delta_bias, softplus, None)
     f32 = torch.float32
