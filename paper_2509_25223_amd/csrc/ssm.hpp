@@ -44,12 +44,9 @@ struct SsmParams {
   const float* dhfin = nullptr;
   void* du = nullptr;
   void* ddelta = nullptr;
-  float* dA = nullptr;
   void* dB = nullptr;
   void* dC = nullptr;
-  float* dskip = nullptr;
   void* dz = nullptr;
-  float* ddbias = nullptr;
   float* dh0 = nullptr;
   // workspace (NP: states padded to the kernels' 8, 16, 32 or 64)
   float* S = nullptr;        // [nchunk][D][NP] end states from a zero start
@@ -105,9 +102,6 @@ template <int NS_, int LPC_, int W_ = 4> struct SsmLanes {
   __device__ __forceinline__ static int q() { return (int)threadIdx.x % LPC; }
   __device__ __forceinline__ static int ch() { return (int)threadIdx.x / LPC; }
 };
-
-typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
-typedef float f32x2u __attribute__((ext_vector_type(2), aligned(4)));
 
 // NS floats from 4-byte aligned memory, `left` of which exist
 template <int NS> __device__ __forceinline__ void load_states(const float* p, int left, float (&h)[NS]) {
