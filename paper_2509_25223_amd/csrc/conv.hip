@@ -2,13 +2,14 @@
 //   pre_t = bias + sum_i weight_i x_{t-W+1+i},  y_t = pre_t or SiLU(pre_t)
 // A channel is W multiply-adds a token, so every kernel here is bound by HBM:
 // each value is read once (twice where a stretch's first rows are its
-// neighbour's last) and written once.  A thread owns the 16-byte piece of a
-// row (8 bf16 or 4 fp32 channels) and walks a stretch of tokens with the last
-// W - 1 rows in registers, so the taps cost no loads; the lanes of a wave take
-// adjacent pieces of one row, so that every access of a wave is 1 KB of adjacent bytes.
+// neighbour's last) and written once.  A thread owns a piece of a row (forward and
+// single tokens: 16 bytes, 8 bf16 or 4 fp32 channels; gradients: 4 channels) and
+// walks a stretch of tokens with the last W - 1 rows in registers, so the taps cost no
+// loads; the lanes of a wave take adjacent pieces of one row, so that an access of a
+// wave is 1 KB of adjacent bytes (bf16 gradients: 512).
 // bf16, four taps, bias and SiLU, us (and of the 5.4 TB/s of a large copy's traffic):
-//   forward, 16384 x 6144 (403 MB)             82.5   4.9 TB/s
-//   forward, 20011 x 2048 packed, of wider rows 36.4   4.5 TB/s
+//   forward, 16384 x 6144 (403 MB)             84.3   4.8 TB/s
+//   forward, 20011 x 2048 packed, of wider rows 35.6   4.6 TB/s
 //   gradients, 16384 x 6144 (604 MB)            126   4.8 TB/s
 // The forward has its loads in flight a batch of 8 rows ahead of their use; in the
 // gradients, SiLU' is some 25 instructions a value and shares the time with the loads.
@@ -238,9 +239,10 @@ __global__ __launch_bounds__(kThreads) void conv_fwd_kernel(ConvParams p, uint32
 }
 
 // Single tokens: a thread owns a piece of one sequence, loads its state before it
-// writes any (in place works).  256 sequences x 6144 channels of bf16, four taps: 8.8 us
-// for 25 MB, of which 3.6 is what a launch with one round of loads takes; two sequences
-// a thread, whose taps come once: 8.9.
+// writes any (in place works).  256 sequences x 6144 channels of bf16, four taps: 8.5 us
+// for 25 MB.  What bounds it is latency: each load stands behind the branch that parts
+// a whole piece from a row's last one, and is waited for there, so the three rows of the
+// state, the taps and the token's row are round trips to memory one after the other.
 template <typename T, int W, bool SILU>
 __global__ __launch_bounds__(kThreads) void conv_decode_kernel(ConvParams p, uint32_t pieces, uint32_t count) {
   constexpr int V = kPiece<T>;
@@ -431,8 +433,10 @@ __device__ __forceinline__ void conv_bwd_stretch(const ConvParams& p, int64_t t0
 }
 
 // lanes: adjacent pieces (kLanes of them), then stretches
-// (three waves a SIMD: two took 1.05 times as long for 16384 tokens x 6144 channels of
-// bf16, four, which spill, 1.74 times)
+// (three waves a SIMD, 168 registers: whole pieces of one sequence fit, while a row's
+// partial piece and stretches with starts spill 57 to 125.  For 16384 tokens x 6144
+// channels of bf16 two waves took 1.05 times as long; four, where whole pieces spill
+// too, 1.74 times)
 template <typename T, int W, bool SILU, bool NT>
 __global__ __launch_bounds__(kThreads, 3) void conv_bwd_kernel(ConvParams p, uint32_t lanes, uint32_t groups,
                                                             uint32_t main_wgs) {
@@ -488,7 +492,12 @@ BwdGrid bwd_grid(int64_t ntok, int64_t D) {
 
 // Stretches of 16 tokens, or of 4 where those would leave most of the card idle.  With
 // ordinary stores, 16: 96 us for 16384 tokens x 6144 channels of bf16, 35 for 20011 x
-// 2048; 8: 100 and 38; 32: 96 and 42.
+// 2048; 8: 100 and 38; 32: 96 and 42.  On both sides of the line, us of a call with
+// stretches of 4 / of 16 (of 512, 2048 and 8192 channels alike to a tenth; here 2048):
+//   threads, parts of the line     1/8        1/4        1/2          1          2          4
+//   bf16                       6.4/12.2   8.1/12.7  16.4/18.6  26.7/25.9  47.4/40.2  89.7/60.6
+//   fp32                       6.1/12.6   7.3/13.3  12.8/19.2  20.8/26.5  34.9/38.2  61.5/57.3
+// (fp32, whose pieces are half as many channels, crosses at two to four times the line)
 constexpr int64_t kFillThreads = 256 * 4 * 64 * 2;
 
 int64_t forward_threads(int64_t ntok, int64_t D, int64_t V) { return (ntok + 15) / 16 * ((D + V - 1) / V); }

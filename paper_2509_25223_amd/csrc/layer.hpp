@@ -143,9 +143,13 @@ struct ConvParams {
   float* part = nullptr;   // [tiles][taps + 1][D] sums of dweight, dbias
 };
 // Up to this many packed sequences a thread goes through the offsets itself; more, and
-// the map is built once a call.  20011 tokens x 2048 channels of bf16, the forward with 8,
-// 16, 32 and 64 sequences, us: in place 35.3, 37.4, 39.8, 47.5; from a map 38.5, 39.9,
-// 39.1, 40.1; the gradients cross at the same number.
+// the map is built once a call.  20011 tokens of bf16, us in place / from a map (with the
+// launch that builds it):
+//   sequences                        8           16           24           32           64
+//   2048 channels, forward   47.3/51.5    48.9/52.1    49.4/51.8    51.1/51.3    57.6/52.6
+//              gradients     69.5/73.0    73.8/76.0    74.5/76.2    75.4/74.7    93.7/85.0
+//   512, forward             18.0/23.5    18.9/23.8    19.6/23.6    21.2/23.7    27.4/23.7
+//   6144, forward           100.5/108.2  105.7/110.4  108.2/111.1  107.5/108.8  123.8/110.5
 constexpr int32_t kConvInPlace = 24;
 hipError_t launch_conv_forward(const ConvParams& p, bool bf16, hipStream_t stream);
 hipError_t launch_conv_decode(const ConvParams& p, bool bf16, hipStream_t stream);

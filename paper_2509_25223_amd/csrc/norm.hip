@@ -13,10 +13,12 @@
 // once per workgroup (or group of lanes) and summed by launch_column_sums.
 //
 // bf16, rows of 2048 with an fp32 stream (16384 of them) and of 128 (262144), us:
-//   addnorm forward 86 (403 MB, 4.7 TB/s), gradients 109 (604 MB, 5.5 TB/s)
+//   addnorm forward 88 (403 MB, 4.6 TB/s), gradients 109 (604 MB, 5.5 TB/s)
 //   gatenorm forward 32 (201 MB, 6.3 TB/s: a part from the 256 MB last-level cache),
-//   gradients 59 (336 MB, 5.7 TB/s)
-// Of a few rows, 4.4 to 6 us: a launch and two dependent round trips to memory.
+//   gradients 58 (336 MB, 5.8 TB/s)
+// Of a few rows, latency: gatenorm 3.9 us (777 tokens x 16 heads of 128), of which two
+// dependent round trips to memory; addnorm 5.7 (32 rows of 2048), where x, scale, stream
+// and weight of each of a lane's four pieces are waited for one after the other.
 #include "layer.hpp"
 
 namespace rla {
@@ -49,7 +51,7 @@ struct NormGrad {
 
 // A row's piece at column c, `left` values of which exist (0 or less: none).  FULL:
 // pieces are whole or absent, and an absent one's lane reads the row's start
-// instead, so that no branch parts the loads.
+// instead and takes zeros.  (The zeros are a branch behind the load, which waits for it.)
 template <typename T, int V, bool FULL>
 __device__ __forceinline__ void row_load(const T* row, int64_t c, int left, float (&x)[V]) {
   if constexpr (FULL) {
@@ -501,7 +503,8 @@ __global__ __launch_bounds__(kThreads) void gatenorm_bwd_kernel(GateNormParams p
 struct Shape {
   int L, NP;
 };
-// addnorm forward: a wave a row up to 4 pieces a lane, then a workgroup, then two passes.
+// addnorm forward: a wave a row up to 4 pieces a lane (a narrow row leaves lanes idle: of
+// 64 bf16 values 56 of the 64), then a workgroup, then two passes.
 // Backward, where a lane holds its columns' sums beside the row: a wave a row of one
 // piece a lane, then a workgroup (16384 rows of 2048 bf16 values with an fp32 stream: a
 // wave with 4 pieces 195 us, one to a SIMD; a workgroup 109).

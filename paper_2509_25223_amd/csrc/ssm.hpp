@@ -15,8 +15,10 @@
 // Four lanes of four states with as many chunks as fill the card, against eight lanes of
 // two states, which fill it without chunks: 16384 tokens in 4 sequences x 4096 channels
 // x 16 states, bf16, forward 161 + 347 against 490 us, gradients 200 + 1161 against 1547
-// (the sums over a channel's lanes and what is once per channel double with the lanes).
-// Eight waves a workgroup instead of four: forward 527, gradients 1660.
+// (the sums over a channel's lanes and what is once per channel double with the lanes):
+// the forward alone would be 18 us shorter with eight, the step is 168 us shorter with
+// four, and both directions share the layout.  Eight waves a workgroup instead of four:
+// forward 527, gradients 1660.
 #pragma once
 
 #include "layer.hpp"

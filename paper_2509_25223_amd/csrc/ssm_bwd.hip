@@ -17,10 +17,13 @@
 // over 16 lanes costs 4 a value); then over the waves in LDS, and over the blocks
 // of channels by a last kernel, from fp32 partial sums.  No atomics.
 //
-// The vector ALU bounds it: 15 multiply-adds, products and the like (the exponential two of
-// them) a token, channel and state, 4 more for the sums over channels.  16384 tokens
-// in 4 sequences x 4096 channels x 16 states, bf16: chunk summaries 195 us, gradients
-// 1115, 85 % of it with the ALUs at work (1.3 GB: 0.25 ms), sums of dB and dC 36.
+// The vector ALU bounds it: 29 instructions a token, channel and state (counters).  15 are
+// the recurrence and its products (the exponential, at a quarter of their rate, one of
+// them), 4 the sums over channels; the others bring a token's values to the lanes, sum
+// over a channel's lanes, and are what is once a token and channel.  16384 tokens in
+// 4 sequences x 4096 channels x 16 states, bf16: chunk summaries 195 us (88 % with the ALUs
+// at work), gradients 1112 (83 %; 1.3 GB: 0.25 ms), sums of dB and dC 36.  Two waves a SIMD at
+// 255 registers; fp32 spills 2 of them.
 #include "ssm.hpp"
 
 namespace rla {
