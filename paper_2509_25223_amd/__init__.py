@@ -531,3 +531,9 @@ from .layer import (  # noqa: E402,F401
     rla_conv_backward, rla_conv_decode, rla_conv_forward, rla_conv_problem, rla_conv_workspace_size,
     rla_gatenorm_backward, rla_gatenorm_forward, rla_gatenorm_problem, rla_gatenorm_workspace_size, rla_ssm_backward,
     rla_ssm_decode, rla_ssm_forward, rla_ssm_problem, rla_ssm_workspace_size)
+# the ends of a language model on these layers, and a second recurrent mixer (include/rla_model.h)
+from .model import (  # noqa: E402,F401
+    MODEL_SYMBOLS, RLA_GLR_BACKWARD, RLA_GLR_FORWARD, RLA_INDEX_I32, RLA_INDEX_I64, make_embed_problem, make_glr_problem,
+    make_logprob_problem, rla_embed_backward, rla_embed_forward, rla_embed_problem, rla_embed_workspace_size,
+    rla_glr_backward, rla_glr_decode, rla_glr_forward, rla_glr_problem, rla_glr_workspace_size, rla_logprob_backward,
+    rla_logprob_forward, rla_logprob_problem, rla_logprob_workspace_size)

@@ -1,0 +1,456 @@
+// Embedding lookup, out_t = scale table[id_t], and the table's gradient: row v gets
+// scale times the sum, in the order of t, of dout_t where id_t = v.
+//
+// The gradient sorts (id, t) by id, stably, in two passes of a counting sort over
+// the id's low and high bits, and sums stretches of equal ids: every row of the table is
+// written once, in one order of summation, and nothing is added by atomics (they count
+// tokens only).  Ids without a row sort behind the others and are dropped.
+//   embed_count   a tile of tokens counts its low digits; clears what is counted later
+//   embed_sort    a tile moves its tokens to their places among all: the counts of smaller
+//                 digits, of the same digit in earlier tiles, and in the tile itself
+//                 (first pass: also counts the high digits by the tile that a token lands in,
+//                 and marks the rows that have a token)
+//   embed_sort    second pass; other workgroups write the rows without a token
+//   embed_sums    a group of lanes takes `chunk` sorted tokens and writes the sums of the ids
+//                 that start there and end there or in the next chunk; of longer runs
+//                 each chunk leaves its part
+//   embed_join    adds these parts
+#include "model.hpp"
+
+namespace rla {
+
+namespace {
+
+// The id as a sorting key: V for one without a row.
+__device__ __forceinline__ uint32_t key_of(const EmbedParams& p, int64_t t) {
+  const int64_t id = p.ids[t];
+  return id >= 0 && id < p.V ? (uint32_t)id : (uint32_t)p.V;
+}
+
+// ---------------------------------------------------------------------------
+// lookup: a thread a piece of a row
+// ---------------------------------------------------------------------------
+template <typename X, typename T, bool FULL, bool NT>
+__global__ __launch_bounds__(kThreads) void embed_fwd_kernel(EmbedParams p, uint32_t pieces, uint32_t count) {
+  constexpr int V = kPiece<T>;
+  const uint32_t id = blockIdx.x * kThreads + threadIdx.x;
+  if (id >= count) return;
+  const uint32_t t = id / pieces;
+  const int64_t c = (int64_t)(id % pieces) * V;
+  const int left = (int)min(p.D - c, (int64_t)V);
+  const uint32_t row = key_of(p, t);
+  float x[V];
+  if (row < (uint32_t)p.V) {
+    load_piece<X, V, FULL>(reinterpret_cast<const X*>(p.table) + (int64_t)row * p.D + c, left, x);
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[e] *= p.scale;
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[e] = 0.f;
+  }
+  store_piece<T, V, FULL, NT>(reinterpret_cast<T*>(p.out) + (int64_t)t * p.D + c, left, x);
+}
+
+// ---------------------------------------------------------------------------
+// sorting
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(kThreads) void embed_count_kernel(EmbedParams p) {
+  extern __shared__ int32_t lds[];
+  const int tid = threadIdx.x, bins = 1 << p.bits1;
+  const int64_t t0 = (int64_t)blockIdx.x * p.tile;
+  for (int b = tid; b < bins; b += kThreads) lds[b] = 0;
+  // what later kernels count in
+  const int64_t all = (int64_t)gridDim.x * kThreads, own = (int64_t)blockIdx.x * kThreads + tid;
+  for (int64_t i = own; i < (int64_t)p.tiles << p.bits2; i += all) p.count2[i] = 0;
+  for (int64_t i = own; i < p.V / 32 + 1; i += all) p.present[i] = 0;
+  __syncthreads();
+  for (int i = tid; i < p.tile && t0 + i < p.n; i += kThreads) atomicAdd(&lds[key_of(p, t0 + i) & (bins - 1)], 1);
+  __syncthreads();
+  for (int b = tid; b < bins; b += kThreads) p.count1[(int64_t)blockIdx.x * bins + b] = lds[b];
+}
+
+// A tile's tokens to their places.  Each wave has a quarter of the tile, in order; lds:
+// [kWaves][bins] next places by wave and digit, then kThreads sums.
+template <bool SECOND> __device__ __forceinline__ void sort_tile(const EmbedParams& p, int tile, int32_t* lds) {
+  const int bits = SECOND ? p.bits2 : p.bits1, bins = 1 << bits;
+  const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63;
+  const int32_t* counts = SECOND ? p.count2 : p.count1;
+  int32_t* place = lds;
+  int32_t* sums = lds + kWaves * bins;
+  const int64_t first = (int64_t)tile * p.tile + (int64_t)w * (p.tile / kWaves);
+  auto key_at = [&](int64_t i) { return SECOND ? (uint32_t)p.key1[i] : key_of(p, i); };
+  auto digit = [&](uint32_t k) { return (int)((SECOND ? k >> p.bits1 : k) & (uint32_t)(bins - 1)); };
+
+  for (int b = tid; b < kWaves * bins; b += kThreads) place[b] = 0;
+  __syncthreads();
+  for (int j = lane; j < p.tile / kWaves; j += 64)
+    if (first + j < p.n) atomicAdd(&place[w * bins + digit(key_at(first + j))], 1);
+  // a thread's digits: how many tokens have them, and how many of those lie in earlier tiles
+  const int per = (bins + kThreads - 1) / kThreads;
+  int32_t total = 0;
+  for (int j = 0; j < per; ++j) {
+    const int b = tid * per + j;
+    if (b >= bins) break;
+    for (int i = 0; i < p.tiles; ++i) total += counts[(int64_t)i * bins + b];
+  }
+  sums[tid] = total;
+  __syncthreads();
+  for (int d = 1; d < kThreads; d <<= 1) {
+    const int32_t o = tid >= d ? sums[tid - d] : 0;
+    __syncthreads();
+    sums[tid] += o;
+    __syncthreads();
+  }
+  int32_t at = sums[tid] - total;   // places before the thread's digits
+  for (int j = 0; j < per; ++j) {
+    const int b = tid * per + j;
+    if (b >= bins) break;
+    int32_t before = 0, behind = 0;
+    for (int i = 0; i < p.tiles; ++i) {
+      const int32_t c = counts[(int64_t)i * bins + b];
+      before += i < tile ? c : 0;
+      behind += i < tile ? 0 : c;
+    }
+    int32_t next = at + before;
+    for (int v = 0; v < kWaves; ++v) {
+      const int32_t c = place[v * bins + b];
+      place[v * bins + b] = next;
+      next += c;
+    }
+    at += before + behind;
+  }
+  __syncthreads();
+  for (int j0 = 0; j0 < p.tile / kWaves; j0 += 64) {
+    const int64_t i = first + j0 + lane;
+    const bool there = i < p.n;
+    const uint32_t k = there ? key_at(i) : 0;
+    const int d = digit(k);
+    // lanes of the same digit
+    uint64_t same = __ballot(there);
+    for (int b = 0; b < bits; ++b) {
+      const uint64_t set = __ballot((d >> b) & 1);
+      same &= (d >> b) & 1 ? set : ~set;
+    }
+    if (!there) continue;
+    const int rank = __popcll(same & ((1ull << lane) - 1));
+    const int32_t to = place[w * bins + d] + rank;
+    // (a wave's accesses to LDS keep their order; the compiler is told so)
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");
+    if (rank == 0) place[w * bins + d] = to + __popcll(same);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    if (SECOND) {
+      p.key[to] = (int32_t)k;
+      p.pos[to] = p.pos1[i];
+    } else {
+      p.key1[to] = (int32_t)k;
+      p.pos1[to] = (int32_t)i;
+      atomicAdd(&p.count2[(((int64_t)(to / p.tile)) << p.bits2) + (k >> p.bits1)], 1);
+      if (k < (uint32_t)p.V) atomicOr(&p.present[k >> 5], 1u << (k & 31));
+    }
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void embed_sort1_kernel(EmbedParams p) {
+  extern __shared__ int32_t lds[];
+  sort_tile<false>(p, blockIdx.x, lds);
+}
+
+constexpr int kFillPieces = 8;   // 16-byte pieces a thread of the workgroups that write rows without a token
+
+template <bool FULL, bool NT>
+__global__ __launch_bounds__(kThreads) void embed_sort2_kernel(EmbedParams p, uint32_t pieces) {
+  extern __shared__ int32_t lds[];
+  if ((int)blockIdx.x < p.tiles) {
+    sort_tile<true>(p, blockIdx.x, lds);
+    return;
+  }
+  const int64_t first = ((int64_t)blockIdx.x - p.tiles) * (kThreads * kFillPieces) + threadIdx.x;
+#pragma unroll
+  for (int j = 0; j < kFillPieces; ++j) {
+    const int64_t id = first + j * kThreads;
+    const int64_t v = id / pieces, c = (id - v * pieces) * 4;
+    if (v >= p.V || (p.present[v >> 5] >> (v & 31)) & 1u) continue;
+    const int left = (int)min(p.D - c, (int64_t)4);
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+    if (p.base) load_piece<float, 4, FULL>(p.base + v * p.D + c, left, x);
+    store_piece<float, 4, FULL, NT>(p.dtable + v * p.D + c, left, x);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// sums
+// ---------------------------------------------------------------------------
+// Whether the run of key k that fills the end of chunk c (tokens up to i1) ends in the
+// next chunk.
+__device__ __forceinline__ bool ends_next(const EmbedParams& p, int64_t i1, int32_t k) {
+  const int64_t i2 = min(i1 + p.chunk, p.n);
+  return p.key[i2 - 1] != k || i2 == p.n || p.key[i2] != k;
+}
+
+// L lanes a chunk of sorted tokens, a piece of the columns a lane (blockIdx.y: which L pieces)
+template <typename T, int L, bool FULL>
+__global__ __launch_bounds__(kThreads) void embed_sums_kernel(EmbedParams p) {
+  constexpr int V = kPiece<T>, kAhead = 4;
+  const int64_t c = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
+  if (c >= p.chunks) return;
+  const int64_t col = ((int64_t)blockIdx.y * L + threadIdx.x % L) * V;
+  if (col >= p.D) return;
+  const int left = (int)min(p.D - col, (int64_t)V);
+  int64_t i = c * p.chunk, end = min(i + p.chunk, p.n);
+  const int32_t kFirst = p.key[i], kLast = p.key[end - 1];
+  bool head = false;   // the first run began in an earlier chunk, which leaves it in parts
+  if (c > 0 && p.key[i - 1] == kFirst) {
+    const bool began_before = c == 1 || p.key[i - p.chunk - 1] != kFirst;
+    const bool ends_here = kLast != kFirst || end == p.n || p.key[end] != kFirst;
+    if (began_before && ends_here) {   // the previous chunk's
+      while (i < end && p.key[i] == kFirst) ++i;
+    } else {
+      head = true;
+    }
+  }
+  bool tail = false;   // the last run goes on beyond the next chunk
+  if (end < p.n && p.key[end] == kLast && !(head && kFirst == kLast)) {
+    if (ends_next(p, end, kLast)) {
+      while (end < p.n && p.key[end] == kLast) ++end;
+    } else {
+      tail = true;
+    }
+  }
+  if (i >= end) return;
+  float sum[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) sum[e] = 0.f;
+  int32_t k = p.key[i];
+  auto flush = [&](bool last) {
+    if (k >= (int32_t)p.V) return;
+    if (head || (last && tail)) {
+      store_piece<float, V, FULL>(p.part + (c * 2 + (head ? 0 : 1)) * p.D + col, left, sum);
+    } else {
+      float b[V];
+      if (p.base) {
+        load_piece<float, V, FULL>(p.base + (int64_t)k * p.D + col, left, b);
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum[e] = __builtin_fmaf(p.scale, sum[e], b[e]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum[e] *= p.scale;
+      }
+      store_piece<float, V, FULL>(p.dtable + (int64_t)k * p.D + col, left, sum);
+    }
+  };
+  const T* dout = reinterpret_cast<const T*>(p.dout) + col;
+  for (; i < end; i += kAhead) {
+    int32_t kk[kAhead];
+    typename RowVec<T, V>::type raw[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {   // (past the end: the last again, not used)
+      const int64_t at = min(i + u, end - 1);
+      kk[u] = p.key[at];
+      load_raw<T, V, FULL>(dout + (int64_t)p.pos[at] * p.dos, left, raw[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (i + u >= end) break;
+      if (kk[u] != k) {
+        flush(false);
+        head = false;
+        k = kk[u];
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum[e] = 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) sum[e] += to_f<T>(raw[u][e]);
+    }
+  }
+  flush(true);
+}
+
+// Runs that a chunk left in parts: its tail and the following chunks' heads.  A workgroup looks at
+// `per` chunks (at most 64) for such runs; 256 columns, a lane 4 of them, the parts over the waves.
+template <bool FULL> __global__ __launch_bounds__(kThreads) void embed_join_kernel(EmbedParams p, int32_t per) {
+  __shared__ float sums[kWaves][64][4];
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t c0 = (int64_t)blockIdx.y * per, col = ((int64_t)blockIdx.x * 64 + lane) * 4;
+  const int left = (int)min(p.D - col, (int64_t)4);
+  bool split = false;
+  if (lane < per && c0 + lane + 1 < p.chunks) {
+    const int64_t i = (c0 + lane) * p.chunk, end = i + p.chunk;
+    const int32_t k = p.key[end - 1];
+    const bool whole = i > 0 && p.key[i] == k && p.key[i - 1] == k;   // inside a run that began earlier
+    split = k < (int32_t)p.V && p.key[end] == k && !whole && !ends_next(p, end, k);
+  }
+  for (uint64_t left_runs = __ballot(split); left_runs; left_runs &= left_runs - 1) {
+    const int64_t c = c0 + __builtin_ctzll(left_runs);
+    const int32_t k = p.key[(c + 1) * p.chunk];
+    // parts: the tail of c, the heads of c + 1 .. c + count
+    int64_t count = 0;
+    while (true) {
+      const int64_t d = c + 1 + count + lane;
+      const uint64_t in = __ballot(d < p.chunks && p.key[min(d, (int64_t)p.chunks - 1) * p.chunk] == k);
+      const int run = in == ~0ull ? 64 : __builtin_ctzll(~in);
+      count += run;
+      if (run < 64) break;
+    }
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    if (left > 0) {
+      for (int64_t j = w; j <= count; j += kWaves) {
+        float x[4];
+        load_piece<float, 4, FULL>(p.part + ((c + j) * 2 + (j == 0 ? 1 : 0)) * p.D + col, left, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] += x[e];
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sums[w][lane][e] = s[e];
+    __syncthreads();
+    if (w == 0 && left > 0) {
+      float b[4] = {0.f, 0.f, 0.f, 0.f};
+      if (p.base) load_piece<float, 4, FULL>(p.base + (int64_t)k * p.D + col, left, b);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        for (int v = 1; v < kWaves; ++v) s[e] += sums[v][lane][e];
+        s[e] = __builtin_fmaf(p.scale, s[e], b[e]);
+      }
+      store_piece<float, 4, FULL>(p.dtable + (int64_t)k * p.D + col, left, s);
+    }
+    __syncthreads();
+  }
+}
+
+// without tokens: dtable = base
+__global__ __launch_bounds__(kThreads) void embed_copy_kernel(const float* base, float* dtable, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads)
+    dtable[i] = base ? base[i] : 0.f;
+}
+
+// ---------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------
+template <typename X, typename T, bool FULL> hipError_t forward(const EmbedParams& p, hipStream_t stream) {
+  const int64_t pieces = (p.D + kPiece<T> - 1) / kPiece<T>;
+  const bool nt = p.n * p.D * (int64_t)sizeof(T) > kNtBytes;
+  // (more pieces than a launch holds: several, of whole rows each)
+  const int64_t most = max((int64_t)1, ((int64_t)1 << 31) / pieces);
+  EmbedParams part = p;
+  for (int64_t t = 0; t < p.n; t += most) {
+    part.n = min(p.n - t, most);
+    part.ids.p = reinterpret_cast<const char*>(p.ids.p) + t * (p.ids.wide ? 8 : 4);
+    part.out = reinterpret_cast<T*>(p.out) + t * p.D;
+    const uint32_t count = (uint32_t)(part.n * pieces);
+    const dim3 grid((count + kThreads - 1) / kThreads);
+    if (nt) hipLaunchKernelGGL((embed_fwd_kernel<X, T, FULL, true>), grid, dim3(kThreads), 0, stream, part, (uint32_t)pieces, count);
+    else hipLaunchKernelGGL((embed_fwd_kernel<X, T, FULL, false>), grid, dim3(kThreads), 0, stream, part, (uint32_t)pieces, count);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+template <typename X, typename T> hipError_t forward(const EmbedParams& p, hipStream_t stream) {
+  return p.D % kPiece<T> == 0 ? forward<X, T, true>(p, stream) : forward<X, T, false>(p, stream);
+}
+
+template <typename T, int L, bool FULL> hipError_t sums(const EmbedParams& p, hipStream_t stream) {
+  constexpr int V = kPiece<T>, sub = kThreads / L;
+  const dim3 grid((uint32_t)((p.chunks + sub - 1) / sub), (uint32_t)((p.D + L * V - 1) / (L * V)));
+  hipLaunchKernelGGL((embed_sums_kernel<T, L, FULL>), grid, dim3(kThreads), 0, stream, p);
+  return hipGetLastError();
+}
+template <typename T, bool FULL> hipError_t sums(const EmbedParams& p, hipStream_t stream) {
+  const int64_t pieces = (p.D + kPiece<T> - 1) / kPiece<T>;
+  if (pieces <= 8) return sums<T, 8, FULL>(p, stream);
+  if (pieces <= 16) return sums<T, 16, FULL>(p, stream);
+  if (pieces <= 32) return sums<T, 32, FULL>(p, stream);
+  if (pieces <= 64) return sums<T, 64, FULL>(p, stream);
+  if (pieces <= 128) return sums<T, 128, FULL>(p, stream);
+  return sums<T, 256, FULL>(p, stream);
+}
+
+template <bool FULL> hipError_t sort_and_fill(const EmbedParams& p, hipStream_t stream) {
+  const size_t lds1 = 4 * ((size_t)kWaves * (1 << p.bits1) + kThreads), lds2 = 4 * ((size_t)kWaves * (1 << p.bits2) + kThreads);
+  hipLaunchKernelGGL(embed_count_kernel, dim3(p.tiles), dim3(kThreads), 4u << p.bits1, stream, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(embed_sort1_kernel, dim3(p.tiles), dim3(kThreads), lds1, stream, p);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t pieces = (p.D + 3) / 4, count = p.base == p.dtable ? 0 : p.V * pieces;
+  const int64_t wgs = (count + kThreads * kFillPieces - 1) / (kThreads * kFillPieces);
+  if (p.V * p.D * 4 > kNtBytes)
+    hipLaunchKernelGGL((embed_sort2_kernel<FULL, true>), dim3((uint32_t)(p.tiles + wgs)), dim3(kThreads), lds2, stream, p,
+                       (uint32_t)pieces);
+  else
+    hipLaunchKernelGGL((embed_sort2_kernel<FULL, false>), dim3((uint32_t)(p.tiles + wgs)), dim3(kThreads), lds2, stream, p,
+                       (uint32_t)pieces);
+  return hipGetLastError();
+}
+
+// One slice's gradient.
+template <typename T> hipError_t backward(const EmbedParams& p, hipStream_t stream) {
+  constexpr int V = kPiece<T>;
+  hipError_t e = p.D % 4 == 0 ? sort_and_fill<true>(p, stream) : sort_and_fill<false>(p, stream);
+  if (e != hipSuccess) return e;
+  e = p.D % V == 0 ? sums<T, true>(p, stream) : sums<T, false>(p, stream);
+  if (e != hipSuccess || p.chunks < 3) return e;   // (a run in parts spans a whole chunk and its neighbours)
+  const int32_t per = (p.chunks + 127) / 128;
+  const dim3 grid((uint32_t)((p.D + 255) / 256), (uint32_t)((p.chunks + per - 1) / per));
+  if (p.D % 4 == 0) hipLaunchKernelGGL(embed_join_kernel<true>, grid, dim3(kThreads), 0, stream, p, per);
+  else hipLaunchKernelGGL(embed_join_kernel<false>, grid, dim3(kThreads), 0, stream, p, per);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t embed_plan(EmbedParams& p, int64_t tokens, unsigned char* ws) {
+  int bits = 1;
+  while (((int64_t)1 << bits) < p.V + 1) ++bits;
+  p.bits1 = (bits + 1) / 2;
+  p.bits2 = bits - p.bits1;
+  p.n = tokens;
+  p.tile = tokens <= 65536 ? 1024 : 4096;
+  p.tiles = (int32_t)((tokens + p.tile - 1) / p.tile);
+  p.chunk = 16;
+  while (p.chunk * 4096 < tokens) p.chunk *= 2;
+  p.chunks = (int32_t)((tokens + p.chunk - 1) / p.chunk);
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    unsigned char* at = ws + off;
+    off += (bytes + 255) / 256 * 256;
+    return at;
+  };
+  p.count1 = reinterpret_cast<int32_t*>(take(4 * ((size_t)p.tiles << p.bits1)));
+  p.count2 = reinterpret_cast<int32_t*>(take(4 * ((size_t)p.tiles << p.bits2)));
+  p.present = reinterpret_cast<uint32_t*>(take(4 * (size_t)(p.V / 32 + 1)));
+  for (int32_t** a : {&p.key1, &p.pos1, &p.key, &p.pos}) *a = reinterpret_cast<int32_t*>(take(4 * (size_t)tokens));
+  p.part = reinterpret_cast<float*>(take(p.chunks < 3 ? 0 : 8 * (size_t)p.chunks * (size_t)p.D));
+  return off;
+}
+
+hipError_t launch_embed_forward(const EmbedParams& p, bool table_bf16, bool bf16, hipStream_t stream) {
+  if (table_bf16) return bf16 ? forward<u16, u16>(p, stream) : forward<u16, float>(p, stream);
+  return bf16 ? forward<float, u16>(p, stream) : forward<float, float>(p, stream);
+}
+
+hipError_t launch_embed_backward(const EmbedParams& p, bool bf16, unsigned char* ws, hipStream_t stream) {
+  EmbedParams q = p;
+  if (p.n == 0) {
+    const int64_t n = p.base == p.dtable ? 0 : p.V * p.D;
+    if (n == 0) return hipSuccess;
+    hipLaunchKernelGGL(embed_copy_kernel, dim3((uint32_t)min((n + kThreads - 1) / kThreads, (int64_t)2048)), dim3(kThreads), 0,
+                       stream, p.base, p.dtable, n);
+    return hipGetLastError();
+  }
+  for (int64_t t = 0; t < p.n; t += kEmbedSlice) {
+    const int64_t n = min(p.n - t, kEmbedSlice);
+    embed_plan(q, n, ws);
+    q.ids.p = reinterpret_cast<const char*>(p.ids.p) + t * (p.ids.wide ? 8 : 4);
+    q.dout = reinterpret_cast<const char*>(p.dout) + t * p.dos * (bf16 ? 2 : 4);
+    if (t > 0) q.base = p.dtable;
+    const hipError_t e = bf16 ? backward<u16>(q, stream) : backward<float>(q, stream);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace rla

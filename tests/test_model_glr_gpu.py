@@ -1,0 +1,278 @@
+"""Gated linear recurrence: outputs, states and gradients against 64 bits."""
+import pytest
+import torch
+
+import paper_2509_25223_amd as rla
+from tests import layer_reference as lref
+from tests import model_reference as ref
+
+pytestmark = pytest.mark.gpu
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+ROWS = ("x", "r", "i", "z", "dO")
+INPUTS = ("x", "r", "A", "i", "z", "h0")
+
+
+def make(device, where, D, dtype, opts="izhn", wide=False, seed=0):
+    """opts: i input gate, z output gate, h initial states, n normalised"""
+    g = torch.Generator().manual_seed(seed)
+    lead, spans, cu = lref.layout(where) if isinstance(where, str) else where
+    rnd = lambda *s: torch.randn(*s, generator=g)   # noqa: E731
+    t, n = TYPES[dtype], len(spans)
+    x = {m: rnd(*lead, D).to(t) for m in ROWS}
+    x.update(A=-3 * torch.rand(D, generator=g), h0=rnd(n, D) if "h" in opts else None, dh_final=rnd(n, D))
+    for m in "iz":
+        if m not in opts:
+            x[m] = None
+    if cu is not None:
+        inside = torch.zeros(lead[0], dtype=torch.bool)
+        for a, b in spans:
+            inside[a:b] = True
+        for m in ROWS:
+            if x[m] is not None:
+                x[m][~inside] = float("nan")
+    x = {m: None if v is None else v.to(device) for m, v in x.items()}
+    if wide:
+        x.update({m: lref.strided(x[m], len(lead)) for m in ROWS if x[m] is not None})
+    x["cu"] = None if cu is None else torch.tensor(cu, dtype=torch.int32, device=device)
+    x["norm"] = "n" in opts
+    return x, spans
+
+
+def reference(x, spans):
+    v = {m: lref.wide(None if x[m] is None else x[m].nan_to_num()) for m in INPUTS}
+    D = x["A"].shape[0]
+    rows = {m: None if v[m] is None else v[m].reshape(-1, D) for m in ("x", "r", "i", "z")}
+    o, fin = ref.glr(rows["x"], rows["r"], v["A"], rows["i"], rows["z"], x["norm"], v["h0"], spans)
+    o = o.reshape(v["x"].shape)
+    if not spans:
+        o = o + 0 * v["x"]
+    up = [x["dO"].nan_to_num().cpu().double(), x["dh_final"].cpu().double()]
+    return o, fin, lref.gradients([o, fin], up, v)
+
+
+def run(x, saved, dh=True, stream=None):
+    how = dict(i=x["i"], z=x["z"], normalize=x["norm"], h0=x["h0"], cu_seqlens=x["cu"], stream=stream)
+    ws = None
+    if saved:
+        problem = rla.make_glr_problem(x["x"], x["cu"])
+        ws = torch.full((max(1, rla.rla_glr_workspace_size(problem, rla.RLA_GLR_BACKWARD)),), 255, dtype=torch.uint8,
+                        device=x["x"].device)
+    o, h = rla.rla_glr_forward(x["x"], x["r"], x["A"], **how, save_for_backward=saved, workspace=ws)
+    g = rla.rla_glr_backward(x["x"], x["r"], x["A"], x["dO"], **how, dh_final=x["dh_final"] if dh else None,
+                             use_saved=saved, workspace=ws)
+    torch.cuda.synchronize()
+    return o, h, g
+
+
+def compare(x, spans, saved):
+    o, fin, grads = reference(x, spans)
+    got, got_fin, g = run(x, saved)
+    T = max([b - a for a, b in spans] + [1])
+    tokens = max(1, o.numel() // x["A"].shape[0])
+    lref.check("o", got, o, 8 + T)
+    lref.check("h_final", got_fin, fin, 8 + T)
+    assert set(g) == {"d" + n for n in grads}
+    for n, want in grads.items():
+        lref.check("d" + n, g["d" + n], want, 8 * tokens if n == "A" else 16 + T)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("where", lref.LAYOUTS)
+@pytest.mark.parametrize("D,opts,wide", [(64, "izhn", False), (30, "ihn", True), (1, "", False), (130, "zh", True),
+                                         (67, "n", False), (72, "izn", True)])
+def test_forward_backward(device, where, dtype, D, opts, wide):
+    x, spans = make(device, where, D, dtype, opts, wide)
+    compare(x, spans, saved=D % 4 == 0)
+
+
+def long(cu, T, B=2):
+    if cu:
+        return (T,), lref.sequences(cu, T), cu
+    return (B, T), [(b * T, (b + 1) * T) for b in range(B)], None
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("cu,T", [(None, 417), ([0, 300, 301, 301, 812], 900), ([5, 700], 700), ([0, 128, 256, 640], 640),
+                                  (list(range(0, 650, 9)), 650), ([0, 2, 1290], 1300)])
+@pytest.mark.parametrize("D", [18, 200])
+def test_chunks(device, cu, T, D, dtype):
+    """Tokens split into chunks, which sequences start and end in, at the edges of, and span."""
+    x, spans = make(device, long(cu, T), D, dtype, seed=T)
+    compare(x, spans, saved=D == 18)
+
+
+@pytest.mark.parametrize("B,T,D", [(600, 3, 40), (40, 33, 1000), (9, 200, 4100), (70, 1, 64)])
+def test_many_sequences(device, B, T, D):
+    """Chunks of whole sequences: some columns of every output."""
+    x, spans = make(device, long(None, T, B), D, "f32", seed=B)
+    got, fin, g = run(x, True)
+    cols = sorted({0, 1, D // 2, D - 1})
+    cut = {m: None if v is None else v[..., cols].contiguous() if torch.is_tensor(v) and v.shape[-1] == D else v
+           for m, v in x.items()}
+    o, want_fin, grads = reference(cut, spans)
+    lref.check("o", got[..., cols], o, 8 + T)
+    lref.check("h", fin[..., cols], want_fin, 8 + T)
+    for n, want in grads.items():
+        lref.check("d" + n, g["d" + n][..., cols], want, 8 * B * T if n == "A" else 16 + T)
+
+
+def test_saved_and_recomputed(device):
+    """A backward that recomputes its forward gives the saving one's bits, without an upstream
+    state gradient those of zeros; and on another stream."""
+    x, spans = make(device, long([0, 300, 812], 900), 70, "bf16")
+    _, _, a = run(x, True)
+    _, _, b = run(x, False)
+    assert all(torch.equal(a[n], b[n]) for n in a)
+    _, _, c = run(x, False, dh=False)
+    x["dh_final"].zero_()
+    _, _, d = run(x, False)
+    assert all(torch.equal(c[n], d[n]) for n in c)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    _, _, e = run(x, False, stream=side)
+    assert all(torch.equal(c[n], e[n]) for n in c)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("D,opts", [(64, "izhn"), (30, "h"), (515, "ihn"), (2, "zhn")])
+def test_decode(device, dtype, D, opts):
+    """Single tokens from 64 bits, several a call as one at a time, in place."""
+    B, T = 3, 6
+    x, spans = make(device, long(None, T, B), D, dtype, opts, wide=True)
+    o, fin, _ = reference(x, spans)
+
+    def step(a, b, **kw):
+        cut = {m: None if x[m] is None else x[m][:, a:b] for m in ("x", "r", "i", "z")}
+        if b - a == 1:
+            cut = {m: None if t is None else t.contiguous() for m, t in cut.items()}
+        return rla.rla_glr_decode(cut["x"], cut["r"], x["A"], i=cut["i"], z=cut["z"], normalize=x["norm"], **kw)
+
+    got, h = step(0, T, h_in=x["h0"])
+    lref.check("o", got, o, 8 + T)
+    lref.check("h", h, fin, 8 + T)
+    state = x["h0"].clone()
+    for t in range(T):
+        one, same = step(t, t + 1, h_in=state, h_out=state)
+        assert same is state and torch.equal(one, got[:, t:t + 1])
+    assert torch.equal(state, h)
+    none, same = step(0, 0, h_in=state)
+    assert none.shape == (B, 0, D) and torch.equal(same, state)
+    first, _ = step(0, 1)
+    x["h0"] = torch.zeros_like(state)
+    zero, _ = step(0, 1, h_in=x["h0"])
+    assert torch.equal(first, zero)
+
+
+def test_sequences_apart(device):
+    """NaN or infinities in one sequence reach no other, forward or backward."""
+    x, spans = make(device, long([0, 300, 500, 812], 812), 70, "f32")
+    o, h, g = run(x, False)
+    a, b = spans[1]
+    x["x"][a + 3, 5], x["r"][a + 40, 6], x["i"][b - 1, 2] = float("nan"), float("nan"), float("inf")
+    x["dO"][a + 100, 8], x["x"][a, 9], x["dh_final"][1, 11], x["h0"][1, 12] = float("nan"), float("inf"), float("nan"), float("nan")
+    o2, h2, g2 = run(x, False)
+    keep = torch.tensor([t for t in range(812) if not a <= t < b], device=device)
+    assert torch.equal(o[keep], o2[keep]) and torch.equal(h[[0, 2]], h2[[0, 2]])
+    assert o2[b - 1, 5].isnan() and o2[b - 1, 12].isnan()
+    for n in ("dx", "dr", "di", "dz"):
+        assert torch.equal(g[n][keep], g2[n][keep]), n
+    assert torch.equal(g["dh0"][[0, 2]], g2["dh0"][[0, 2]])
+
+
+def test_gates_at_the_ends(device):
+    """Closed and open gates, decays of 0 and 1: no NaN, and small differences keep their digits."""
+    x, spans = make(device, "odd", 64, "f32", opts="ihn")
+    x["r"][:, ::3] = -40.0
+    x["r"][:, 1::3] = 30.0
+    x["i"][:, ::4] = -90.0
+    x["A"][:8], x["A"][8:16] = 0.0, -200.0
+    o, fin, g = run(x, False)
+    want, want_fin, grads = reference(x, spans)
+    assert all(torch.isfinite(t).all() for t in [o, fin, *g.values()])
+    lref.check("o", o, want, 64)
+    lref.check("h", fin, want_fin, 64)
+    some = x["A"] < 0   # (no decay: the gradient of sqrt(1 - a^2) counts as 0)
+    for n in ("dx", "dh0"):
+        lref.check(n, g[n][..., some], grads[n[1:]].detach()[..., some.cpu()], 64)
+    # m = sqrt(1 - a^2) at every size of 1 - a
+    A = -torch.logspace(-12, 1, 64, device=device)
+    one = torch.ones(1, 1, 64, device=device)
+    o, _ = rla.rla_glr_forward(one, 100 * one, A)
+    want = torch.sqrt(-torch.expm1(2 * A.double()))
+    assert ((o[0, 0].double() - want).abs() / want).max().item() < 2.0 ** -21
+
+
+def test_differences(device):
+    """The gradients along a direction against differences of the 64-bit forward."""
+    x, spans = make(device, long([0, 200, 201, 410], 420), 6, "f32", seed=11)
+    _, _, g = run(x, False)
+    gen = torch.Generator().manual_seed(12)
+    base = {n: x[n].nan_to_num().cpu().double() for n in INPUTS}
+    base["A"] = base["A"] - 0.1
+    x["A"] = base["A"].float().to(device)
+    base["A"] = x["A"].cpu().double()
+    _, _, g = run(x, False)
+    d = {n: torch.randn(base[n].shape, generator=gen, dtype=torch.float64) for n in INPUTS}
+    up = [x["dO"].nan_to_num().cpu().double(), x["dh_final"].cpu().double()]
+
+    def loss(e):
+        v = {n: base[n] + e * d[n] for n in INPUTS}
+        o, fin = ref.glr(v["x"], v["r"], v["A"], v["i"], v["z"], True, v["h0"], spans)
+        return ((o * up[0]).sum() + (fin * up[1]).sum()).item()
+
+    e = 1e-5
+    want = (loss(e) - loss(-e)) / (2 * e)
+    parts = [g["d" + n].cpu().double() * d[n] for n in INPUTS]
+    assert abs(sum(p.sum().item() for p in parts) - want) <= 5e-6 * sum(p.abs().sum().item() for p in parts)
+
+
+def test_empty(device):
+    A = -torch.rand(16, device=device)
+    u = torch.empty(0, 16, device=device)
+    cu = torch.zeros(3, dtype=torch.int32, device=device)
+    h0 = torch.randn(2, 16, device=device)
+    o, h = rla.rla_glr_forward(u, u, A, i=u, z=u, h0=h0, cu_seqlens=cu)
+    g = rla.rla_glr_backward(u, u, A, u, i=u, z=u, h0=h0, dh_final=h0, cu_seqlens=cu)
+    assert o.numel() == 0 and torch.equal(h, h0) and torch.equal(g["dh0"], h0) and (g["dA"] == 0).all()
+    o, h = rla.rla_glr_forward(torch.empty(2, 0, 16, device=device), torch.empty(2, 0, 16, device=device), A, h0=h0)
+    assert o.shape == (2, 0, 16) and torch.equal(h, h0)
+
+
+BAD = {
+    "A shape": (dict(A=lambda t: t[:-1].contiguous()), ValueError, "A"),
+    "A type": (dict(A=lambda t: t.double()), TypeError, "A"),
+    "r type": (dict(r=lambda t: t.float()), TypeError, "r"),
+    "i shape": (dict(i=lambda t: t[:-1].contiguous()), ValueError, "i"),
+    "z rows": (dict(z=lambda t: t.t().contiguous().t()), ValueError, "contiguous"),
+    "h0 shape": (dict(h0=lambda t: t[:-1].contiguous()), ValueError, "h0"),
+    "device": (dict(r=lambda t: t.cpu()), ValueError, "r"),
+    "save": (dict(save_for_backward=lambda t: True), ValueError, "workspace"),
+    "offsets": (dict(cu_seqlens=lambda t: t.long()), TypeError, "cu_seqlens"),
+}
+
+
+@pytest.mark.parametrize("case", list(BAD))
+def test_refused(device, case):
+    x, _ = make(device, "ragged", 64, "bf16")
+    args = {m: x[m] for m in INPUTS}
+    args.update(cu_seqlens=x["cu"], save_for_backward=False)
+    change, error, match = BAD[case]
+    args.update({n: f(args[n]) for n, f in change.items()})
+    with pytest.raises(error, match=match):
+        rla.rla_glr_forward(**args)
+
+
+def test_refused_gradients(device):
+    x, _ = make(device, "odd", 64, "f32")
+    args = [x[m] for m in ("x", "r", "A")]
+    with pytest.raises(ValueError, match="dO"):
+        rla.rla_glr_backward(*args, None)
+    with pytest.raises(ValueError, match="use_saved"):
+        rla.rla_glr_backward(*args, x["dO"], use_saved=True)
+    with pytest.raises(ValueError, match="required"):
+        rla.rla_glr_backward(*args, x["dO"], grads={})
+    with pytest.raises(ValueError, match="workspace"):
+        rla.rla_glr_backward(*args, x["dO"], workspace=torch.empty(16, dtype=torch.uint8, device=device))
+    h = torch.zeros(3, 64, device=device)
+    with pytest.raises(rla.RLAError):   # states that overlap in part
+        rla.rla_glr_decode(*args, h_in=h[:2], h_out=h[1:])
