@@ -117,10 +117,10 @@ rla_status rla_logprob_backward(const rla_logprob_problem *problem, const void *
  * ------------------------------------------------------------------------ */
 typedef struct {
   int64_t batch, seq_len;    /* B, T (packed: 1, all tokens) */
-  int64_t channels;          /* D, 1 to 2^24 */
+  int64_t channels;          /* D, 1 to 2^23 - 1 */
   int64_t num_seqs;          /* N with cu_seqlens, else ignored */
   const int32_t *cu_seqlens; /* device, N + 1 offsets, or NULL */
-  int64_t x_stride, r_stride, i_stride, z_stride, do_stride;   /* 0: D */
+  int64_t x_stride, r_stride, i_stride, z_stride, do_stride;   /* 0: D; all < 2^23 */
   int32_t normalize;         /* 0 or 1 */
   int32_t dtype;             /* rla_dtype of x, r, i, z, o and their gradients */
 } rla_glr_problem;

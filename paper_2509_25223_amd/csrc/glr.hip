@@ -25,208 +25,240 @@ namespace rla {
 
 namespace {
 
-constexpr int kGlrThreads = 512, kGlrWaves = kGlrThreads / 64, kV = 4;
-constexpr int kLanes = kGlrChannels / kV;        // of a token's row: 16
-constexpr int kSegs = kGlrThreads / kLanes;      // stretches of a tile
-constexpr int kTok = 4;                          // tokens of a stretch
-constexpr int kGlrTile = kSegs * kTok;           // 128
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kGlrThreads = 512, kGlrWaves = kGlrThreads / 64;
+constexpr int kV = 2;                            // channels of a thread
+constexpr int kLanes = kGlrChannels / kV;        // of a token's row: 32
+constexpr int kSegs = kGlrThreads / kLanes;      // stretches of a tile: 16
+constexpr int kTok = 8;                          // tokens of a stretch
+constexpr int kTile = kSegs * kTok;              // 128
 
 // A stretch of tokens: (P, S), P = -1 where a sequence starts in it (then S alone is the state
 // behind it).
 struct Step {
   float P, S;
 };
-__device__ __forceinline__ float apply(const Step& s, float h) { return s.P < 0.f ? s.S : __builtin_fmaf(s.P, h, s.S); }
+__device__ __forceinline__ float apply(const Step& s, float h) {
+  const float next = __builtin_fmaf(s.P, h, s.S);
+  return s.P < 0.f ? s.S : next;
+}
 // first a, then b
 __device__ __forceinline__ Step join(const Step& a, const Step& b) {
-  return Step{a.P < 0.f || b.P < 0.f ? -1.f : a.P * b.P, apply(b, a.S)};
+  const float both = a.P * b.P;
+  return Step{fminf(a.P, b.P) < 0.f ? -1.f : both, apply(b, a.S)};
 }
 
-__device__ __forceinline__ float sigmoid_of(float x, float& rest) {   // and 1 - sigmoid, with its digits
-  const float e = __expf(-x), s = __builtin_amdgcn_rcpf(1.f + e);
-  rest = e < 3e38f ? e * s : 1.f;
-  return s;
+// e^l and 1 - e^2l for l = ln 2 y <= 0: near 0 by the series (to y = -0.18, l = -1/8, off by less
+// than a rounding), else as it stands (3.5 roundings of e^2l there)
+constexpr float series(int n) {   // (2 ln 2)^n / n!
+  double v = 1;
+  for (int i = 1; i <= n; ++i) v *= 2 * 0.69314718055994530942 / i;
+  return (float)v;
+}
+template <bool NORM> __device__ __forceinline__ void decay(float y, float& a, float& w) {
+  a = __builtin_amdgcn_exp2f(y);
+  w = 1.f;
+  if (NORM) {
+    float p = series(6);
+    p = __builtin_fmaf(p, y, series(5));
+    p = __builtin_fmaf(p, y, series(4));
+    p = __builtin_fmaf(p, y, series(3));
+    p = __builtin_fmaf(p, y, series(2));
+    p = -y * __builtin_fmaf(p, y, series(1));
+    float far = __builtin_fmaf(-a, a, 1.f);
+    // (both computed, one selected: the compiler would branch around the series, value by value)
+    asm volatile("" : "+v"(p), "+v"(far));
+    w = y > -0.18f ? p : far;
+  }
 }
 
-// 1 - e^y for y <= 0: near 0 by the series
-__device__ __forceinline__ float one_minus_exp(float y, float ey) {
-  float p = 1.f / 40320.f;
-  p = __builtin_fmaf(p, y, 1.f / 5040.f);
-  p = __builtin_fmaf(p, y, 1.f / 720.f);
-  p = __builtin_fmaf(p, y, 1.f / 120.f);
-  p = __builtin_fmaf(p, y, 1.f / 24.f);
-  p = __builtin_fmaf(p, y, 1.f / 6.f);
-  p = __builtin_fmaf(p, y, 0.5f);
-  p = __builtin_fmaf(p, y, 1.f);
-  return y > -0.5f ? -y * p : 1.f - ey;
+// The channels of a thread, and of a workgroup's 64: the last block and the last piece of a
+// row are moved back to its end, so that all are whole.  What lies in two of them is computed by
+// both, to the same bits.  (WHOLE false: rows of a single channel.)
+template <bool WHOLE> struct Channels {
+  int64_t c;
+  int left;
+  __device__ __forceinline__ Channels(int64_t D, uint32_t b) {
+    const int64_t block = WHOLE ? max(min((int64_t)b * kGlrChannels, D - kGlrChannels), (int64_t)0) : 0;
+    c = block + (threadIdx.x % kLanes) * kV;
+    if (WHOLE) c = min(c, D - kV);
+    left = WHOLE ? kV : (int)max((int64_t)0, min(D - c, (int64_t)kV));
+  }
+  template <typename T> __device__ __forceinline__ void load(const T* row, float (&x)[kV]) const {
+    load_piece<T, kV, WHOLE>(row + c, left, x);
+  }
+  template <typename T> __device__ __forceinline__ void store(T* row, const float (&x)[kV]) const {
+    store_piece<T, kV, WHOLE>(row + c, left, x);
+  }
+  __device__ __forceinline__ void state(const float* rows, int32_t n, int64_t D, float (&h)[kV]) const {
+    if (rows && n >= 0) load(rows + (int64_t)n * D, h);
+    else
+#pragma unroll
+      for (int e = 0; e < kV; ++e) h[e] = 0.f;
+  }
+};
+
+// What a workgroup works on; blocks of channels vary fastest over the workgroups.
+template <bool WHOLE> struct Work {
+  uint32_t chunk;
+  Channels<WHOLE> ch;
+  int64_t t0, end, channel;   // (channel: the lane's own, of the states that waves carry)
+  bool owner;                 // the first wave's lanes write what there is one of per channel
+  __device__ __forceinline__ Work(const GlrParams& p, uint32_t blocks) : chunk(blockIdx.x / blocks), ch(p.D, blockIdx.x - chunk * blocks) {
+    t0 = chunk * p.L;
+    end = min(t0 + p.L, p.map.ntok);
+    channel = ch.c + (threadIdx.x & 63) / kLanes;
+    owner = threadIdx.x < 64 && channel < p.D;
+  }
+  __device__ __forceinline__ int tiles() const { return (int)((end - t0 + kTile - 1) / kTile); }
+};
+
+// One tensor's rows of the thread's tokens, as stored: a tile's base and the rows' distance are the
+// workgroup's, a thread adds an offset of 32 bits.  Past the chunk's end the last row again: loads
+// without branches, all in flight at once.
+template <typename T> struct Rows {
+  typedef typename RowVec<T, kV>::type Vec;
+  Vec v[kTok];
+  template <bool WHOLE>
+  __device__ __forceinline__ void load(const void* base, int64_t stride, int64_t tile, const Work<WHOLE>& w) {
+    const char* row = reinterpret_cast<const char*>(reinterpret_cast<const T*>(base) + tile * stride);
+    const uint32_t first = threadIdx.x / kLanes * kTok, step = (uint32_t)stride * (uint32_t)sizeof(T);
+    const uint32_t col = (uint32_t)w.ch.c * (uint32_t)sizeof(T);
+    if (tile + kTile <= w.end) {
+      const uint32_t off = first * step + col;
+#pragma unroll
+      for (int k = 0; k < kTok; ++k) take<WHOLE>(row + (int64_t)k * step + off, w.ch.left, v[k]);
+    } else {
+      const uint32_t last = (uint32_t)(w.end - tile) - 1;
+#pragma unroll
+      for (int k = 0; k < kTok; ++k) take<WHOLE>(row + (min(first + k, last) * step + col), w.ch.left, v[k]);
+    }
+  }
+  template <bool WHOLE> __device__ __forceinline__ static void take(const char* at, int left, Vec& x) {
+    load_raw<T, kV, WHOLE>(reinterpret_cast<const T*>(at), left, x);
+  }
+  __device__ __forceinline__ float at(int k, int e) const { return to_f<T>(v[k][e]); }
+  __device__ __forceinline__ void clear(int k) {
+#pragma unroll
+    for (int e = 0; e < kV; ++e) v[k][e] = from_f<T>(0.f);
+  }
+};
+// ... written, of a tensor with rows next to each other
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void store_row(const GlrParams& p, void* base, int64_t tile, int k, const Work<WHOLE>& w, const float (&x)[kV]) {
+  const uint32_t off = (threadIdx.x / kLanes * kTok * (uint32_t)p.D + (uint32_t)w.ch.c) * (uint32_t)sizeof(T);
+  char* row = reinterpret_cast<char*>(reinterpret_cast<T*>(base) + (tile + k) * p.D);
+  store_piece<T, kV, WHOLE>(reinterpret_cast<T*>(row + off), w.ch.left, x);
 }
 
-// a and m of a token from its gate's sigmoid
-__device__ __forceinline__ void decay(float A, float sr, bool norm, float& a, float& m) {
-  const float l = A * sr;
-  a = __expf(l);
-  m = norm ? __builtin_amdgcn_sqrtf(fmaxf(one_minus_exp(2.f * l, a * a), 0.f)) : 1.f;
+// Whether no sequence starts in the tile or right behind it, and all of it is of one, in this
+// chunk: then no token needs a look at where it lies.  The same for the whole workgroup.
+__device__ __forceinline__ bool plain_tile(const GlrParams& p, int64_t tile, int64_t end) {
+  if (tile + kTile > end) return false;
+  if (!p.map.seq) {
+    const uint32_t r = (uint32_t)tile % (uint32_t)p.map.T;
+    return r > 0 && r + kTile < (uint32_t)p.map.T;
+  }
+  uint32_t bits = p.map.start_bits(tile + kTile) & 1u;
+#pragma unroll
+  for (int i = 0; i < kTile / 32; ++i) bits |= p.map.start_bits(tile + 32 * i);
+  return bits == 0 && p.map.seq_of(tile) >= 0;
 }
 
-// Where a thread's tokens lie: bits of the tokens t .. t + kTok.
+// Where a thread's tokens lie.  Bit k: token t + k ...
 struct Place {
-  uint32_t in = 0;       // of a sequence (and of this chunk)
-  uint32_t starts = 0;   // first of a sequence, or of a gap
-  int32_t seq[kTok];
-};
-__device__ __forceinline__ Place place_of(const GlrParams& p, int64_t t, int64_t end) {
-  Place q;
-  const int64_t left = end - t;
-  const uint32_t there = left >= kTok ? (1u << kTok) - 1u : left > 0 ? (1u << left) - 1u : 0u;
-  if (!there) {
+  int64_t t;
+  uint32_t in = (1u << kTok) - 1u;   // is of a sequence (and of this chunk)
+  uint32_t there = in;               // is of this chunk
+  uint32_t starts = 0;               // is the first of a sequence, or of a gap
+  uint32_t ends = 0;                 // is the last one of it
+  __device__ __forceinline__ Place(const GlrParams& p, int64_t t_, int64_t end, bool plain) : t(t_) {
+    if (plain) return;
+    const int64_t left = end - t;
+    there = left >= kTok ? there : left > 0 ? (1u << left) - 1u : 0u;
+    in = there;
+    if (!there) return;
+    const uint32_t bits = p.map.start_bits(t);   // (past the last token of all they are set)
+    starts = bits & there;
+    ends = (bits >> 1) & there;
+    if (p.map.seq) {
 #pragma unroll
-    for (int k = 0; k < kTok; ++k) q.seq[k] = -1;
-    return q;
-  }
-  // (bit kTok too: whether the last token ends its sequence; past the last of all they are set)
-  q.starts = p.map.start_bits(t) & ((there << 1) | 1u);
-  q.in = there;
-  if (p.map.seq) {
-#pragma unroll
-    for (int k = 0; k < kTok; ++k) {
-      q.seq[k] = (there >> k) & 1u ? p.map.seq[t + k] : -1;
-      if (q.seq[k] < 0) q.in &= ~(1u << k);
+      for (int k = 0; k < kTok; ++k)
+        if (p.map.seq[min(t + k, end - 1)] < 0) in &= ~(1u << k);
     }
-  } else {
-    const int32_t n = (int32_t)((uint32_t)t / (uint32_t)p.map.T);
-    q.seq[0] = n;
-#pragma unroll
-    for (int k = 1; k < kTok; ++k) q.seq[k] = q.seq[k - 1] + ((q.starts >> k) & 1u);
   }
-  return q;
-}
+  __device__ __forceinline__ int32_t seq(const GlrParams& p, int k) const { return p.map.seq_of(t + k); }
+};
 
-template <typename T, bool FULL>
-__device__ __forceinline__ void load4(const void* base, int64_t stride, int64_t t, int64_t c, int left, bool there, float (&x)[kV]) {
-  if (there) load_piece<T, kV, FULL>(reinterpret_cast<const T*>(base) + t * stride + c, left, x);
-  else
-#pragma unroll
-    for (int e = 0; e < kV; ++e) x[e] = 0.f;
-}
-
-// What a workgroup's waves share: each wave's pair per channel, and the state before it.
+// What a workgroup's waves hand each other: their pairs by channel, of two tiles in turn.
 struct GlrLds {
-  Step wave[kGlrWaves][kGlrChannels];
-  float before[kGlrWaves][kGlrChannels];
+  Step wave[2][kGlrWaves][kGlrChannels];
 };
 
-// The state before the thread's stretch, from the stretches' pairs and the state before the
-// tile.  FORWARD: stretches in order, else from the last one.  `carry` and `pair` are those of channel
-// threadIdx.x (the first 64 threads'): the state, or the pair of everything so far.
+// The pair of the wave's stretches before the thread's (FORWARD: in time, else behind it) into
+// `before`; the wave's own to LDS.
 template <bool FORWARD>
-__device__ __forceinline__ void state_before(const Step (&own)[kV], GlrLds& s, float& carry, Step& pair, float (&h)[kV]) {
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, l = lane % kLanes, seg = lane / kLanes;
-  Step incl[kV], excl[kV];
+__device__ __forceinline__ void wave_steps(const Step (&own)[kV], Step (&wave)[kGlrChannels], Step (&before)[kV]) {
+  static_assert(kLanes == 32, "two stretches a wave");
+  const int lane = threadIdx.x & 63, l = lane % kLanes;
+  const bool later = FORWARD ? lane >= kLanes : lane < kLanes;
 #pragma unroll
   for (int e = 0; e < kV; ++e) {
-    incl[e] = own[e];
-#pragma unroll
-    for (int d = kLanes; d < 64; d <<= 1) {
-      Step o;
-      o.P = FORWARD ? __shfl_up(incl[e].P, d) : __shfl_down(incl[e].P, d);
-      o.S = FORWARD ? __shfl_up(incl[e].S, d) : __shfl_down(incl[e].S, d);
-      if (FORWARD ? lane >= d : lane + d < 64) incl[e] = join(o, incl[e]);
-    }
-    excl[e].P = FORWARD ? __shfl_up(incl[e].P, kLanes) : __shfl_down(incl[e].P, kLanes);
-    excl[e].S = FORWARD ? __shfl_up(incl[e].S, kLanes) : __shfl_down(incl[e].S, kLanes);
-  }
-  const bool outer = FORWARD ? seg == 64 / kLanes - 1 : seg == 0, first = FORWARD ? seg == 0 : seg == 64 / kLanes - 1;
-  if (outer)
-#pragma unroll
-    for (int e = 0; e < kV; ++e) s.wave[w][l * kV + e] = incl[e];
-  __syncthreads();
-  if (threadIdx.x < kGlrChannels) {
-#pragma unroll
-    for (int v = 0; v < kGlrWaves; ++v) {
-      const int u = FORWARD ? v : kGlrWaves - 1 - v;
-      const Step x = s.wave[u][threadIdx.x];
-      s.before[u][threadIdx.x] = carry;
-      carry = apply(x, carry);
-      pair = join(pair, x);
-    }
-  }
-  __syncthreads();
-#pragma unroll
-  for (int e = 0; e < kV; ++e) {
-    h[e] = s.before[w][l * kV + e];
-    if (!first) h[e] = apply(excl[e], h[e]);
+    const Step other{__shfl_xor(own[e].P, kLanes), __shfl_xor(own[e].S, kLanes)};
+    before[e].P = later ? other.P : 1.f;
+    before[e].S = later ? other.S : 0.f;
+    const Step both = join(other, own[e]);
+    if (later) wave[l * kV + e] = both;
   }
 }
 
-// Channel threadIdx.x of the first 64 threads: the state before chunk c, from the pairs
-// of the chunks before it (FORWARD) or behind it.
+// After the barrier: the state before the thread's stretch.  Each wave goes through all waves' pairs
+// for itself, a lane for one channel (kV (lane % kLanes) + lane / kLanes), whose state it carries from
+// tile to tile (PAIR: the pair of everything so far).
+template <bool FORWARD, bool PAIR>
+__device__ __forceinline__ void state_before(const Step (&wave)[kGlrWaves][kGlrChannels], const Step (&before)[kV], float& carry,
+                                             Step& pair, float (&h)[kV]) {
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, own = (lane % kLanes) * kV + lane / kLanes;
+  float mine = carry;
+#pragma unroll
+  for (int v = 0; v < kGlrWaves; ++v) {
+    const int u = FORWARD ? v : kGlrWaves - 1 - v;
+    const Step x = wave[u][own];
+    mine = u == w ? carry : mine;
+    carry = apply(x, carry);
+    if (PAIR) pair = join(pair, x);
+  }
+#pragma unroll
+  for (int e = 0; e < kV; ++e) h[e] = apply(before[e], __shfl(mine, e * kLanes + lane % kLanes));
+}
+
+// The state of the lane's channel before chunk c, from the pairs of the chunks before it (FORWARD)
+// or behind it.
 template <bool FORWARD> __device__ __forceinline__ float chunk_state(const GlrParams& p, int c, int64_t channel) {
   float h = 0.f;
   if (p.apart || channel >= p.D) return h;
-  for (int k = FORWARD ? 0 : p.nchunk - 1; k != c; k += FORWARD ? 1 : -1) {
-    const float* at = p.sum + ((int64_t)k * 2) * p.D + channel;
-    h = apply(Step{at[0], at[p.D]}, h);
+  const int count = FORWARD ? c : p.nchunk - 1 - c;
+  constexpr int U = 8;   // loads in flight
+  for (int k0 = 0; k0 < count; k0 += U) {
+    Step x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = min(k0 + u, count - 1), chunk = FORWARD ? k : p.nchunk - 1 - k;
+      const float* at = p.sum + ((int64_t)chunk * 2) * p.D + channel;
+      x[u] = Step{at[0], at[p.D]};
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (k0 + u < count) h = apply(x[u], h);
   }
   return h;
 }
-
-// the thread's channels of a state row, zeros without one
-template <bool FULL>
-__device__ __forceinline__ void load_state(const float* state, int32_t n, int64_t D, int64_t c, int left, float (&h)[kV]) {
-  if (state && n >= 0) load_piece<float, kV, FULL>(state + (int64_t)n * D + c, left, h);
-  else
-#pragma unroll
-    for (int e = 0; e < kV; ++e) h[e] = 0.f;
+__device__ __forceinline__ void write_pair(const GlrParams& p, uint32_t chunk, int64_t channel, const Step& pair) {
+  float* at = p.sum + (int64_t)chunk * 2 * p.D + channel;
+  at[0] = pair.P;
+  at[p.D] = pair.S;
 }
 
-// The thread's tokens as a, b; tokens outside every sequence have b = 0.
-template <typename T, bool HAS_I, bool FULL>
-__device__ __forceinline__ void load_steps(const GlrParams& p, const Place& q, int64_t t, int64_t c, int left, const float (&A)[kV],
-                                           float (&a)[kTok][kV], float (&b)[kTok][kV]) {
-#pragma unroll
-  for (int k = 0; k < kTok; ++k) {
-    const bool in = (q.in >> k) & 1u;
-    float x[kV], r[kV], i[kV];
-    load4<T, FULL>(p.x, p.xs, t + k, c, left, in, x);
-    load4<T, FULL>(p.r, p.rs, t + k, c, left, in, r);
-    if (HAS_I) load4<T, FULL>(p.i, p.is, t + k, c, left, in, i);
-#pragma unroll
-    for (int e = 0; e < kV; ++e) {
-      float m;
-      decay(A[e], sigmoid_fast(r[e]), p.normalize, a[k][e], m);
-      b[k][e] = m * x[e];
-      if (HAS_I) b[k][e] *= sigmoid_fast(i[e]);
-      if (!in) a[k][e] = 1.f, b[k][e] = 0.f;
-    }
-  }
-}
-
-// The stretch's pair.
-template <bool FULL>
-__device__ __forceinline__ void steps_pair(const GlrParams& p, const Place& q, int64_t c, int left, const float (&a)[kTok][kV],
-                                           const float (&b)[kTok][kV], Step (&own)[kV]) {
-#pragma unroll
-  for (int e = 0; e < kV; ++e) own[e] = Step{1.f, 0.f};
-#pragma unroll
-  for (int k = 0; k < kTok; ++k) {
-    if ((q.starts >> k) & 1u) {
-      float h[kV];
-      load_state<FULL>(p.h0, q.seq[k], p.D, c, left, h);
-#pragma unroll
-      for (int e = 0; e < kV; ++e) own[e] = Step{-1.f, h[e]};
-    }
-#pragma unroll
-    for (int e = 0; e < kV; ++e) {
-      own[e].P = own[e].P < 0.f ? -1.f : own[e].P * a[k][e];
-      own[e].S = __builtin_fmaf(a[k][e], own[e].S, b[k][e]);
-    }
-  }
-}
-
-// ---------------------------------------------------------------------------
-// forward.  blockIdx.x: block of channels, fastest, then chunk; behind them workgroups that copy the
-// states of sequences without tokens.  SUMMARY: the chunk's pair only.
-// ---------------------------------------------------------------------------
 constexpr uint32_t kGlrEmptyWgs = 16;
 __device__ __forceinline__ void copy_empty(const GlrParams& p, const float* from, float* to, uint32_t wg) {
   for (int64_t n = wg; n < p.map.nseq; n += kGlrEmptyWgs) {
@@ -235,225 +267,340 @@ __device__ __forceinline__ void copy_empty(const GlrParams& p, const float* from
   }
 }
 
-template <typename T, bool HAS_I, bool HAS_Z, bool SUMMARY, bool FULL>
+// The pair of the thread's stretch.
+template <bool PLAIN, bool WHOLE>
+__device__ __forceinline__ void stretch_forward(const GlrParams& p, const Place& q, const Channels<WHOLE>& ch,
+                                                const float (&a)[kTok][kV], const float (&b)[kTok][kV], Step (&own)[kV]) {
+#pragma unroll
+  for (int e = 0; e < kV; ++e) own[e] = Step{1.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < kTok; ++k) {
+    if (!PLAIN && ((q.starts >> k) & 1u)) {
+      float h[kV];
+      ch.state(p.h0, q.seq(p, k), p.D, h);
+#pragma unroll
+      for (int e = 0; e < kV; ++e) own[e].S = h[e];
+    }
+#pragma unroll
+    for (int e = 0; e < kV; ++e) {
+      own[e].P *= a[k][e];
+      own[e].S = __builtin_fmaf(a[k][e], own[e].S, b[k][e]);
+    }
+  }
+  if (!PLAIN && q.starts)
+#pragma unroll
+    for (int e = 0; e < kV; ++e) own[e].P = -1.f;
+}
+
+// ---------------------------------------------------------------------------
+// forward.  Behind the chunks' workgroups those that copy the states of sequences without
+// tokens.  SUMMARY: the chunk's pair only.
+// ---------------------------------------------------------------------------
+template <typename T, bool HAS_I, bool HAS_Z, bool NORM, bool SUMMARY, bool WHOLE>
 __global__ __launch_bounds__(kGlrThreads) void glr_fwd_kernel(GlrParams p, uint32_t blocks, int save) {
   __shared__ GlrLds lds;
-  const uint32_t chunk = blockIdx.x / blocks;
-  if (chunk >= (uint32_t)p.nchunk) {
+  if (blockIdx.x >= blocks * p.nchunk) {
     copy_empty(p, p.h0, p.hfin, blockIdx.x - p.nchunk * blocks);
     return;
   }
-  const int64_t block = (int64_t)(blockIdx.x - chunk * blocks) * kGlrChannels;
-  const int64_t c = block + (threadIdx.x % kLanes) * kV, own_channel = block + threadIdx.x;
-  const int left = (int)min(p.D - c, (int64_t)kV);
-  const int64_t t0 = chunk * p.L, end = min(t0 + p.L, p.map.ntok);
+  const Work<WHOLE> w(p, blocks);
   float A[kV];
-  if (left > 0) load_piece<float, kV, FULL>(p.A + c, left, A);
-  float carry = SUMMARY || threadIdx.x >= kGlrChannels ? 0.f : chunk_state<true>(p, (int)chunk, own_channel);
-  Step pair{1.f, 0.f};
-  for (int tile = 0; t0 + (int64_t)tile * kGlrTile < end; ++tile) {
-    const int64_t t = t0 + (int64_t)tile * kGlrTile + (threadIdx.x / kLanes) * kTok;
-    if (save && !SUMMARY && threadIdx.x < kGlrChannels && own_channel < p.D)
-      p.ck[((int64_t)chunk * p.tiles + tile) * p.D + own_channel] = carry;
-    Place q = place_of(p, left > 0 ? t : end, end);
-    float a[kTok][kV], b[kTok][kV], h[kV];
-    Step own[kV];
-    load_steps<T, HAS_I, FULL>(p, q, t, c, left, A, a, b);
-    steps_pair<FULL>(p, q, c, left, a, b, own);
-    state_before<true>(own, lds, carry, pair, h);
-    if (SUMMARY) continue;
+  w.ch.load(p.A, A);
 #pragma unroll
-    for (int k = 0; k < kTok; ++k) {
-      if (t + k >= end || left <= 0) break;
-      if ((q.starts >> k) & 1u) load_state<FULL>(p.h0, q.seq[k], p.D, c, left, h);
-      const bool in = (q.in >> k) & 1u;
-      float o[kV], z[kV];
-      if (HAS_Z) load4<T, FULL>(p.z, p.zs, t + k, c, left, in, z);
+  for (int e = 0; e < kV; ++e) A[e] *= kLog2e;
+  float carry = SUMMARY ? 0.f : chunk_state<true>(p, (int)w.chunk, w.channel);
+  Step pair{1.f, 0.f};
+  Rows<T> x, r, i, z;
+  auto load = [&](int64_t tile) {
+    x.load(p.x, p.xs, tile, w);
+    r.load(p.r, p.rs, tile, w);
+    if (HAS_I) i.load(p.i, p.is, tile, w);
+  };
+  load(w.t0);
+  const int tiles = w.tiles();
+  for (int n = 0; n < tiles; ++n) {
+    const int64_t tile = w.t0 + (int64_t)n * kTile;
+    const bool plain = plain_tile(p, tile, w.end);
+    if (HAS_Z && !SUMMARY) z.load(p.z, p.zs, tile, w);
+    if (save && !SUMMARY && w.owner) p.ck[((int64_t)w.chunk * p.tiles + n) * p.D + w.channel] = carry;
+    const Place q(p, tile + threadIdx.x / kLanes * kTok, w.end, plain);
+    float a[kTok][kV], b[kTok][kV], h[kV];
+    Step own[kV], before[kV];
+#pragma unroll
+    for (int k = 0; k < kTok; ++k)
 #pragma unroll
       for (int e = 0; e < kV; ++e) {
-        h[e] = __builtin_fmaf(a[k][e], h[e], b[k][e]);
-        o[e] = HAS_Z ? h[e] * z[e] * sigmoid_fast(z[e]) : h[e];
-        if (!in) o[e] = 0.f;
+        float m;
+        decay<NORM>(A[e] * sigmoid_fast(r.at(k, e)), a[k][e], m);
+        b[k][e] = x.at(k, e);
+        if (NORM) b[k][e] *= __builtin_amdgcn_sqrtf(fmaxf(m, 0.f));
+        if (HAS_I) b[k][e] *= sigmoid_fast(i.at(k, e));
       }
-      if (p.o) store_piece<T, kV, FULL>(reinterpret_cast<T*>(p.o) + (t + k) * p.D + c, left, o);
-      if (p.hfin && in && ((q.starts >> (k + 1)) & 1u))
-        store_piece<float, kV, FULL>(p.hfin + (int64_t)q.seq[k] * p.D + c, left, h);
+    if (n + 1 < tiles) load(tile + kTile);
+    if (!plain) {   // tokens of no sequence: nothing happens, and zeros come out
+#pragma unroll
+      for (int k = 0; k < kTok; ++k) {
+        if ((q.in >> k) & 1u) continue;
+        if (HAS_Z && !SUMMARY) z.clear(k);
+#pragma unroll
+        for (int e = 0; e < kV; ++e) a[k][e] = 1.f, b[k][e] = 0.f;
+      }
     }
+    if (plain) stretch_forward<true>(p, q, w.ch, a, b, own);
+    else stretch_forward<false>(p, q, w.ch, a, b, own);
+    wave_steps<true>(own, lds.wave[n & 1][threadIdx.x >> 6], before);
+    __syncthreads();
+    state_before<true, SUMMARY>(lds.wave[n & 1], before, carry, pair, h);
+    if (SUMMARY) continue;
+    auto finish = [&](auto only) {
+      constexpr bool PLAIN = decltype(only)::value;
+#pragma unroll
+      for (int k = 0; k < kTok; ++k) {
+        if (!PLAIN) {
+          if (!((q.there >> k) & 1u)) break;
+          if ((q.starts >> k) & 1u) w.ch.state(p.h0, q.seq(p, k), p.D, h);
+        }
+        float out[kV];
+#pragma unroll
+        for (int e = 0; e < kV; ++e) {
+          h[e] = __builtin_fmaf(a[k][e], h[e], b[k][e]);
+          out[e] = h[e];
+          if (HAS_Z) out[e] *= z.at(k, e) * sigmoid_fast(z.at(k, e));
+        }
+        if (p.o) store_row<T>(p, p.o, tile, k, w, out);
+        if (!PLAIN && p.hfin && ((q.in & q.ends) >> k) & 1u) w.ch.store(p.hfin + (int64_t)q.seq(p, k) * p.D, h);
+      }
+    };
+    if (plain) finish(std::true_type());
+    else finish(std::false_type());
   }
-  if (SUMMARY && threadIdx.x < kGlrChannels && own_channel < p.D) {
-    float* at = p.sum + (int64_t)chunk * 2 * p.D + own_channel;
-    at[0] = pair.P;
-    at[p.D] = pair.S;
-  }
+  if (SUMMARY && w.owner) write_pair(p, w.chunk, w.channel, pair);
+}
+
+// Every second token: keeps the scheduler from taking the tokens' independent chains all at once,
+// for which there are not registers enough.
+__device__ __forceinline__ void few_registers(int k) {
+  if (k % 2 == 0) __builtin_amdgcn_sched_barrier(0);
 }
 
 // ---------------------------------------------------------------------------
 // backward.  The message from a token to the one before it is u_t = a_t l_t, l_t = g_t + u_{t+1};
-// a sequence's last token gets dh_final, its first one's message is dh_init.
+// a sequence's last token gets dh_final, its first one's message is dh_init.  A tile's states and
+// messages need nothing of each other, so one barrier a tile serves both.
 // ---------------------------------------------------------------------------
-template <typename T, bool HAS_I, bool HAS_Z, bool SUMMARY, bool FULL>
-__global__ __launch_bounds__(kGlrThreads) void glr_bwd_kernel(GlrParams p, uint32_t blocks) {
-  __shared__ GlrLds lds;
-  const uint32_t chunk = blockIdx.x / blocks;
-  if (chunk >= (uint32_t)p.nchunk) {
+template <typename T, bool HAS_I, bool HAS_Z, bool NORM, bool SUMMARY, bool WHOLE>
+__global__ __launch_bounds__(kGlrThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void glr_bwd_kernel(GlrParams p, uint32_t blocks) {
+  __shared__ GlrLds fwd, rev;
+  if (blockIdx.x >= blocks * p.nchunk) {
     copy_empty(p, p.dhfin, p.dh0, blockIdx.x - p.nchunk * blocks);
     return;
   }
-  const int64_t block = (int64_t)(blockIdx.x - chunk * blocks) * kGlrChannels;
-  const int64_t c = block + (threadIdx.x % kLanes) * kV, own_channel = block + threadIdx.x;
-  const int left = (int)min(p.D - c, (int64_t)kV);
-  const int64_t t0 = chunk * p.L, end = min(t0 + p.L, p.map.ntok);
-  float A[kV], dA[kV] = {0.f, 0.f, 0.f, 0.f};
-  if (left > 0) load_piece<float, kV, FULL>(p.A + c, left, A);
-  float carry = SUMMARY || threadIdx.x >= kGlrChannels ? 0.f : chunk_state<false>(p, (int)chunk, own_channel);
+  const Work<WHOLE> w(p, blocks);
+  float A[kV], dA[kV] = {0.f, 0.f};
+  w.ch.load(p.A, A);
+  float carry = SUMMARY ? 0.f : chunk_state<false>(p, (int)w.chunk, w.channel);
   Step pair{1.f, 0.f};
-  for (int tile = (int)((end - t0 + kGlrTile - 1) / kGlrTile) - 1; tile >= 0; --tile) {
-    const int64_t t = t0 + (int64_t)tile * kGlrTile + (threadIdx.x / kLanes) * kTok;
-    Place q = place_of(p, left > 0 ? t : end, end);
-    const uint32_t ends = q.starts >> 1;   // last of a sequence
-    float a[kTok][kV], b[kTok][kV], h[kV], before[kTok][kV];
-    Step own[kV];
-    load_steps<T, HAS_I, FULL>(p, q, t, c, left, A, a, b);
+  Rows<T> x, r, i, z, d;
+  auto load = [&](int64_t tile) {
+    r.load(p.r, p.rs, tile, w);
+    d.load(p.dO, p.dos, tile, w);
+    if (HAS_Z) z.load(p.z, p.zs, tile, w);
+    if (HAS_I && !SUMMARY) i.load(p.i, p.is, tile, w);
+  };
+  const int tiles = w.tiles();
+  load(w.t0 + (int64_t)(tiles - 1) * kTile);
+  for (int n = tiles - 1; n >= 0; --n) {
+    const int64_t tile = w.t0 + (int64_t)n * kTile;
+    const bool plain = plain_tile(p, tile, w.end);
+    float state = 0.f;
     if (!SUMMARY) {
-      float state = 0.f;
-      Step none{1.f, 0.f};
-      if (threadIdx.x < kGlrChannels && own_channel < p.D) state = p.ck[((int64_t)chunk * p.tiles + tile) * p.D + own_channel];
-      steps_pair<FULL>(p, q, c, left, a, b, own);
-      state_before<true>(own, lds, state, none, h);
-#pragma unroll
-      for (int k = 0; k < kTok; ++k) {
-        if ((q.starts >> k) & 1u) load_state<FULL>(p.h0, q.seq[k], p.D, c, left, h);
-#pragma unroll
-        for (int e = 0; e < kV; ++e) {
-          before[k][e] = h[e];
-          h[e] = __builtin_fmaf(a[k][e], h[e], b[k][e]);
-        }
-      }
+      x.load(p.x, p.xs, tile, w);
+      if (w.channel < p.D) state = p.ck[((int64_t)w.chunk * p.tiles + n) * p.D + w.channel];
     }
-    // g, and the messages' pairs from the last token on
-    float g[kTok][kV];
+    const Place q(p, tile + threadIdx.x / kLanes * kTok, w.end, plain);
+    // m: 1 - a^2; slope: dO SiLU'(z)
+    float a[kTok][kV], m[kTok][kV], sr[kTok][kV], si[kTok][kV], g[kTok][kV], slope[kTok][kV], h[kV], u[kV];
+    Step own[kV], before[kV], behind[kV];
 #pragma unroll
     for (int k = 0; k < kTok; ++k) {
-      const bool in = (q.in >> k) & 1u;
-      float z[kV];
-      load4<T, FULL>(p.dO, p.dos, t + k, c, left, in, g[k]);
-      if (HAS_Z) {
-        load4<T, FULL>(p.z, p.zs, t + k, c, left, in, z);
+      few_registers(k);
+#pragma unroll
+      for (int e = 0; e < kV; ++e) {
+        sr[k][e] = sigmoid_fast(r.at(k, e));
+        decay<NORM && !SUMMARY>(A[e] * kLog2e * sr[k][e], a[k][e], m[k][e]);
+        if (HAS_I && !SUMMARY) si[k][e] = sigmoid_fast(i.at(k, e));
+        else si[k][e] = 1.f;
+        g[k][e] = d.at(k, e);
+        if (HAS_Z) {
+          float silu;
+          slope[k][e] = silu_grad_f(z.at(k, e), silu) * g[k][e];
+          g[k][e] *= silu;
+        }
+      }
+    }
+    if (!plain) {   // tokens of no sequence: nothing happens, and zeros come out
+#pragma unroll
+      for (int k = 0; k < kTok; ++k) {
+        if ((q.in >> k) & 1u) continue;
+        if (!SUMMARY) x.clear(k);
 #pragma unroll
         for (int e = 0; e < kV; ++e) {
-          const float d = g[k][e];
-          float silu;
-          const float slope = silu_grad_f(z[e], silu);
-          g[k][e] = d * silu;
-          if (!SUMMARY) z[e] = in ? d * __builtin_fmaf(a[k][e], before[k][e], b[k][e]) * slope : 0.f;
+          a[k][e] = m[k][e] = 1.f;
+          g[k][e] = sr[k][e] = si[k][e] = 0.f;
+          if (HAS_Z) slope[k][e] = 0.f;
         }
-        if (!SUMMARY && t + k < end && left > 0)
-          store_piece<T, kV, FULL>(reinterpret_cast<T*>(p.dz) + (t + k) * p.D + c, left, z);
       }
     }
+    if (n > 0) load(tile - kTile);
+    // messages from the last token on
 #pragma unroll
     for (int e = 0; e < kV; ++e) own[e] = Step{1.f, 0.f};
+    auto messages = [&](auto only) {
+      constexpr bool PLAIN = decltype(only)::value;
 #pragma unroll
-    for (int k = kTok - 1; k >= 0; --k) {
-      if ((ends >> k) & 1u) {
-        float d[kV];
-        load_state<FULL>(p.dhfin, q.seq[k], p.D, c, left, d);
+      for (int k = kTok - 1; k >= 0; --k) {
+        if (!PLAIN && ((q.ends >> k) & 1u)) {
+          w.ch.state(p.dhfin, q.seq(p, k), p.D, u);
 #pragma unroll
-        for (int e = 0; e < kV; ++e) own[e] = Step{-1.f, d[e]};
+          for (int e = 0; e < kV; ++e) own[e].S = u[e];
+        }
+#pragma unroll
+        for (int e = 0; e < kV; ++e) {
+          own[e].P *= a[k][e];
+          own[e].S = a[k][e] * (own[e].S + g[k][e]);
+        }
       }
+      if (!PLAIN && q.ends)
 #pragma unroll
-      for (int e = 0; e < kV; ++e) {
-        own[e].P = own[e].P < 0.f ? -1.f : own[e].P * a[k][e];
-        own[e].S = a[k][e] * (own[e].S + g[k][e]);
-      }
+        for (int e = 0; e < kV; ++e) own[e].P = -1.f;
+    };
+    if (plain) messages(std::true_type());
+    else messages(std::false_type());
+    wave_steps<false>(own, rev.wave[n & 1][threadIdx.x >> 6], behind);
+    if (!SUMMARY) {   // states
+      float b[kTok][kV];
+#pragma unroll
+      for (int k = 0; k < kTok; ++k)
+#pragma unroll
+        for (int e = 0; e < kV; ++e) {
+          b[k][e] = si[k][e] * x.at(k, e);
+          if (NORM) b[k][e] *= __builtin_amdgcn_sqrtf(fmaxf(m[k][e], 0.f));
+        }
+      if (plain) stretch_forward<true>(p, q, w.ch, a, b, own);
+      else stretch_forward<false>(p, q, w.ch, a, b, own);
+      wave_steps<true>(own, fwd.wave[n & 1][threadIdx.x >> 6], before);
     }
-    float u[kV];
-    state_before<false>(own, lds, carry, pair, u);
+    __syncthreads();
+    state_before<false, SUMMARY>(rev.wave[n & 1], behind, carry, pair, u);
     if (SUMMARY) continue;
+    Step none{1.f, 0.f};
+    state_before<true, false>(fwd.wave[n & 1], before, state, none, h);
+    auto finish = [&](auto only) {
+      constexpr bool PLAIN = decltype(only)::value;
+      float prev[kTok][kV];
 #pragma unroll
-    for (int k = kTok - 1; k >= 0; --k) {
-      if (t + k >= end || left <= 0) continue;
-      const bool in = (q.in >> k) & 1u;
-      if ((ends >> k) & 1u) load_state<FULL>(p.dhfin, q.seq[k], p.D, c, left, u);
-      float x[kV], r[kV], i[kV];
-      load4<T, FULL>(p.x, p.xs, t + k, c, left, in, x);
-      load4<T, FULL>(p.r, p.rs, t + k, c, left, in, r);
-      if (HAS_I) load4<T, FULL>(p.i, p.is, t + k, c, left, in, i);
+      for (int k = 0; k < kTok; ++k) {
+        few_registers(k);
+        if (!PLAIN && ((q.starts >> k) & 1u)) w.ch.state(p.h0, q.seq(p, k), p.D, h);
+        float dz[kV];
 #pragma unroll
-      for (int e = 0; e < kV; ++e) {
-        float rest_r, rest_i = 0.f, si = 1.f, a1, m;
-        const float sr = sigmoid_of(r[e], rest_r);
-        if (HAS_I) si = sigmoid_of(i[e], rest_i);
-        decay(A[e], sr, p.normalize, a1, m);
-        const float l = g[k][e] + u[e], lm = l * m * si;
-        float dlog = l * before[k][e] * a1;
-        if (p.normalize && m > 0.f) dlog -= l * si * x[e] * (a1 * a1) * __builtin_amdgcn_rcpf(m);
-        i[e] = in ? lm * x[e] * rest_i : 0.f;
-        x[e] = in ? lm : 0.f;
-        r[e] = in ? dlog * (A[e] * sr) * rest_r : 0.f;
-        dA[e] += in ? dlog * sr : 0.f;
-        u[e] = a[k][e] * l;
+        for (int e = 0; e < kV; ++e) {
+          float b = si[k][e] * x.at(k, e);
+          if (NORM) b *= __builtin_amdgcn_sqrtf(fmaxf(m[k][e], 0.f));
+          prev[k][e] = h[e];
+          h[e] = __builtin_fmaf(a[k][e], h[e], b);
+          if (HAS_Z) dz[e] = slope[k][e] * h[e];
+        }
+        if (HAS_Z && (PLAIN || ((q.there >> k) & 1u))) store_row<T>(p, p.dz, tile, k, w, dz);
       }
-      store_piece<T, kV, FULL>(reinterpret_cast<T*>(p.dx) + (t + k) * p.D + c, left, x);
-      store_piece<T, kV, FULL>(reinterpret_cast<T*>(p.dr) + (t + k) * p.D + c, left, r);
-      if (HAS_I) store_piece<T, kV, FULL>(reinterpret_cast<T*>(p.di) + (t + k) * p.D + c, left, i);
-      if (p.dh0 && in && (q.starts >> k) & 1u) store_piece<float, kV, FULL>(p.dh0 + (int64_t)q.seq[k] * p.D + c, left, u);
-    }
+#pragma unroll
+      for (int k = kTok - 1; k >= 0; --k) {
+        few_registers(k);
+        if (!PLAIN) {
+          if (!((q.there >> k) & 1u)) continue;
+          if ((q.ends >> k) & 1u) w.ch.state(p.dhfin, q.seq(p, k), p.D, u);
+        }
+        float dx[kV], dr[kV], di[kV];
+#pragma unroll
+        for (int e = 0; e < kV; ++e) {
+          const float l = g[k][e] + u[e];
+          float into = l * si[k][e], dlog = prev[k][e];
+          if (NORM) {   // m is the root of 1 - a^2, `over` its inverse
+            const float one = fmaxf(m[k][e], 0.f), over = one > 0.f ? __builtin_amdgcn_rsqf(one) : 0.f;
+            dlog = __builtin_fmaf(-(si[k][e] * x.at(k, e)), a[k][e] * over, dlog);
+            into *= one * over;
+          }
+          u[e] = a[k][e] * l;
+          dlog *= u[e] * sr[k][e];
+          dx[e] = into;
+          di[e] = into * x.at(k, e) * (1.f - si[k][e]);
+          dr[e] = dlog * A[e] * (1.f - sr[k][e]);
+          dA[e] += dlog;
+        }
+        store_row<T>(p, p.dx, tile, k, w, dx);
+        store_row<T>(p, p.dr, tile, k, w, dr);
+        if (HAS_I) store_row<T>(p, p.di, tile, k, w, di);
+        if (!PLAIN && p.dh0 && ((q.in & q.starts) >> k) & 1u) w.ch.store(p.dh0 + (int64_t)q.seq(p, k) * p.D, u);
+      }
+    };
+    if (plain) finish(std::true_type());
+    else finish(std::false_type());
   }
   if (SUMMARY) {
-    if (threadIdx.x < kGlrChannels && own_channel < p.D) {
-      float* at = p.sum + (int64_t)chunk * 2 * p.D + own_channel;
-      at[0] = pair.P;
-      at[p.D] = pair.S;
-    }
+    if (w.owner) write_pair(p, w.chunk, w.channel, pair);
     return;
   }
   // dA over the workgroup's stretches
-#pragma unroll
-  for (int e = 0; e < kV; ++e)
-#pragma unroll
-    for (int d = kLanes; d < 64; d <<= 1) dA[e] += __shfl_xor(dA[e], d);
-  if ((threadIdx.x & 63) < kLanes)
-#pragma unroll
-    for (int e = 0; e < kV; ++e) lds.before[threadIdx.x >> 6][(threadIdx.x % kLanes) * kV + e] = dA[e];
   __syncthreads();
-  if (threadIdx.x < kGlrChannels && own_channel < p.D) {
+  float* sums = reinterpret_cast<float*>(&fwd);
+#pragma unroll
+  for (int e = 0; e < kV; ++e) {
+    dA[e] += __shfl_xor(dA[e], kLanes);
+    if ((threadIdx.x & 63) < kLanes) sums[(threadIdx.x >> 6) * kGlrChannels + threadIdx.x % kLanes * kV + e] = dA[e];
+  }
+  __syncthreads();
+  if (w.owner) {
+    const int own = threadIdx.x % kLanes * kV + threadIdx.x / kLanes;
     float sum = 0.f;
-    for (int w = 0; w < kGlrWaves; ++w) sum += lds.before[w][threadIdx.x];
-    p.pA[(int64_t)chunk * p.D + own_channel] = sum;
+    for (int v = 0; v < kGlrWaves; ++v) sum += sums[v * kGlrChannels + own];
+    p.pA[(int64_t)w.chunk * p.D + w.channel] = sum;
   }
 }
 
 // Single tokens: a thread owns 4 channels of a sequence, whose state it reads before it
-// writes (in place works).
-template <typename T, bool HAS_I, bool HAS_Z, bool FULL>
+// writes (in place works: a row's last piece is its own, in part).
+constexpr int kDecV = 4;
+template <typename T, bool HAS_I, bool HAS_Z, bool NORM, bool FULL>
 __global__ __launch_bounds__(kThreads) void glr_decode_kernel(GlrParams p, uint32_t pieces, uint32_t count) {
   const uint32_t id = blockIdx.x * kThreads + threadIdx.x;
   if (id >= count) return;
-  const int64_t n = id / pieces, c = (int64_t)(id % pieces) * kV;
-  const int left = (int)min(p.D - c, (int64_t)kV);
-  float A[kV], h[kV];
-  load_piece<float, kV, FULL>(p.A + c, left, A);
-  load_state<FULL>(p.h0, (int32_t)n, p.D, c, left, h);
+  const int64_t n = id / pieces, c = (int64_t)(id % pieces) * kDecV;
+  const int left = (int)min(p.D - c, (int64_t)kDecV);
+  float A[kDecV], h[kDecV];
+  load_piece<float, kDecV, FULL>(p.A + c, left, A);
+  if (p.h0) load_piece<float, kDecV, FULL>(p.h0 + n * p.D + c, left, h);
+  else
+#pragma unroll
+    for (int e = 0; e < kDecV; ++e) h[e] = 0.f;
   for (int64_t k = 0; k < p.map.T; ++k) {
     const int64_t t = n * p.map.T + k;
-    float x[kV], r[kV], i[kV], z[kV];
-    load4<T, FULL>(p.x, p.xs, t, c, left, true, x);
-    load4<T, FULL>(p.r, p.rs, t, c, left, true, r);
-    if (HAS_I) load4<T, FULL>(p.i, p.is, t, c, left, true, i);
-    if (HAS_Z) load4<T, FULL>(p.z, p.zs, t, c, left, true, z);
+    float x[kDecV], r[kDecV], i[kDecV], z[kDecV];
+    load_piece<T, kDecV, FULL>(reinterpret_cast<const T*>(p.x) + t * p.xs + c, left, x);
+    load_piece<T, kDecV, FULL>(reinterpret_cast<const T*>(p.r) + t * p.rs + c, left, r);
+    if (HAS_I) load_piece<T, kDecV, FULL>(reinterpret_cast<const T*>(p.i) + t * p.is + c, left, i);
+    if (HAS_Z) load_piece<T, kDecV, FULL>(reinterpret_cast<const T*>(p.z) + t * p.zs + c, left, z);
 #pragma unroll
-    for (int e = 0; e < kV; ++e) {
-      float a, m;
-      decay(A[e], sigmoid_fast(r[e]), p.normalize, a, m);
-      float b = m * x[e];
+    for (int e = 0; e < kDecV; ++e) {
+      float a, m, b = x[e];
+      decay<NORM>(A[e] * kLog2e * sigmoid_fast(r[e]), a, m);
+      if (NORM) b *= __builtin_amdgcn_sqrtf(fmaxf(m, 0.f));
       if (HAS_I) b *= sigmoid_fast(i[e]);
       h[e] = __builtin_fmaf(a, h[e], b);
-      x[e] = HAS_Z ? h[e] * z[e] * sigmoid_fast(z[e]) : h[e];
+      x[e] = HAS_Z ? h[e] * (z[e] * sigmoid_fast(z[e])) : h[e];
     }
-    store_piece<T, kV, FULL>(reinterpret_cast<T*>(p.o) + t * p.D + c, left, x);
+    store_piece<T, kDecV, FULL>(reinterpret_cast<T*>(p.o) + t * p.D + c, left, x);
   }
-  store_piece<float, kV, FULL>(p.hfin + n * p.D + c, left, h);
+  store_piece<float, kDecV, FULL>(p.hfin + n * p.D + c, left, h);
 }
 
 // ---------------------------------------------------------------------------
@@ -461,12 +608,16 @@ __global__ __launch_bounds__(kThreads) void glr_decode_kernel(GlrParams p, uint3
 // ---------------------------------------------------------------------------
 uint32_t blocks_of(const GlrParams& p) { return (uint32_t)((p.D + kGlrChannels - 1) / kGlrChannels); }
 
-template <typename F> hipError_t with(bool bf16, bool i, bool z, bool full, F f) {
+template <typename F> hipError_t with(const GlrParams& p, bool bf16, bool i, bool z, bool whole, F f) {
   auto types = [&](auto T) {
     auto gates = [&](auto I) {
       auto out = [&](auto Z) {
-        if (full) f(T, I, Z, std::true_type());
-        else f(T, I, Z, std::false_type());
+        auto norm = [&](auto N) {
+          if (whole) f(T, I, Z, N, std::true_type());
+          else f(T, I, Z, N, std::false_type());
+        };
+        if (p.normalize) norm(std::true_type());
+        else norm(std::false_type());
       };
       if (z) out(std::true_type());
       else out(std::false_type());
@@ -483,32 +634,33 @@ template <typename F> hipError_t with(bool bf16, bool i, bool z, bool full, F f)
 
 void glr_plan(GlrParams& p, bool packed) {
   const int64_t blocks = blocks_of(p), ntok = p.map.ntok;
-  constexpr int64_t fill = 512;   // workgroups that fill the card
-  int64_t want = max((int64_t)1, fill / blocks);
+  constexpr int64_t tile = kTile;
+  constexpr int64_t fill = 256;   // workgroups that fill the card
+  const int64_t want = max((int64_t)1, fill / blocks);
   p.apart = 0;
   if (!packed && p.map.nseq >= want) {   // whole sequences
-    const int64_t T = max(p.map.T, (int64_t)1), each = max(p.map.nseq / want, (kGlrTile + T - 1) / T);
+    const int64_t T = max(p.map.T, (int64_t)1), each = max(p.map.nseq / want, (tile + T - 1) / T);
     p.L = each * p.map.T;
     p.apart = 1;
   } else {
-    want = min(want, (ntok + kGlrTile - 1) / kGlrTile);
-    p.L = ((ntok + max(want, (int64_t)1) - 1) / max(want, (int64_t)1) + kGlrTile - 1) / kGlrTile * kGlrTile;
+    const int64_t n = max((int64_t)1, min(want, (ntok + tile - 1) / tile));
+    p.L = ((ntok + n - 1) / n + tile - 1) / tile * tile;
   }
-  if (p.L < 1) p.L = kGlrTile;
+  if (p.L < 1) p.L = tile;
   const int64_t n = (ntok + p.L - 1) / p.L;
   p.nchunk = (int32_t)n;
-  p.tiles = (int32_t)((p.L + kGlrTile - 1) / kGlrTile);
+  p.tiles = (int32_t)((p.L + tile - 1) / tile);
   if (n <= 1) p.apart = 1;
 }
 
-int64_t glr_decode_wgs(const GlrParams& p) { return ((p.D + kV - 1) / kV * p.map.nseq + kThreads - 1) / kThreads; }
+int64_t glr_decode_wgs(const GlrParams& p) { return ((p.D + kDecV - 1) / kDecV * p.map.nseq + kThreads - 1) / kThreads; }
 
 hipError_t launch_glr_forward(const GlrParams& p, bool bf16, bool save, bool outputs, hipStream_t stream) {
   const uint32_t blocks = blocks_of(p), main = blocks * p.nchunk;
   hipError_t e = hipSuccess;
   if (!p.apart) {
-    e = with(bf16, p.i, false, p.D % kV == 0, [&](auto T, auto I, auto Z, auto F) {
-      hipLaunchKernelGGL((glr_fwd_kernel<decltype(T), I.value, Z.value, true, F.value>), dim3(main), dim3(kGlrThreads), 0, stream, p,
+    e = with(p, bf16, p.i, false, p.D >= kV, [&](auto T, auto I, auto Z, auto N, auto F) {
+      hipLaunchKernelGGL((glr_fwd_kernel<decltype(T), I.value, Z.value, N.value, true, F.value>), dim3(main), dim3(kGlrThreads), 0, stream, p,
                          blocks, 0);
     });
     if (e != hipSuccess) return e;
@@ -516,8 +668,8 @@ hipError_t launch_glr_forward(const GlrParams& p, bool bf16, bool save, bool out
   GlrParams q = p;
   if (!outputs) q.o = nullptr, q.hfin = nullptr;
   const uint32_t extra = p.map.seq && q.hfin ? kGlrEmptyWgs : 0;
-  return with(bf16, p.i, p.z && outputs, p.D % kV == 0, [&](auto T, auto I, auto Z, auto F) {
-    hipLaunchKernelGGL((glr_fwd_kernel<decltype(T), I.value, Z.value, false, F.value>), dim3(main + extra), dim3(kGlrThreads), 0,
+  return with(p, bf16, p.i, p.z && outputs, p.D >= kV, [&](auto T, auto I, auto Z, auto N, auto F) {
+    hipLaunchKernelGGL((glr_fwd_kernel<decltype(T), I.value, Z.value, N.value, false, F.value>), dim3(main + extra), dim3(kGlrThreads), 0,
                        stream, q, blocks, save ? 1 : 0);
   });
 }
@@ -525,22 +677,22 @@ hipError_t launch_glr_forward(const GlrParams& p, bool bf16, bool save, bool out
 hipError_t launch_glr_backward(const GlrParams& p, bool bf16, hipStream_t stream) {
   const uint32_t blocks = blocks_of(p), main = blocks * p.nchunk, extra = p.map.seq && p.dh0 ? kGlrEmptyWgs : 0;
   if (!p.apart) {
-    const hipError_t e = with(bf16, p.i, p.z, p.D % kV == 0, [&](auto T, auto I, auto Z, auto F) {
-      hipLaunchKernelGGL((glr_bwd_kernel<decltype(T), I.value, Z.value, true, F.value>), dim3(main), dim3(kGlrThreads), 0, stream, p,
+    const hipError_t e = with(p, bf16, p.i, p.z, p.D >= kV, [&](auto T, auto I, auto Z, auto N, auto F) {
+      hipLaunchKernelGGL((glr_bwd_kernel<decltype(T), I.value, Z.value, N.value, true, F.value>), dim3(main), dim3(kGlrThreads), 0, stream, p,
                          blocks);
     });
     if (e != hipSuccess) return e;
   }
-  return with(bf16, p.i, p.z, p.D % kV == 0, [&](auto T, auto I, auto Z, auto F) {
-    hipLaunchKernelGGL((glr_bwd_kernel<decltype(T), I.value, Z.value, false, F.value>), dim3(main + extra), dim3(kGlrThreads), 0,
+  return with(p, bf16, p.i, p.z, p.D >= kV, [&](auto T, auto I, auto Z, auto N, auto F) {
+    hipLaunchKernelGGL((glr_bwd_kernel<decltype(T), I.value, Z.value, N.value, false, F.value>), dim3(main + extra), dim3(kGlrThreads), 0,
                        stream, p, blocks);
   });
 }
 
 hipError_t launch_glr_decode(const GlrParams& p, bool bf16, hipStream_t stream) {
-  const uint32_t pieces = (uint32_t)((p.D + kV - 1) / kV), count = pieces * (uint32_t)p.map.nseq;
-  return with(bf16, p.i, p.z, p.D % kV == 0, [&](auto T, auto I, auto Z, auto F) {
-    hipLaunchKernelGGL((glr_decode_kernel<decltype(T), I.value, Z.value, F.value>), dim3((count + kThreads - 1) / kThreads),
+  const uint32_t pieces = (uint32_t)((p.D + kDecV - 1) / kDecV), count = pieces * (uint32_t)p.map.nseq;
+  return with(p, bf16, p.i, p.z, p.D % kDecV == 0, [&](auto T, auto I, auto Z, auto N, auto F) {
+    hipLaunchKernelGGL((glr_decode_kernel<decltype(T), I.value, Z.value, N.value, F.value>), dim3((count + kThreads - 1) / kThreads),
                        dim3(kThreads), 0, stream, p, pieces, count);
   });
 }

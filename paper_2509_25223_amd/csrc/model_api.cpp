@@ -184,14 +184,14 @@ rla_status check_glr(const rla_glr_problem* q, GlrParams& p) {
   if (!is_type(q->dtype)) return RLA_ERR_DTYPE;
   const rla_status st = tokens(q->batch, q->seq_len, q->num_seqs, q->cu_seqlens, p.map);
   if (st != RLA_OK) return st;
-  if (q->channels < 1 || q->channels > (1 << 24)) return RLA_ERR_SHAPE;
+  if (q->channels < 1 || q->channels >= (1 << 23)) return RLA_ERR_SHAPE;
   if (q->normalize != 0 && q->normalize != 1) return RLA_ERR_VALUE;
   p.D = q->channels;
   if (!stride(q->x_stride, p.D, p.xs) || !stride(q->r_stride, p.D, p.rs) || !stride(q->i_stride, p.D, p.is) ||
       !stride(q->z_stride, p.D, p.zs) || !stride(q->do_stride, p.D, p.dos))
     return RLA_ERR_SHAPE;
-  for (int64_t s : {p.xs, p.rs, p.is, p.zs, p.dos})
-    if (times(times(p.map.ntok, s), 4) < 0) return RLA_ERR_SHAPE;
+  for (int64_t s : {p.xs, p.rs, p.is, p.zs, p.dos})   // (a tile's rows: 32-bit offsets of bytes)
+    if (s >= (1 << 23) || times(times(p.map.ntok, s), 4) < 0) return RLA_ERR_SHAPE;
   if (times(times(p.map.nseq, p.D), 4) < 0) return RLA_ERR_SHAPE;
   p.normalize = q->normalize;
   return RLA_OK;

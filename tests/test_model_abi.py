@@ -127,9 +127,9 @@ def test_glr(lib):
         return lib.rla_glr_decode(p, FAKE, FAKE, FAKE, None, None, h, o, out, None)
 
     assert fwd(None) == NULL
-    for bad, want in [(dict(channels=0), SHAPE), (dict(channels=(1 << 24) + 1), SHAPE), (dict(batch=-1), SHAPE),
+    for bad, want in [(dict(channels=0), SHAPE), (dict(channels=1 << 23), SHAPE), (dict(batch=-1), SHAPE),
                       (dict(seq_len=1 << 33), SHAPE), (dict(dtype=-1), DTYPE), (dict(normalize=2), VALUE),
-                      (dict(x_stride=8), SHAPE), (dict(z_stride=-24), SHAPE), (dict(do_stride=1 << 61), SHAPE),
+                      (dict(x_stride=8), SHAPE), (dict(z_stride=-24), SHAPE), (dict(do_stride=1 << 61), SHAPE), (dict(r_stride=1 << 23), SHAPE),
                       (dict(cu_seqlens=FAKE), SHAPE), (dict(batch=1, cu_seqlens=FAKE, num_seqs=-1), SHAPE)]:
         assert fwd(make(**bad)) == want, bad
         assert rla.rla_glr_workspace_size(make(**bad), rla.RLA_GLR_BACKWARD) == 0
