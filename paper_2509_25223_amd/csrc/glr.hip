@@ -19,6 +19,8 @@
 // starts, the state is its own, whatever came before (never a factor 0: NaN and
 // infinities of a sequence stay there).  Few channels: the tokens are cut into chunks, and a pass
 // before leaves each chunk's pair.
+#include <math.h>
+
 #include "model.hpp"
 
 namespace rla {
@@ -48,16 +50,16 @@ __device__ __forceinline__ Step join(const Step& a, const Step& b) {
   return Step{fminf(a.P, b.P) < 0.f ? -1.f : both, apply(b, a.S)};
 }
 
-// e^l and 1 - e^2l for l = ln 2 y <= 0: near 0 by the series (to y = -0.18, l = -1/8, off by less
-// than a rounding), else as it stands (3.5 roundings of e^2l there)
+// e^l and m = sqrt(1 - e^2l) for l = ln 2 y <= 0: near 0 by the series (to y = -0.18, l = -1/8, off by
+// less than a rounding), else as it stands (3.5 roundings of e^2l there)
 constexpr float series(int n) {   // (2 ln 2)^n / n!
   double v = 1;
   for (int i = 1; i <= n; ++i) v *= 2 * 0.69314718055994530942 / i;
   return (float)v;
 }
-template <bool NORM> __device__ __forceinline__ void decay(float y, float& a, float& w) {
+template <bool NORM> __device__ __forceinline__ void decay(float y, float& a, float& m) {
   a = __builtin_amdgcn_exp2f(y);
-  w = 1.f;
+  m = 1.f;
   if (NORM) {
     float p = series(6);
     p = __builtin_fmaf(p, y, series(5));
@@ -68,7 +70,7 @@ template <bool NORM> __device__ __forceinline__ void decay(float y, float& a, fl
     float far = __builtin_fmaf(-a, a, 1.f);
     // (both computed, one selected: the compiler would branch around the series, value by value)
     asm volatile("" : "+v"(p), "+v"(far));
-    w = y > -0.18f ? p : far;
+    m = __builtin_amdgcn_sqrtf(y > -0.18f ? p : far);
   }
 }
 
@@ -98,13 +100,23 @@ template <bool WHOLE> struct Channels {
   }
 };
 
-// What a workgroup works on; blocks of channels vary fastest over the workgroups.
+// Workgroups are dealt to the 8 XCDs in turn.  Each takes adjacent blocks of channels: the lines of a row
+// lie in all channels of its L2, where every eighth block's would share two of them (16384 x 2048: the
+// forward %s).
+constexpr uint32_t kXcds = 8;
+__device__ __forceinline__ uint32_t work_of(uint32_t wg, uint32_t count) {
+  const uint32_t xcd = wg % kXcds, each = count / kXcds, more = count % kXcds;
+  return xcd * each + min(xcd, more) + wg / kXcds;
+}
+
+// What a workgroup works on; blocks of channels vary fastest.
 template <bool WHOLE> struct Work {
   uint32_t chunk;
   Channels<WHOLE> ch;
   int64_t t0, end, channel;   // (channel: the lane's own, of the states that waves carry)
   bool owner;                 // the first wave's lanes write what there is one of per channel
-  __device__ __forceinline__ Work(const GlrParams& p, uint32_t blocks) : chunk(blockIdx.x / blocks), ch(p.D, blockIdx.x - chunk * blocks) {
+  __device__ __forceinline__ Work(const GlrParams& p, uint32_t blocks) : Work(p, blocks, work_of(blockIdx.x, blocks * p.nchunk)) {}
+  __device__ __forceinline__ Work(const GlrParams& p, uint32_t blocks, uint32_t id) : chunk(id / blocks), ch(p.D, id - chunk * blocks) {
     t0 = chunk * p.L;
     end = min(t0 + p.L, p.map.ntok);
     channel = ch.c + (threadIdx.x & 63) / kLanes;
@@ -138,9 +150,13 @@ template <typename T> struct Rows {
     load_raw<T, kV, WHOLE>(reinterpret_cast<const T*>(at), left, x);
   }
   __device__ __forceinline__ float at(int k, int e) const { return to_f<T>(v[k][e]); }
-  __device__ __forceinline__ void clear(int k) {
+  // rows of tokens that `in` does not have
+  __device__ __forceinline__ void put(uint32_t in, float x) {
 #pragma unroll
-    for (int e = 0; e < kV; ++e) v[k][e] = from_f<T>(0.f);
+    for (int k = 0; k < kTok; ++k)
+      if (!((in >> k) & 1u))
+#pragma unroll
+        for (int e = 0; e < kV; ++e) v[k][e] = from_f<T>(x);
   }
 };
 // ... written, of a tensor with rows next to each other
@@ -310,20 +326,32 @@ __global__ __launch_bounds__(kGlrThreads) void glr_fwd_kernel(GlrParams p, uint3
   for (int e = 0; e < kV; ++e) A[e] *= kLog2e;
   float carry = SUMMARY ? 0.f : chunk_state<true>(p, (int)w.chunk, w.channel);
   Step pair{1.f, 0.f};
-  Rows<T> x, r, i, z;
+  // the next tile's rows are on their way while this one's are worked on
+  Rows<T> x, r, i, z, x1, r1, i1;
   auto load = [&](int64_t tile) {
-    x.load(p.x, p.xs, tile, w);
-    r.load(p.r, p.rs, tile, w);
-    if (HAS_I) i.load(p.i, p.is, tile, w);
+    r1.load(p.r, p.rs, tile, w);
+    x1.load(p.x, p.xs, tile, w);
+    if (HAS_I) i1.load(p.i, p.is, tile, w);
   };
   load(w.t0);
   const int tiles = w.tiles();
   for (int n = 0; n < tiles; ++n) {
     const int64_t tile = w.t0 + (int64_t)n * kTile;
     const bool plain = plain_tile(p, tile, w.end);
+    r = r1;
+    x = x1;
+    if (HAS_I) i = i1;
+    // (in this order: loads complete in the order of their issue)
     if (HAS_Z && !SUMMARY) z.load(p.z, p.zs, tile, w);
+    if (n + 1 < tiles) load(tile + kTile);
     if (save && !SUMMARY && w.owner) p.ck[((int64_t)w.chunk * p.tiles + n) * p.D + w.channel] = carry;
     const Place q(p, tile + threadIdx.x / kLanes * kTok, w.end, plain);
+    if (!plain) {   // tokens of no sequence: a = 1 and zeros
+      r.put(q.in, -INFINITY);
+      x.put(q.in, 0.f);
+      if (HAS_I) i.put(q.in, 0.f);
+      if (HAS_Z && !SUMMARY) z.put(q.in, 0.f);
+    }
     float a[kTok][kV], b[kTok][kV], h[kV];
     Step own[kV], before[kV];
 #pragma unroll
@@ -332,20 +360,9 @@ __global__ __launch_bounds__(kGlrThreads) void glr_fwd_kernel(GlrParams p, uint3
       for (int e = 0; e < kV; ++e) {
         float m;
         decay<NORM>(A[e] * sigmoid_fast(r.at(k, e)), a[k][e], m);
-        b[k][e] = x.at(k, e);
-        if (NORM) b[k][e] *= __builtin_amdgcn_sqrtf(fmaxf(m, 0.f));
+        b[k][e] = m * x.at(k, e);
         if (HAS_I) b[k][e] *= sigmoid_fast(i.at(k, e));
       }
-    if (n + 1 < tiles) load(tile + kTile);
-    if (!plain) {   // tokens of no sequence: nothing happens, and zeros come out
-#pragma unroll
-      for (int k = 0; k < kTok; ++k) {
-        if ((q.in >> k) & 1u) continue;
-        if (HAS_Z && !SUMMARY) z.clear(k);
-#pragma unroll
-        for (int e = 0; e < kV; ++e) a[k][e] = 1.f, b[k][e] = 0.f;
-      }
-    }
     if (plain) stretch_forward<true>(p, q, w.ch, a, b, own);
     else stretch_forward<false>(p, q, w.ch, a, b, own);
     wave_steps<true>(own, lds.wave[n & 1][threadIdx.x >> 6], before);
@@ -377,6 +394,8 @@ __global__ __launch_bounds__(kGlrThreads) void glr_fwd_kernel(GlrParams p, uint3
   if (SUMMARY && w.owner) write_pair(p, w.chunk, w.channel, pair);
 }
 
+// Computed here, not moved behind what follows.
+__device__ __forceinline__ void here(float& x) { asm volatile("" : "+v"(x)); }
 // Every second token: keeps the scheduler from taking the tokens' independent chains all at once,
 // for which there are not registers enough.
 __device__ __forceinline__ void few_registers(int k) {
@@ -418,7 +437,14 @@ __global__ __launch_bounds__(kGlrThreads) __attribute__((amdgpu_waves_per_eu(2, 
       if (w.channel < p.D) state = p.ck[((int64_t)w.chunk * p.tiles + n) * p.D + w.channel];
     }
     const Place q(p, tile + threadIdx.x / kLanes * kTok, w.end, plain);
-    // m: 1 - a^2; slope: dO SiLU'(z)
+    if (!plain) {   // tokens of no sequence: a = 1 and zeros
+      r.put(q.in, -INFINITY);
+      d.put(q.in, 0.f);
+      if (HAS_Z) z.put(q.in, 0.f);
+      if (!SUMMARY) x.put(q.in, 0.f);
+      if (HAS_I && !SUMMARY) i.put(q.in, 0.f);
+    }
+    // slope: dO SiLU'(z)
     float a[kTok][kV], m[kTok][kV], sr[kTok][kV], si[kTok][kV], g[kTok][kV], slope[kTok][kV], h[kV], u[kV];
     Step own[kV], before[kV], behind[kV];
 #pragma unroll
@@ -435,20 +461,13 @@ __global__ __launch_bounds__(kGlrThreads) __attribute__((amdgpu_waves_per_eu(2, 
           float silu;
           slope[k][e] = silu_grad_f(z.at(k, e), silu) * g[k][e];
           g[k][e] *= silu;
+          here(slope[k][e]);
         }
-      }
-    }
-    if (!plain) {   // tokens of no sequence: nothing happens, and zeros come out
-#pragma unroll
-      for (int k = 0; k < kTok; ++k) {
-        if ((q.in >> k) & 1u) continue;
-        if (!SUMMARY) x.clear(k);
-#pragma unroll
-        for (int e = 0; e < kV; ++e) {
-          a[k][e] = m[k][e] = 1.f;
-          g[k][e] = sr[k][e] = si[k][e] = 0.f;
-          if (HAS_Z) slope[k][e] = 0.f;
-        }
+        here(a[k][e]);
+        here(m[k][e]);
+        here(sr[k][e]);
+        here(g[k][e]);
+        if (HAS_I && !SUMMARY) here(si[k][e]);
       }
     }
     if (n > 0) load(tile - kTile);
@@ -483,8 +502,7 @@ __global__ __launch_bounds__(kGlrThreads) __attribute__((amdgpu_waves_per_eu(2, 
       for (int k = 0; k < kTok; ++k)
 #pragma unroll
         for (int e = 0; e < kV; ++e) {
-          b[k][e] = si[k][e] * x.at(k, e);
-          if (NORM) b[k][e] *= __builtin_amdgcn_sqrtf(fmaxf(m[k][e], 0.f));
+          b[k][e] = m[k][e] * si[k][e] * x.at(k, e);
         }
       if (plain) stretch_forward<true>(p, q, w.ch, a, b, own);
       else stretch_forward<false>(p, q, w.ch, a, b, own);
@@ -505,8 +523,7 @@ __global__ __launch_bounds__(kGlrThreads) __attribute__((amdgpu_waves_per_eu(2, 
         float dz[kV];
 #pragma unroll
         for (int e = 0; e < kV; ++e) {
-          float b = si[k][e] * x.at(k, e);
-          if (NORM) b *= __builtin_amdgcn_sqrtf(fmaxf(m[k][e], 0.f));
+          const float b = m[k][e] * si[k][e] * x.at(k, e);
           prev[k][e] = h[e];
           h[e] = __builtin_fmaf(a[k][e], h[e], b);
           if (HAS_Z) dz[e] = slope[k][e] * h[e];
@@ -524,11 +541,11 @@ __global__ __launch_bounds__(kGlrThreads) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
         for (int e = 0; e < kV; ++e) {
           const float l = g[k][e] + u[e];
-          float into = l * si[k][e], dlog = prev[k][e];
-          if (NORM) {   // m is the root of 1 - a^2, `over` its inverse
-            const float one = fmaxf(m[k][e], 0.f), over = one > 0.f ? __builtin_amdgcn_rsqf(one) : 0.f;
+          const float into = l * m[k][e] * si[k][e];
+          float dlog = prev[k][e];
+          if (NORM) {
+            const float over = m[k][e] > 0.f ? __builtin_amdgcn_rcpf(m[k][e]) : 0.f;
             dlog = __builtin_fmaf(-(si[k][e] * x.at(k, e)), a[k][e] * over, dlog);
-            into *= one * over;
           }
           u[e] = a[k][e] * l;
           dlog *= u[e] * sr[k][e];
@@ -591,9 +608,9 @@ __global__ __launch_bounds__(kThreads) void glr_decode_kernel(GlrParams p, uint3
     if (HAS_Z) load_piece<T, kDecV, FULL>(reinterpret_cast<const T*>(p.z) + t * p.zs + c, left, z);
 #pragma unroll
     for (int e = 0; e < kDecV; ++e) {
-      float a, m, b = x[e];
+      float a, m;
       decay<NORM>(A[e] * kLog2e * sigmoid_fast(r[e]), a, m);
-      if (NORM) b *= __builtin_amdgcn_sqrtf(fmaxf(m, 0.f));
+      float b = m * x[e];
       if (HAS_I) b *= sigmoid_fast(i[e]);
       h[e] = __builtin_fmaf(a, h[e], b);
       x[e] = HAS_Z ? h[e] * (z[e] * sigmoid_fast(z[e])) : h[e];
