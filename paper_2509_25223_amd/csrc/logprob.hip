@@ -10,11 +10,11 @@
 // value, sums and alternatives, which logprob_join merges.
 //
 // Alternatives: values are compared as whole numbers in their order (0: none, -inf or NaN).
-// Of 64 lanes' largest values the `top`-th is a bound that at least `top` values of
-// the row reach; values from the bound on are collected in LDS and ranked by
-// counting, (value, place) being different for each.  Where more reach the bound than LDS
-// has room for (equal or neighbouring large logits), it is raised by bisection until exactly
-// `top` do.
+// Of a wave's 64 lanes' largest values the q-th is a bound that q values of the wave reach (its upper
+// 16 bits are enough), and the r-th of the waves' bounds one that q r >= `top` values of the row do; values from the bound on are collected in LDS, where a
+// piece's largest says that it has any, and ranked by counting, (value, place) being different
+// for each.  Where more reach the bound than LDS has room for (equal or neighbouring large
+// logits), it is raised by bisection until exactly `top` do.
 #include "model.hpp"
 
 namespace rla {
@@ -33,9 +33,12 @@ __device__ __forceinline__ float from_order_key(uint32_t k) {
 }
 
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
+  v = fmaxf(v, dpp<0xB1>(v));
+  v = fmaxf(v, dpp<0x4E>(v));
+  v = fmaxf(v, dpp<0x141>(v));
+  v = fmaxf(v, dpp<0x140>(v));
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
 }
 __device__ __forceinline__ float wave_sum(float v) {
   v = group_sum<16>(v);
@@ -43,16 +46,7 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v + __shfl_xor(v, 32);
 }
 
-// Over the L lanes of a row (64, or the workgroup); `slot`: LDS of its own for each use
-// between two barriers.
-template <int L, typename Op> __device__ __forceinline__ float over_waves(float v, float (&slot)[kWaves], Op op) {
-  if constexpr (L > 64) {
-    if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = op(op(slot[0], slot[1]), op(slot[2], slot[3]));
-  }
-  return v;
-}
+// Barrier of a row's L lanes (64, or the workgroup).
 template <int L> __device__ __forceinline__ void row_barrier() {
   if constexpr (L > 64) {
     __syncthreads();
@@ -61,14 +55,24 @@ template <int L> __device__ __forceinline__ void row_barrier() {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
 }
+template <int N, typename Op> __device__ __forceinline__ float over(const float (&x)[N], Op op) {
+  float v = x[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) v = op(v, x[i]);
+  return v;
+}
+struct Max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
+struct Add { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
 
-// The `want`-th largest of the 64 lanes' keys, or 0 if fewer are not 0.
-__device__ __forceinline__ uint32_t kth_of_lanes(uint32_t key, int want) {
+// A bound, in the upper 16 bits of a key, that `want` of the 64 lanes' keys reach; 0 if fewer are
+// not 0.
+__device__ __forceinline__ uint32_t bound_of_lanes(uint32_t key, int want) {
   uint32_t t = 0;
-  for (uint32_t bit = 0x80000000u; bit; bit >>= 1)
+  for (uint32_t bit = 0x80000000u; bit > 0xffffu; bit >>= 1)
     if (__popcll(__ballot(key >= (t | bit))) >= want) t |= bit;
   return t;
 }
+constexpr uint32_t kLowestKey = 0x00800000u;   // of the lowest finite value
 
 struct Candidate {
   uint32_t key;
@@ -77,8 +81,8 @@ struct Candidate {
 template <int L> constexpr int kRoom = L > 64 ? 256 : 128;
 
 template <int L> struct TopLds {
-  uint32_t bound[kWaves];
-  int32_t count, sums[2][kWaves];
+  uint32_t bound[L / 64];
+  int32_t count, sums[2][L / 64];
   Candidate list[kRoom<L>];
 };
 
@@ -89,58 +93,53 @@ template <int L> __device__ __forceinline__ int row_count(int c, TopLds<L>& s, i
   if constexpr (L > 64) {
     if ((threadIdx.x & 63) == 0) s.sums[turn & 1][threadIdx.x >> 6] = c;
     __syncthreads();
-    c = s.sums[turn & 1][0] + s.sums[turn & 1][1] + s.sums[turn & 1][2] + s.sums[turn & 1][3];
+    c = 0;
+#pragma unroll
+    for (int w = 0; w < L / 64; ++w) c += s.sums[turn & 1][w];
   }
   return c;
 }
+template <int L> __device__ __forceinline__ void collect(TopLds<L>& s, uint32_t key, int at) {
+  const int j = atomicAdd(&s.count, 1);
+  if (j < kRoom<L>) s.list[j] = Candidate{key, at};
+}
 
-// The largest `want` of the values that for_each(f) hands to f(key, place), place by place the same
-// each time; out(rank, key, place) for each.  A row's L lanes call it together.
-template <int L, typename Each, typename Out>
-__device__ __forceinline__ void select_top(int want, TopLds<L>& s, Each for_each, Out out) {
-  const int lane = threadIdx.x & 63, w = L > 64 ? threadIdx.x >> 6 : 0;
-  uint32_t best = 0;
-  for_each([&](uint32_t k, int) { best = max(best, k); });
-  uint32_t bound = kth_of_lanes(best, want);
-  if (lane == 0) s.bound[w] = bound;
-  if (threadIdx.x % L == 0) s.count = 0;
-  row_barrier<L>();
-  if constexpr (L > 64) bound = max(max(s.bound[0], s.bound[1]), max(s.bound[2], s.bound[3]));
-  bound = max(bound, 1u);
+// More than fit were collected: the largest bound that `want` values reach, of the values equal to
+// it those up to the place that leaves `want`, collected anew.  for_each(f) hands all of the lane's
+// (key, place) to f.
+template <int L, typename Each> __device__ __forceinline__ void collect_exactly(int want, TopLds<L>& s, Each for_each) {
   int turn = 0;
   auto reach = [&](uint32_t t) {
     int c = 0;
     for_each([&](uint32_t k, int) { c += k >= t ? 1 : 0; });
     return row_count<L>(c, s, turn++);
   };
-  int32_t last = 0x7fffffff;   // of the values equal to the bound, those up to this place
-  if (reach(bound) > kRoom<L>) {
-    // the largest bound that `want` values reach, then the place that leaves `want`
-    uint32_t t = 0;
-    for (uint32_t bit = 0x80000000u; bit; bit >>= 1)
-      if (reach(t | bit) >= want) t |= bit;
-    bound = t;
-    const int above = t == 0xffffffffu ? 0 : reach(t + 1);
-    int32_t place = 0;   // fewer than want - above equal values lie before it
-    for (int32_t bit = 1 << 30; bit; bit >>= 1) {
-      int c = 0;
-      const int32_t upto = place | bit;
-      for_each([&](uint32_t k, int at) { c += k == t && at < upto ? 1 : 0; });
-      if (row_count<L>(c, s, turn++) < want - above) place = upto;
-    }
-    last = place;
+  uint32_t t = 0;
+  for (uint32_t bit = 0x80000000u; bit; bit >>= 1)
+    if (reach(t | bit) >= want) t |= bit;
+  const int above = t == 0xffffffffu ? 0 : reach(t + 1);
+  int32_t last = 0;   // fewer than want - above equal values lie before it
+  for (int32_t bit = 1 << 30; bit; bit >>= 1) {
+    int c = 0;
+    const int32_t upto = last | bit;
+    for_each([&](uint32_t k, int at) { c += k == t && at < upto ? 1 : 0; });
+    if (row_count<L>(c, s, turn++) < want - above) last = upto;
   }
+  if (threadIdx.x % L == 0) s.count = 0;
+  row_barrier<L>();
   for_each([&](uint32_t k, int at) {
-    if (k > bound || (k == bound && at <= last)) {
-      const int j = atomicAdd(&s.count, 1);
-      s.list[j] = Candidate{k, at};
-    }
+    if (k > t || (k == t && at <= last)) collect(s, k, at);
   });
   row_barrier<L>();
+}
+
+// out(rank, key, place) of the collected ones' largest `want` (key 0, place -1 past the last).
+template <int L, typename Out> __device__ __forceinline__ void rank_collected(int want, const TopLds<L>& s, Out out) {
   const int count = s.count;
   for (int j = threadIdx.x % L; j < count; j += L) {
     const Candidate own = s.list[j];
     int rank = 0;
+#pragma unroll 8
     for (int i = 0; i < count; ++i) {
       const Candidate c = s.list[i];
       rank += c.key > own.key || (c.key == own.key && c.at < own.at) ? 1 : 0;
@@ -163,50 +162,109 @@ struct RowResult {
   __device__ __forceinline__ float entropy(float s, float e) const { return none ? 0.f : ln - kLn2 * (e / s); }
 };
 
+// The lane's values of a part, as stored: N pieces of V, piece j of lane l from column (j L + l) V on,
+// -inf past its end.
+template <typename T, int L, int N> struct Part {
+  static constexpr int V = kPiece<T>;
+  typedef typename RowVec<T, V>::type Vec;
+  Vec raw[N];
+  __device__ __forceinline__ static int col(int j, int lane) { return (j * L + lane) * V; }
+  // Whole pieces without branches, so that all are in flight at once (past the end the last
+  // one again), then what is not whole.
+  __device__ __forceinline__ void load(const T* x, int width, int lane) {
+    if (width >= V)
+#pragma unroll
+      for (int j = 0; j < N; ++j) raw[j] = *reinterpret_cast<const Vec*>(x + min(col(j, lane), width - V));
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if (width >= (j + 1) * L * V) continue;
+      const int c = col(j, lane), left = width - c;
+      if (left >= V) continue;
+#pragma unroll
+      for (int e = 0; e < V; ++e) raw[j][e] = e < left ? x[c + e] : from_f<T>(-kInf);
+    }
+  }
+  // Values are converted anew in each pass over them: kept, they would take twice the registers.
+  __device__ __forceinline__ void again() {
+    typedef uint32_t Words __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      Words w = __builtin_bit_cast(Words, raw[j]);
+      asm volatile("" : "+v"(w));
+      raw[j] = __builtin_bit_cast(Vec, w);
+    }
+  }
+  template <typename F> __device__ __forceinline__ void each(F f) {
+    again();
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int e = 0; e < V; ++e) f(j, e, to_f<T>(raw[j][e]));
+  }
+};
+
+// The logit of a row's token (`there`: it has one).
+template <typename T> __device__ __forceinline__ float given_logit(const LogprobParams& p, int64_t row, bool& there) {
+  const int64_t y = p.targets[row];
+  there = y >= 0 && y < p.V;
+  return there ? to_f<T>(reinterpret_cast<const T*>(p.x)[row * p.xs + y]) : 0.f;
+}
 // What one lane writes of a row.
-template <typename T>
-__device__ __forceinline__ void write_row(const LogprobParams& p, int64_t row, const RowResult& r, float s, float e) {
+__device__ __forceinline__ void write_row(const LogprobParams& p, int64_t row, const RowResult& r, float s, float e, float given,
+                                          bool there) {
   if (p.lse) p.lse[row] = r.lse();
   if (p.entropy) p.entropy[row] = r.entropy(s, e);
-  if (p.logprob) {
-    const int64_t y = p.targets[row];
-    p.logprob[row] = y >= 0 && y < p.V ? r.of(to_f<T>(reinterpret_cast<const T*>(p.x)[row * p.xs + y])) : 0.f;
-  }
+  if (p.logprob) p.logprob[row] = there ? r.of(given) : 0.f;
 }
 
 // ---------------------------------------------------------------------------
 // L lanes a part of a row, N pieces a lane.  Part: row / part = id / p.parts, id % p.parts.
 // ---------------------------------------------------------------------------
 template <typename T, int L, int N, bool TOP>
-__global__ __launch_bounds__(kThreads) void logprob_fwd_kernel(LogprobParams p, int64_t first) {
-  constexpr int V = kPiece<T>, kSub = kThreads / L;
-  __shared__ float slots[3][kWaves];
-  __shared__ TopLds<L> top[TOP ? kSub : 1];
+__global__ __launch_bounds__(L > kThreads ? L : kThreads) void logprob_fwd_kernel(LogprobParams p, int64_t first) {
+  constexpr int V = kPiece<T>, kSub = L > kThreads ? 1 : kThreads / L, W = L / 64;
+  __shared__ float slots[3][kSub][W];
+  __shared__ TopLds<L> tops[TOP ? kSub : 1];
+  const int sub = L > 64 ? 0 : threadIdx.x / L, w = L > 64 ? threadIdx.x >> 6 : 0, lane = threadIdx.x % L;
   const int64_t id = first + (int64_t)blockIdx.x * kSub + threadIdx.x / L;
   if (id >= p.n * p.parts) return;   // (whole rows of lanes)
-  const int64_t row = id / p.parts, part = id - row * p.parts;
+  TopLds<L>& top = tops[TOP ? sub : 0];
+  const int64_t row = p.parts == 1 ? id : id / p.parts, part = id - row * p.parts;
   const int64_t c0 = part * p.width;
-  const int width = (int)min(p.width, p.V - c0);
+  const int width = (int)min(p.width, p.V - c0), want = TOP ? min(p.top, width) : 0;
   const T* x = reinterpret_cast<const T*>(p.x) + row * p.xs + c0;
-  const int lane = threadIdx.x % L;
 
-  typename RowVec<T, V>::type raw[N];
+  Part<T, L, N> v;
+  v.load(x, width, lane);
+  float given = 0.f;
+  bool there = false;
+  if (p.logprob && p.parts == 1 && lane == 0) given = given_logit<T>(p, row, there);
+
+  // the largest value, of each piece and of all
+  float big[N], mx = -kInf;
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    const int c = (j * L + lane) * V, left = width - c;
-    if (left >= V) {
-      raw[j] = *reinterpret_cast<const typename RowVec<T, V>::type*>(x + c);
-    } else {
+    big[j] = to_f<T>(v.raw[j][0]);
 #pragma unroll
-      for (int e = 0; e < V; ++e) raw[j][e] = e < left ? x[c + e] : from_f<T>(-kInf);
-    }
+    for (int e = 1; e < V; ++e) big[j] = fmaxf(big[j], to_f<T>(v.raw[j][e]));
+    mx = fmaxf(mx, big[j]);
   }
-  float mx = -kInf;
-#pragma unroll
-  for (int j = 0; j < N; ++j)
-#pragma unroll
-    for (int e = 0; e < V; ++e) mx = fmaxf(mx, to_f<T>(raw[j][e]));
-  mx = over_waves<L>(wave_max(mx), slots[0], [](float a, float b) { return fmaxf(a, b); });
+  uint32_t bound = 0;
+  // (a wave's q-th; the workgroup's: the r-th of its waves', so that r waves have q each)
+  const int q = (want + max(W / 2, 1) - 1) / max(W / 2, 1);
+  if constexpr (TOP) bound = bound_of_lanes(order_key(mx), q);
+  mx = wave_max(mx);
+  if ((threadIdx.x & 63) == 0) {
+    slots[0][sub][w] = mx;
+    if (TOP) top.bound[w] = bound;
+  }
+  if (TOP && lane == 0) top.count = 0;
+  row_barrier<L>();
+  if constexpr (L > 64) {
+    mx = over(slots[0][0], Max());
+    if constexpr (TOP) bound = bound_of_lanes((threadIdx.x & 63) < W ? top.bound[threadIdx.x & 63 & (W - 1)] : 0u, (want + q - 1) / q);
+  }
+
   const float k = p.scale * kLog2e, m0 = mx == -kInf ? 0.f : mx, c = m0 * k;
   float s = 0.f, ent = 0.f;
   auto add = [&](float d) {
@@ -215,44 +273,54 @@ __global__ __launch_bounds__(kThreads) void logprob_fwd_kernel(LogprobParams p, 
     ent = __builtin_fmaf(y, fmaxf(d, -1000.f), ent);   // (0 times -inf)
   };
   if (__builtin_fabsf(c) > 1e30f) {   // c could overflow (a row at the type's lowest value)
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-#pragma unroll
-      for (int e = 0; e < V; ++e) add((to_f<T>(raw[j][e]) - m0) * k);
+    v.each([&](int, int, float z) { add((z - m0) * k); });
   } else if (p.entropy) {
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-#pragma unroll
-      for (int e = 0; e < V; ++e) add(__builtin_fmaf(to_f<T>(raw[j][e]), k, -c));
+    v.each([&](int, int, float z) { add(__builtin_fmaf(z, k, -c)); });
   } else {
+    v.each([&](int, int, float z) { s += __builtin_amdgcn_exp2f(__builtin_fmaf(z, k, -c)); });
+  }
+  if constexpr (TOP) {
+    const float least = from_order_key(max(bound, kLowestKey));
+    v.again();
 #pragma unroll
     for (int j = 0; j < N; ++j)
+      if (big[j] >= least)
 #pragma unroll
-      for (int e = 0; e < V; ++e) s += __builtin_amdgcn_exp2f(__builtin_fmaf(to_f<T>(raw[j][e]), k, -c));
+        for (int e = 0; e < V; ++e) {
+          const float z = to_f<T>(v.raw[j][e]);
+          if (z >= least) collect(top, order_key(z), v.col(j, lane) + e);
+        }
   }
-  if (p.entropy) ent = over_waves<L>(wave_sum(ent), slots[2], [](float a, float b) { return a + b; });
-  s = over_waves<L>(wave_sum(s), slots[1], [](float a, float b) { return a + b; });
+  s = wave_sum(s);
+  if (p.entropy) ent = wave_sum(ent);
+  if constexpr (L > 64) {
+    if ((threadIdx.x & 63) == 0) {
+      slots[1][0][w] = s;
+      slots[2][0][w] = ent;
+    }
+    __syncthreads();
+    s = over(slots[1][0], Add());
+    ent = over(slots[2][0], Add());
+  } else if (TOP) {
+    row_barrier<L>();
+  }
   if (__builtin_fabsf(c) <= 1e30f) {   // the factor 2^(mx k - c) out of the sums
     const float lost = __builtin_fmaf(m0, k, -c), f = __builtin_amdgcn_exp2f(-lost);
     ent = (ent - lost * s) * f;
     s *= f;
   }
   const RowResult r(m0, s, p.scale);
-  if (p.parts == 1) {
-    if (lane == 0) write_row<T>(p, row, r, s, ent);
-  } else if (lane == 0) {
-    *reinterpret_cast<floatx4*>(p.stat + id * 4) = floatx4{mx, s, ent, 0.f};
+  if (lane == 0) {
+    if (p.parts == 1) write_row(p, row, r, s, ent, given, there);
+    else *reinterpret_cast<floatx4*>(p.stat + id * 4) = floatx4{mx, s, ent, 0.f};
   }
   if constexpr (TOP) {
-    auto each = [&](auto&& f) {
-#pragma unroll
-      for (int j = 0; j < N; ++j)
-#pragma unroll
-        for (int e = 0; e < V; ++e) f(order_key(to_f<T>(raw[j][e])), (j * L + lane) * V + e);
-    };
-    const int want = min(p.top, width);
+    if (top.count > kRoom<L>)
+      collect_exactly<L>(want, top, [&](auto&& f) {   // (read again: rare, and registers are few)
+        for (int i = lane; i < width; i += L) f(order_key(to_f<T>(x[i])), i);
+      });
     const int64_t base = id * p.top;
-    select_top<L>(want, top[threadIdx.x / L], each, [&](int rank, uint32_t key, int at) {
+    rank_collected<L>(want, top, [&](int rank, uint32_t key, int at) {
       if (p.parts == 1) {
         p.top_lp[base + rank] = key ? r.of(from_order_key(key)) : r.ln == r.ln ? -kInf : r.ln;
         p.top_ids[base + rank] = key ? at : -1;
@@ -271,7 +339,7 @@ __global__ __launch_bounds__(kThreads) void logprob_fwd_kernel(LogprobParams p, 
 
 // A wave a row: its parts merged.
 template <typename T, bool TOP> __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobParams p) {
-  __shared__ TopLds<64> top[TOP ? kWaves : 1];
+  __shared__ TopLds<64> tops[TOP ? kWaves : 1];
   const int64_t row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
   if (row >= p.n) return;
   const int lane = threadIdx.x & 63;
@@ -289,8 +357,13 @@ template <typename T, bool TOP> __global__ __launch_bounds__(kThreads) void logp
   s = wave_sum(s);
   e = wave_sum(e);
   const RowResult r(m0, s, p.scale);
-  if (lane == 0) write_row<T>(p, row, r, s, e);
+  if (lane == 0) {
+    bool there = false;
+    const float given = p.logprob ? given_logit<T>(p, row, there) : 0.f;
+    write_row(p, row, r, s, e, given, there);
+  }
   if constexpr (TOP) {
+    TopLds<64>& top = tops[threadIdx.x >> 6];
     const int64_t count = p.parts * p.top;
     auto each = [&](auto&& f) {
       for (int64_t j = lane; j < count; j += 64) {
@@ -298,7 +371,17 @@ template <typename T, bool TOP> __global__ __launch_bounds__(kThreads) void logp
         f(at < 0 ? 0u : order_key(p.cand_x[row * count + j]), at);
       }
     };
-    select_top<64>(p.top, top[threadIdx.x >> 6], each, [&](int rank, uint32_t key, int at) {
+    uint32_t best = 0;
+    each([&](uint32_t key, int) { best = max(best, key); });
+    const uint32_t bound = max(bound_of_lanes(best, p.top), kLowestKey);
+    if (lane == 0) top.count = 0;
+    row_barrier<64>();
+    each([&](uint32_t key, int at) {
+      if (key >= bound) collect(top, key, at);
+    });
+    row_barrier<64>();
+    if (top.count > kRoom<64>) collect_exactly<64>(p.top, top, each);
+    rank_collected<64>(p.top, top, [&](int rank, uint32_t key, int at) {
       p.top_lp[row * p.top + rank] = key ? r.of(from_order_key(key)) : r.ln == r.ln ? -kInf : r.ln;
       p.top_ids[row * p.top + rank] = key ? at : -1;
     });
@@ -317,9 +400,19 @@ template <typename T, int L> __device__ __forceinline__ void far_row(const Logpr
   const float k = p.scale * kLog2e;
   float m = -kInf, s = 0.f;
   for (int64_t j = threadIdx.x % L; j < p.V; j += L) m = fmaxf(m, to_f<T>(x[j]));
-  m = over_waves<L>(wave_max(m), slots[0], [](float a, float b) { return fmaxf(a, b); });
+  m = wave_max(m);
+  if constexpr (L > 64) {
+    if ((threadIdx.x & 63) == 0) slots[0][threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = over(slots[0], Max());
+  }
   for (int64_t j = threadIdx.x % L; j < p.V; j += L) s += __builtin_amdgcn_exp2f((to_f<T>(x[j]) - m) * k);
-  s = over_waves<L>(wave_sum(s), slots[1], [](float a, float b) { return a + b; });
+  s = wave_sum(s);
+  if constexpr (L > 64) {
+    if ((threadIdx.x & 63) == 0) slots[1][threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = over(slots[1], Add());
+  }
   mx = m;
   ln = logf(s);
 }
@@ -375,28 +468,35 @@ __global__ __launch_bounds__(kThreads) void logprob_bwd_kernel(LogprobParams p, 
 constexpr int64_t kMaxGrid = (int64_t)1 << 23;   // workgroups a launch
 
 template <typename T, int L, int N> hipError_t forward(const LogprobParams& p, hipStream_t stream) {
-  const int64_t sub = kThreads / L, wgs = (p.n * p.parts + sub - 1) / sub;
+  const int64_t sub = L > kThreads ? 1 : kThreads / L, wgs = (p.n * p.parts + sub - 1) / sub;
+  const dim3 threads(L > kThreads ? L : kThreads);
   for (int64_t w = 0; w < wgs; w += kMaxGrid) {
     const dim3 grid((uint32_t)min(wgs - w, kMaxGrid));
-    if (p.top) hipLaunchKernelGGL((logprob_fwd_kernel<T, L, N, true>), grid, dim3(kThreads), 0, stream, p, w * sub);
-    else hipLaunchKernelGGL((logprob_fwd_kernel<T, L, N, false>), grid, dim3(kThreads), 0, stream, p, w * sub);
+    if (p.top) hipLaunchKernelGGL((logprob_fwd_kernel<T, L, N, true>), grid, threads, 0, stream, p, w * sub);
+    else hipLaunchKernelGGL((logprob_fwd_kernel<T, L, N, false>), grid, threads, 0, stream, p, w * sub);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
-// Values in a lane's registers: 64 at most.
+// The fewest lanes that hold a part in few enough pieces; the most where there are few rows.
+constexpr int64_t kFewRows = 512;
 template <typename T> hipError_t forward(const LogprobParams& p, hipStream_t stream) {
   constexpr int V = kPiece<T>;
   const int64_t pieces = (p.width + V - 1) / V;
+  const bool few = p.n * p.parts <= kFewRows;
   hipError_t e;
   if (pieces <= 64) e = forward<T, 64, 1>(p, stream);
-  else if (pieces <= 128) e = forward<T, 64, 2>(p, stream);
+  else if (pieces <= 128 && !few) e = forward<T, 64, 2>(p, stream);
   else if (pieces <= 256) e = forward<T, 256, 1>(p, stream);
-  else if (pieces <= 512) e = forward<T, 256, 2>(p, stream);
-  else if (pieces <= 1024) e = forward<T, 256, 4>(p, stream);
-  else if (V == 8 || pieces <= 2048) e = forward<T, 256, 8>(p, stream);
-  else e = forward<T, 256, 64 / V>(p, stream);
+  else if (pieces <= 512 && !few) e = forward<T, 256, 2>(p, stream);
+  else if (pieces <= 1024 && !few) e = forward<T, 256, 4>(p, stream);
+  else if (pieces <= 1024) e = forward<T, 1024, 1>(p, stream);
+  else if (pieces <= 2048 && !few) e = forward<T, 256, 8>(p, stream);
+  else if (pieces <= 2048) e = forward<T, 1024, 2>(p, stream);
+  else if (pieces <= 4096) e = forward<T, 1024, 4>(p, stream);
+  else if (pieces <= 8192) e = forward<T, 1024, 8>(p, stream);
+  else e = forward<T, 1024, 16>(p, stream);
   if (e != hipSuccess || p.parts == 1) return e;
   const dim3 grid((uint32_t)((p.n + kWaves - 1) / kWaves));
   if (p.top) hipLaunchKernelGGL((logprob_join_kernel<T, true>), grid, dim3(kThreads), 0, stream, p);
@@ -425,10 +525,8 @@ template <typename T> hipError_t backward(const LogprobParams& p, hipStream_t st
 }  // namespace
 
 size_t logprob_plan(LogprobParams& p, bool bf16, unsigned char* ws) {
-  const int64_t most = 64 * kThreads, piece = bf16 ? 8 : 4;   // values that a workgroup holds
-  constexpr int64_t fill = 1024, least = 1024;                // workgroups, values a part
-  int64_t parts = (p.V + most - 1) / most;
-  if (p.n * parts < fill) parts = max(parts, min(min((fill + p.n - 1) / max(p.n, (int64_t)1), p.V / least), (int64_t)64));
+  const int64_t piece = bf16 ? 8 : 4, most = 16 * 1024 * piece;   // values that a workgroup holds
+  const int64_t parts = (p.V + most - 1) / most;
   p.width = ((p.V + parts - 1) / parts + piece - 1) / piece * piece;
   p.parts = (p.V + p.width - 1) / p.width;
   if (p.parts == 1) return 0;
