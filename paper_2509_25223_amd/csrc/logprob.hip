@@ -3,16 +3,14 @@
 // gradient by the logits, scale (g (1[j = y] - p_j) - e p_j (z_j - lse + H)).
 //
 // A row is read once, into registers: with its largest value mx known, the sums are of
-// 2^((x - mx) k), k = scale log2 e, and of these times (x - mx) k.  Taken as
-// fma(x, k, -c) with c = mx k rounded, a value is two instructions; what c lost (one factor
-// for the whole row) is taken out of the sums at the end.  A row longer than the registers of a
+// 2^((x - mx) k), k = scale log2 e, and of these times (x - mx) k.  A row longer than the registers of a
 // workgroup hold, or one of few rows, is read in parts by several, each leaving its largest
 // value, sums and alternatives, which logprob_join merges.
 //
 // Alternatives: values are compared as whole numbers in their order (0: none, -inf or NaN).
 // Of a wave's 64 lanes' largest values the q-th is a bound that q values of the wave reach (its upper
-// 16 bits are enough), and the r-th of the waves' bounds one that q r >= `top` values of the row do; values from the bound on are collected in LDS, where a
-// piece's largest says that it has any, and ranked by counting, (value, place) being different
+// 16 bits are enough), and the r-th of the waves' bounds one that q r >= `top` values of the row do; values from the bound on are collected in LDS by
+// the few lanes whose largest reaches it, and ranked by counting, (value, place) being different
 // for each.  Where more reach the bound than LDS has room for (equal or neighbouring large
 // logits), it is raised by bisection until exactly `top` do.
 #include "model.hpp"
@@ -184,7 +182,7 @@ template <typename T, int L, int N> struct Part {
       for (int e = 0; e < V; ++e) raw[j][e] = e < left ? x[c + e] : from_f<T>(-kInf);
     }
   }
-  // Values are converted anew in each pass over them: kept, they would take twice the registers.
+  // Before each pass: values are converted anew, kept they would take twice the registers.
   __device__ __forceinline__ void again() {
     typedef uint32_t Words __attribute__((ext_vector_type(4)));
 #pragma unroll
@@ -195,7 +193,6 @@ template <typename T, int L, int N> struct Part {
     }
   }
   template <typename F> __device__ __forceinline__ void each(F f) {
-    again();
 #pragma unroll
     for (int j = 0; j < N; ++j)
 #pragma unroll
@@ -220,8 +217,9 @@ __device__ __forceinline__ void write_row(const LogprobParams& p, int64_t row, c
 // ---------------------------------------------------------------------------
 // L lanes a part of a row, N pieces a lane.  Part: row / part = id / p.parts, id % p.parts.
 // ---------------------------------------------------------------------------
+// (1024 lanes, up to 7 pieces: in 64 registers, for two rows on a CU)
 template <typename T, int L, int N, bool TOP>
-__global__ __launch_bounds__(L > kThreads ? L : kThreads) void logprob_fwd_kernel(LogprobParams p, int64_t first) {
+__global__ __launch_bounds__(L > kThreads ? L : kThreads, !TOP && L == 1024 && N <= 7 ? 8 : 1) void logprob_fwd_kernel(LogprobParams p, int64_t first) {
   constexpr int V = kPiece<T>, kSub = L > kThreads ? 1 : kThreads / L, W = L / 64;
   __shared__ float slots[3][kSub][W];
   __shared__ TopLds<L> tops[TOP ? kSub : 1];
@@ -240,20 +238,13 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void logprob_fwd_kerne
   bool there = false;
   if (p.logprob && p.parts == 1 && lane == 0) given = given_logit<T>(p, row, there);
 
-  // the largest value, of each piece and of all
-  float big[N], mx = -kInf;
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    big[j] = to_f<T>(v.raw[j][0]);
-#pragma unroll
-    for (int e = 1; e < V; ++e) big[j] = fmaxf(big[j], to_f<T>(v.raw[j][e]));
-    mx = fmaxf(mx, big[j]);
-  }
-  uint32_t bound = 0;
+  float own = -kInf;   // the lane's largest
+  v.each([&](int, int, float z) { own = fmaxf(own, z); });
+  float mx = wave_max(own);
   // (a wave's q-th; the workgroup's: the r-th of its waves', so that r waves have q each)
   const int q = (want + max(W / 2, 1) - 1) / max(W / 2, 1);
-  if constexpr (TOP) bound = bound_of_lanes(order_key(mx), q);
-  mx = wave_max(mx);
+  uint32_t bound = 0;
+  if constexpr (TOP) bound = bound_of_lanes(order_key(own), q);
   if ((threadIdx.x & 63) == 0) {
     slots[0][sub][w] = mx;
     if (TOP) top.bound[w] = bound;
@@ -265,31 +256,30 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void logprob_fwd_kerne
     if constexpr (TOP) bound = bound_of_lanes((threadIdx.x & 63) < W ? top.bound[threadIdx.x & 63 & (W - 1)] : 0u, (want + q - 1) / q);
   }
 
-  const float k = p.scale * kLog2e, m0 = mx == -kInf ? 0.f : mx, c = m0 * k;
-  float s = 0.f, ent = 0.f;
-  auto add = [&](float d) {
-    const float y = __builtin_amdgcn_exp2f(d);
-    s += y;
-    ent = __builtin_fmaf(y, fmaxf(d, -1000.f), ent);   // (0 times -inf)
-  };
-  if (__builtin_fabsf(c) > 1e30f) {   // c could overflow (a row at the type's lowest value)
-    v.each([&](int, int, float z) { add((z - m0) * k); });
-  } else if (p.entropy) {
-    v.each([&](int, int, float z) { add(__builtin_fmaf(z, k, -c)); });
-  } else {
-    v.each([&](int, int, float z) { s += __builtin_amdgcn_exp2f(__builtin_fmaf(z, k, -c)); });
-  }
   if constexpr (TOP) {
     const float least = from_order_key(max(bound, kLowestKey));
     v.again();
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (big[j] >= least)
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float z = to_f<T>(v.raw[j][e]);
-          if (z >= least) collect(top, order_key(z), v.col(j, lane) + e);
-        }
+    if (own >= least) {
+      int at = lane * V;   // (computed here: kept from the loads, the pieces' columns take registers)
+      asm volatile("" : "+v"(at));
+      v.each([&](int j, int e, float z) {
+        if (z >= least) collect(top, order_key(z), at + j * (L * V) + e);
+      });
+    }
+  }
+  // (the difference first: mx k alone could overflow, in a row at the type's lowest value)
+  const float k = p.scale * kLog2e, m0 = mx == -kInf ? 0.f : mx;
+  float s = 0.f, ent = 0.f;
+  if (p.entropy) {
+    v.again();
+    v.each([&](int, int, float z) {
+      const float d = (z - m0) * k, y = __builtin_amdgcn_exp2f(d);
+      s += y;
+      ent = __builtin_fmaf(y, fmaxf(d, -1000.f), ent);   // (0 times -inf)
+    });
+  } else {
+    v.again();   // (in each branch: what both convert would be taken out of them)
+    v.each([&](int, int, float z) { s += __builtin_amdgcn_exp2f((z - m0) * k); });
   }
   s = wave_sum(s);
   if (p.entropy) ent = wave_sum(ent);
@@ -303,11 +293,6 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void logprob_fwd_kerne
     ent = over(slots[2][0], Add());
   } else if (TOP) {
     row_barrier<L>();
-  }
-  if (__builtin_fabsf(c) <= 1e30f) {   // the factor 2^(mx k - c) out of the sums
-    const float lost = __builtin_fmaf(m0, k, -c), f = __builtin_amdgcn_exp2f(-lost);
-    ent = (ent - lost * s) * f;
-    s *= f;
   }
   const RowResult r(m0, s, p.scale);
   if (lane == 0) {
@@ -371,9 +356,12 @@ template <typename T, bool TOP> __global__ __launch_bounds__(kThreads) void logp
         f(at < 0 ? 0u : order_key(p.cand_x[row * count + j]), at);
       }
     };
-    uint32_t best = 0;
-    each([&](uint32_t key, int) { best = max(best, key); });
-    const uint32_t bound = max(bound_of_lanes(best, p.top), kLowestKey);
+    uint32_t bound = kLowestKey;
+    if (count > kRoom<64>) {
+      uint32_t best = 0;
+      each([&](uint32_t key, int) { best = max(best, key); });
+      bound = max(bound_of_lanes(best, p.top), bound);
+    }
     if (lane == 0) top.count = 0;
     row_barrier<64>();
     each([&](uint32_t key, int at) {
@@ -479,24 +467,35 @@ template <typename T, int L, int N> hipError_t forward(const LogprobParams& p, h
   }
   return hipSuccess;
 }
-// The fewest lanes that hold a part in few enough pieces; the most where there are few rows.
+// Lanes of a row: few rows take the most; of many, 64 up to 4 pieces a lane, 256 up to 6, or 16 with
+// alternatives (whose search costs each wave the same), then 1024.  us, bf16: 16384 x 32768 on 1024 lanes
+// (256 of 16 pieces) 167 (189), with five alternatives 257 (232); 4001 x 49152 with five on 1024 lanes (512
+// of 12) 90 (114).
 constexpr int64_t kFewRows = 512;
+template <typename T, int L> hipError_t forward_pieces(const LogprobParams& p, int64_t n, hipStream_t stream) {
+  if (n <= 1) return forward<T, L, 1>(p, stream);
+  if (n <= 2) return forward<T, L, 2>(p, stream);
+  if constexpr (L == 64) return forward<T, L, 4>(p, stream);
+  else {
+    if (n <= 4) return forward<T, L, 4>(p, stream);
+    if (n <= 5) return forward<T, L, 5>(p, stream);
+    if (n <= 6) return forward<T, L, 6>(p, stream);
+    if (n <= 7) return forward<T, L, 7>(p, stream);
+    if (n <= 8) return forward<T, L, 8>(p, stream);
+    if (n <= 10) return forward<T, L, 10>(p, stream);
+    if (n <= 13) return forward<T, L, 13>(p, stream);
+    return forward<T, L, 16>(p, stream);
+  }
+}
 template <typename T> hipError_t forward(const LogprobParams& p, hipStream_t stream) {
   constexpr int V = kPiece<T>;
   const int64_t pieces = (p.width + V - 1) / V;
   const bool few = p.n * p.parts <= kFewRows;
-  hipError_t e;
-  if (pieces <= 64) e = forward<T, 64, 1>(p, stream);
-  else if (pieces <= 128 && !few) e = forward<T, 64, 2>(p, stream);
-  else if (pieces <= 256) e = forward<T, 256, 1>(p, stream);
-  else if (pieces <= 512 && !few) e = forward<T, 256, 2>(p, stream);
-  else if (pieces <= 1024 && !few) e = forward<T, 256, 4>(p, stream);
-  else if (pieces <= 1024) e = forward<T, 1024, 1>(p, stream);
-  else if (pieces <= 2048 && !few) e = forward<T, 256, 8>(p, stream);
-  else if (pieces <= 2048) e = forward<T, 1024, 2>(p, stream);
-  else if (pieces <= 4096) e = forward<T, 1024, 4>(p, stream);
-  else if (pieces <= 8192) e = forward<T, 1024, 8>(p, stream);
-  else e = forward<T, 1024, 16>(p, stream);
+  const int64_t lanes = pieces <= 64 * (few ? 1 : 4) ? 64 : pieces <= 256 * (few ? 1 : p.top ? 16 : 6) ? 256 : 1024;
+  const int64_t n = (pieces + lanes - 1) / lanes;
+  hipError_t e = lanes == 64    ? forward_pieces<T, 64>(p, n, stream)
+                 : lanes == 256 ? forward_pieces<T, 256>(p, n, stream)
+                                : forward_pieces<T, 1024>(p, n, stream);
   if (e != hipSuccess || p.parts == 1) return e;
   const dim3 grid((uint32_t)((p.n + kWaves - 1) / kWaves));
   if (p.top) hipLaunchKernelGGL((logprob_join_kernel<T, true>), grid, dim3(kThreads), 0, stream, p);
@@ -525,8 +524,11 @@ template <typename T> hipError_t backward(const LogprobParams& p, hipStream_t st
 }  // namespace
 
 size_t logprob_plan(LogprobParams& p, bool bf16, unsigned char* ws) {
-  const int64_t piece = bf16 ? 8 : 4, most = 16 * 1024 * piece;   // values that a workgroup holds
-  const int64_t parts = (p.V + most - 1) / most;
+  // Values that a workgroup holds; few long rows: as many workgroups as CUs, of no less than 32768 values.
+  const int64_t piece = bf16 ? 8 : 4, most = 16 * 1024 * piece;
+  constexpr int64_t cus = 256, least = 32768;
+  int64_t parts = (p.V + most - 1) / most;
+  if (p.n * parts < cus) parts = max(parts, min(cus / max(p.n, (int64_t)1), p.V / least));
   p.width = ((p.V + parts - 1) / parts + piece - 1) / piece * piece;
   p.parts = (p.V + p.width - 1) / p.width;
   if (p.parts == 1) return 0;
