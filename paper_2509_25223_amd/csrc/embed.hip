@@ -21,6 +21,14 @@ namespace rla {
 
 namespace {
 
+// Pieces of V values of a row, the i-th from column i V.  FULL: the last one moved back to the row's end,
+// so that all are whole (what two of them cover is computed by both, to the same bits; not where
+// a row is added to in place).
+template <int V, bool FULL> __device__ __forceinline__ int64_t piece_col(int64_t i, int64_t D) {
+  return FULL ? min(i * V, D - V) : i * V;
+}
+bool full(const EmbedParams& p, int V) { return p.D % V == 0 || (p.D >= V && (!p.base || p.base != p.dtable)); }
+
 // The id as a sorting key: V for one without a row.
 __device__ __forceinline__ uint32_t key_of(const EmbedParams& p, int64_t t) {
   const int64_t id = p.ids[t];
@@ -36,7 +44,7 @@ __global__ __launch_bounds__(kThreads) void embed_fwd_kernel(EmbedParams p, uint
   const uint32_t id = blockIdx.x * kThreads + threadIdx.x;
   if (id >= count) return;
   const uint32_t t = id / pieces;
-  const int64_t c = (int64_t)(id % pieces) * V;
+  const int64_t c = piece_col<V, FULL>(id % pieces, p.D);
   const int left = (int)min(p.D - c, (int64_t)V);
   const uint32_t row = key_of(p, t);
   float x[V];
@@ -54,6 +62,8 @@ __global__ __launch_bounds__(kThreads) void embed_fwd_kernel(EmbedParams p, uint
 // ---------------------------------------------------------------------------
 // sorting
 // ---------------------------------------------------------------------------
+constexpr int kEmbedTile = 1024, kEmbedLargeTile = 4096;   // tokens of a tile: of up to 65536 tokens, of more
+// ---------------------------------------------------------------------------
 __global__ __launch_bounds__(kThreads) void embed_count_kernel(EmbedParams p) {
   extern __shared__ int32_t lds[];
   const int tid = threadIdx.x, bins = 1 << p.bits1;
@@ -69,61 +79,81 @@ __global__ __launch_bounds__(kThreads) void embed_count_kernel(EmbedParams p) {
   for (int b = tid; b < bins; b += kThreads) p.count1[(int64_t)blockIdx.x * bins + b] = lds[b];
 }
 
-// A tile's tokens to their places.  Each wave has a quarter of the tile, in order; lds:
+// A tile's tokens to their places.  Each wave has a quarter of the tile, in order, ROUNDS of 64; lds:
 // [kWaves][bins] next places by wave and digit, then kThreads sums.
-template <bool SECOND> __device__ __forceinline__ void sort_tile(const EmbedParams& p, int tile, int32_t* lds) {
+template <bool SECOND, int ROUNDS> __device__ __forceinline__ void sort_tile(const EmbedParams& p, int tile, int32_t* lds) {
   const int bits = SECOND ? p.bits2 : p.bits1, bins = 1 << bits;
   const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63;
   const int32_t* counts = SECOND ? p.count2 : p.count1;
   int32_t* place = lds;
   int32_t* sums = lds + kWaves * bins;
-  const int64_t first = (int64_t)tile * p.tile + (int64_t)w * (p.tile / kWaves);
-  auto key_at = [&](int64_t i) { return SECOND ? (uint32_t)p.key1[i] : key_of(p, i); };
+  const int64_t first = (int64_t)tile * p.tile + (int64_t)w * (ROUNDS * 64) + lane;
   auto digit = [&](uint32_t k) { return (int)((SECOND ? k >> p.bits1 : k) & (uint32_t)(bins - 1)); };
 
-  for (int b = tid; b < kWaves * bins; b += kThreads) place[b] = 0;
-  __syncthreads();
-  for (int j = lane; j < p.tile / kWaves; j += 64)
-    if (first + j < p.n) atomicAdd(&place[w * bins + digit(key_at(first + j))], 1);
-  // a thread's digits: how many tokens have them, and how many of those lie in earlier tiles
+  uint32_t key[ROUNDS];
+  int32_t pos[ROUNDS];
+#pragma unroll
+  for (int j = 0; j < ROUNDS; ++j) {
+    const int64_t i = min(first + j * 64, p.n - 1);
+    key[j] = SECOND ? (uint32_t)p.key1[i] : key_of(p, i);
+    pos[j] = SECOND ? p.pos1[i] : (int32_t)i;
+  }
+  // a thread's digits: how many tokens have each, and how many of those lie in earlier tiles
+  constexpr int kMost = (1 << 11) / kThreads, kAhead = 8;   // digits of a thread; loads in flight
   const int per = (bins + kThreads - 1) / kThreads;
-  int32_t total = 0;
-  for (int j = 0; j < per; ++j) {
+  int32_t before[kMost], all[kMost], total = 0;
+#pragma unroll
+  for (int j = 0; j < kMost; ++j) {
+    before[j] = all[j] = 0;
     const int b = tid * per + j;
-    if (b >= bins) break;
-    for (int i = 0; i < p.tiles; ++i) total += counts[(int64_t)i * bins + b];
-  }
-  sums[tid] = total;
-  __syncthreads();
-  for (int d = 1; d < kThreads; d <<= 1) {
-    const int32_t o = tid >= d ? sums[tid - d] : 0;
-    __syncthreads();
-    sums[tid] += o;
-    __syncthreads();
-  }
-  int32_t at = sums[tid] - total;   // places before the thread's digits
-  for (int j = 0; j < per; ++j) {
-    const int b = tid * per + j;
-    if (b >= bins) break;
-    int32_t before = 0, behind = 0;
-    for (int i = 0; i < p.tiles; ++i) {
-      const int32_t c = counts[(int64_t)i * bins + b];
-      before += i < tile ? c : 0;
-      behind += i < tile ? 0 : c;
+    if (j >= per || b >= bins) continue;
+    for (int i0 = 0; i0 < p.tiles; i0 += kAhead) {
+      int32_t c[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) c[u] = counts[(int64_t)min(i0 + u, p.tiles - 1) * bins + b];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        all[j] += i0 + u < p.tiles ? c[u] : 0;
+        before[j] += i0 + u < tile ? c[u] : 0;
+      }
     }
-    int32_t next = at + before;
+    total += all[j];
+  }
+  for (int b = tid; b < kWaves * bins; b += kThreads) place[b] = 0;
+  // places before the thread's digits: over the wave's lanes, then over the waves
+  int32_t at = total;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int32_t o = __shfl_up(at, d);
+    at += lane >= d ? o : 0;
+  }
+  if (lane == 63) sums[w] = at;
+  at -= total;
+  __syncthreads();
+#pragma unroll
+  for (int v = 0; v < kWaves - 1; ++v) at += v < w ? sums[v] : 0;
+#pragma unroll
+  for (int j = 0; j < ROUNDS; ++j)
+    if (first + j * 64 < p.n) atomicAdd(&place[w * bins + digit(key[j])], 1);
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kMost; ++j) {
+    const int b = tid * per + j;
+    if (j >= per || b >= bins) continue;
+    int32_t next = at + before[j];
+#pragma unroll
     for (int v = 0; v < kWaves; ++v) {
       const int32_t c = place[v * bins + b];
       place[v * bins + b] = next;
       next += c;
     }
-    at += before + behind;
+    at += all[j];
   }
   __syncthreads();
-  for (int j0 = 0; j0 < p.tile / kWaves; j0 += 64) {
-    const int64_t i = first + j0 + lane;
-    const bool there = i < p.n;
-    const uint32_t k = there ? key_at(i) : 0;
+#pragma unroll
+  for (int j = 0; j < ROUNDS; ++j) {
+    const bool there = first + j * 64 < p.n;
+    const uint32_t k = key[j];
     const int d = digit(k);
     // lanes of the same digit
     uint64_t same = __ballot(there);
@@ -142,35 +172,47 @@ template <bool SECOND> __device__ __forceinline__ void sort_tile(const EmbedPara
     __builtin_amdgcn_wave_barrier();
     if (SECOND) {
       p.key[to] = (int32_t)k;
-      p.pos[to] = p.pos1[i];
+      p.pos[to] = pos[j];
     } else {
       p.key1[to] = (int32_t)k;
-      p.pos1[to] = (int32_t)i;
-      atomicAdd(&p.count2[(((int64_t)(to / p.tile)) << p.bits2) + (k >> p.bits1)], 1);
-      if (k < (uint32_t)p.V) atomicOr(&p.present[k >> 5], 1u << (k & 31));
+      p.pos1[to] = pos[j];
+      // one lane for all of a key (and of a tile that they land in: two at most), or a frequent id's tokens
+      // wait for each other (16384 tokens, 10 % of one id: 17 us)
+      uint64_t equal = same;
+      for (int b = 0; b < p.bits2; ++b) {
+        const uint32_t bit = k >> (p.bits1 + b) & 1u;
+        const uint64_t set = __ballot(bit);
+        equal &= bit ? set : ~set;
+      }
+      const uint64_t odd = __ballot(to / p.tile & 1);
+      equal &= to / p.tile & 1 ? odd : ~odd;
+      if ((equal & ((1ull << lane) - 1)) == 0) {
+        atomicAdd(&p.count2[(((int64_t)(to / p.tile)) << p.bits2) + (k >> p.bits1)], __popcll(equal));
+        if (k < (uint32_t)p.V) atomicOr(&p.present[k >> 5], 1u << (k & 31));
+      }
     }
   }
 }
 
-__global__ __launch_bounds__(kThreads) void embed_sort1_kernel(EmbedParams p) {
+template <int ROUNDS> __global__ __launch_bounds__(kThreads) void embed_sort1_kernel(EmbedParams p) {
   extern __shared__ int32_t lds[];
-  sort_tile<false>(p, blockIdx.x, lds);
+  sort_tile<false, ROUNDS>(p, blockIdx.x, lds);
 }
 
 constexpr int kFillPieces = 8;   // 16-byte pieces a thread of the workgroups that write rows without a token
 
-template <bool FULL, bool NT>
+template <int ROUNDS, bool FULL, bool NT>
 __global__ __launch_bounds__(kThreads) void embed_sort2_kernel(EmbedParams p, uint32_t pieces) {
   extern __shared__ int32_t lds[];
   if ((int)blockIdx.x < p.tiles) {
-    sort_tile<true>(p, blockIdx.x, lds);
+    sort_tile<true, ROUNDS>(p, blockIdx.x, lds);
     return;
   }
   const int64_t first = ((int64_t)blockIdx.x - p.tiles) * (kThreads * kFillPieces) + threadIdx.x;
 #pragma unroll
   for (int j = 0; j < kFillPieces; ++j) {
     const int64_t id = first + j * kThreads;
-    const int64_t v = id / pieces, c = (id - v * pieces) * 4;
+    const int64_t v = id / pieces, c = piece_col<4, FULL>(id - v * pieces, p.D);
     if (v >= p.V || (p.present[v >> 5] >> (v & 31)) & 1u) continue;
     const int left = (int)min(p.D - c, (int64_t)4);
     float x[4] = {0.f, 0.f, 0.f, 0.f};
@@ -186,24 +228,28 @@ __global__ __launch_bounds__(kThreads) void embed_sort2_kernel(EmbedParams p, ui
 // next chunk.
 __device__ __forceinline__ bool ends_next(const EmbedParams& p, int64_t i1, int32_t k) {
   const int64_t i2 = min(i1 + p.chunk, p.n);
-  return p.key[i2 - 1] != k || i2 == p.n || p.key[i2] != k;
+  const int32_t last = p.key[i2 - 1], behind = p.key[min(i2, p.n - 1)];
+  return last != k || i2 == p.n || behind != k;
 }
 
-// L lanes a chunk of sorted tokens, a piece of the columns a lane (blockIdx.y: which L pieces)
-template <typename T, int L, bool FULL>
+// L lanes a chunk of sorted tokens, a piece of the columns a lane (blockIdx.y: which L pieces).
+// BASE: what the sums are added to is loaded with the rows, for each token (those of one run hit the caches).
+template <typename T, int L, bool FULL, bool BASE>
 __global__ __launch_bounds__(kThreads) void embed_sums_kernel(EmbedParams p) {
-  constexpr int V = kPiece<T>, kAhead = 4;
+  constexpr int V = kPiece<T>, kAhead = BASE ? 4 : 8;
   const int64_t c = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
   if (c >= p.chunks) return;
-  const int64_t col = ((int64_t)blockIdx.y * L + threadIdx.x % L) * V;
-  if (col >= p.D) return;
+  const int64_t piece = (int64_t)blockIdx.y * L + threadIdx.x % L, col = piece_col<V, FULL>(piece, p.D);
+  if (piece * V >= p.D) return;
   const int left = (int)min(p.D - col, (int64_t)V);
   int64_t i = c * p.chunk, end = min(i + p.chunk, p.n);
-  const int32_t kFirst = p.key[i], kLast = p.key[end - 1];
+  const int32_t kFirst = p.key[i], kLast = p.key[end - 1], kBefore = p.key[max(i - 1, (int64_t)0)],
+                kEarlier = p.key[max(i - p.chunk - 1, (int64_t)0)], kBehind = p.key[min(end, p.n - 1)];
+  const bool goes_on = end < p.n && kBehind == kLast, short_tail = ends_next(p, end, kLast);
   bool head = false;   // the first run began in an earlier chunk, which leaves it in parts
-  if (c > 0 && p.key[i - 1] == kFirst) {
-    const bool began_before = c == 1 || p.key[i - p.chunk - 1] != kFirst;
-    const bool ends_here = kLast != kFirst || end == p.n || p.key[end] != kFirst;
+  if (c > 0 && kBefore == kFirst) {
+    const bool began_before = c == 1 || kEarlier != kFirst;
+    const bool ends_here = kLast != kFirst || !goes_on;
     if (began_before && ends_here) {   // the previous chunk's
       while (i < end && p.key[i] == kFirst) ++i;
     } else {
@@ -211,32 +257,25 @@ __global__ __launch_bounds__(kThreads) void embed_sums_kernel(EmbedParams p) {
     }
   }
   bool tail = false;   // the last run goes on beyond the next chunk
-  if (end < p.n && p.key[end] == kLast && !(head && kFirst == kLast)) {
-    if (ends_next(p, end, kLast)) {
+  if (goes_on && !(head && kFirst == kLast)) {
+    if (short_tail) {
       while (end < p.n && p.key[end] == kLast) ++end;
     } else {
       tail = true;
     }
   }
   if (i >= end) return;
-  float sum[V];
+  float sum[V], base[V];
 #pragma unroll
-  for (int e = 0; e < V; ++e) sum[e] = 0.f;
+  for (int e = 0; e < V; ++e) sum[e] = base[e] = 0.f;
   int32_t k = p.key[i];
   auto flush = [&](bool last) {
     if (k >= (int32_t)p.V) return;
     if (head || (last && tail)) {
       store_piece<float, V, FULL>(p.part + (c * 2 + (head ? 0 : 1)) * p.D + col, left, sum);
     } else {
-      float b[V];
-      if (p.base) {
-        load_piece<float, V, FULL>(p.base + (int64_t)k * p.D + col, left, b);
 #pragma unroll
-        for (int e = 0; e < V; ++e) sum[e] = __builtin_fmaf(p.scale, sum[e], b[e]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < V; ++e) sum[e] *= p.scale;
-      }
+      for (int e = 0; e < V; ++e) sum[e] = BASE ? __builtin_fmaf(p.scale, sum[e], base[e]) : p.scale * sum[e];
       store_piece<float, V, FULL>(p.dtable + (int64_t)k * p.D + col, left, sum);
     }
   };
@@ -244,11 +283,13 @@ __global__ __launch_bounds__(kThreads) void embed_sums_kernel(EmbedParams p) {
   for (; i < end; i += kAhead) {
     int32_t kk[kAhead];
     typename RowVec<T, V>::type raw[kAhead];
+    float bb[BASE ? kAhead : 1][V];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {   // (past the end: the last again, not used)
       const int64_t at = min(i + u, end - 1);
       kk[u] = p.key[at];
       load_raw<T, V, FULL>(dout + (int64_t)p.pos[at] * p.dos, left, raw[u]);
+      if constexpr (BASE) load_piece<float, V, FULL>(p.base + min((int64_t)kk[u], p.V - 1) * p.D + col, left, bb[u]);
     }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
@@ -261,7 +302,10 @@ __global__ __launch_bounds__(kThreads) void embed_sums_kernel(EmbedParams p) {
         for (int e = 0; e < V; ++e) sum[e] = 0.f;
       }
 #pragma unroll
-      for (int e = 0; e < V; ++e) sum[e] += to_f<T>(raw[u][e]);
+      for (int e = 0; e < V; ++e) {
+        sum[e] += to_f<T>(raw[u][e]);
+        if constexpr (BASE) base[e] = bb[u][e];
+      }
     }
   }
   flush(true);
@@ -272,8 +316,8 @@ __global__ __launch_bounds__(kThreads) void embed_sums_kernel(EmbedParams p) {
 template <bool FULL> __global__ __launch_bounds__(kThreads) void embed_join_kernel(EmbedParams p, int32_t per) {
   __shared__ float sums[kWaves][64][4];
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t c0 = (int64_t)blockIdx.y * per, col = ((int64_t)blockIdx.x * 64 + lane) * 4;
-  const int left = (int)min(p.D - col, (int64_t)4);
+  const int64_t c0 = (int64_t)blockIdx.y * per, piece = (int64_t)blockIdx.x * 64 + lane, col = piece_col<4, FULL>(piece, p.D);
+  const int left = piece * 4 < p.D ? (int)min(p.D - col, (int64_t)4) : 0;
   bool split = false;
   if (lane < per && c0 + lane + 1 < p.chunks) {
     const int64_t i = (c0 + lane) * p.chunk, end = i + p.chunk;
@@ -295,11 +339,18 @@ template <bool FULL> __global__ __launch_bounds__(kThreads) void embed_join_kern
     }
     float s[4] = {0.f, 0.f, 0.f, 0.f};
     if (left > 0) {
-      for (int64_t j = w; j <= count; j += kWaves) {
-        float x[4];
-        load_piece<float, 4, FULL>(p.part + ((c + j) * 2 + (j == 0 ? 1 : 0)) * p.D + col, left, x);
+      constexpr int kAhead = 8;   // loads in flight (past the last: it again, not used)
+      for (int64_t j0 = w; j0 <= count; j0 += kAhead * kWaves) {
+        float x[kAhead][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] += x[e];
+        for (int u = 0; u < kAhead; ++u) {
+          const int64_t j = min(j0 + u * kWaves, count);
+          load_piece<float, 4, FULL>(p.part + ((c + j) * 2 + (j == 0 ? 1 : 0)) * p.D + col, left, x[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[e] += j0 + u * kWaves <= count ? x[u][e] : 0.f;
       }
     }
 #pragma unroll
@@ -348,13 +399,14 @@ template <typename X, typename T, bool FULL> hipError_t forward(const EmbedParam
   return hipSuccess;
 }
 template <typename X, typename T> hipError_t forward(const EmbedParams& p, hipStream_t stream) {
-  return p.D % kPiece<T> == 0 ? forward<X, T, true>(p, stream) : forward<X, T, false>(p, stream);
+  return full(p, kPiece<T>) ? forward<X, T, true>(p, stream) : forward<X, T, false>(p, stream);
 }
 
 template <typename T, int L, bool FULL> hipError_t sums(const EmbedParams& p, hipStream_t stream) {
   constexpr int V = kPiece<T>, sub = kThreads / L;
   const dim3 grid((uint32_t)((p.chunks + sub - 1) / sub), (uint32_t)((p.D + L * V - 1) / (L * V)));
-  hipLaunchKernelGGL((embed_sums_kernel<T, L, FULL>), grid, dim3(kThreads), 0, stream, p);
+  if (p.base) hipLaunchKernelGGL((embed_sums_kernel<T, L, FULL, true>), grid, dim3(kThreads), 0, stream, p);
+  else hipLaunchKernelGGL((embed_sums_kernel<T, L, FULL, false>), grid, dim3(kThreads), 0, stream, p);
   return hipGetLastError();
 }
 template <typename T, bool FULL> hipError_t sums(const EmbedParams& p, hipStream_t stream) {
@@ -367,21 +419,21 @@ template <typename T, bool FULL> hipError_t sums(const EmbedParams& p, hipStream
   return sums<T, 256, FULL>(p, stream);
 }
 
-template <bool FULL> hipError_t sort_and_fill(const EmbedParams& p, hipStream_t stream) {
+template <int ROUNDS, bool FULL> hipError_t sort_and_fill(const EmbedParams& p, hipStream_t stream) {
   const size_t lds1 = 4 * ((size_t)kWaves * (1 << p.bits1) + kThreads), lds2 = 4 * ((size_t)kWaves * (1 << p.bits2) + kThreads);
   hipLaunchKernelGGL(embed_count_kernel, dim3(p.tiles), dim3(kThreads), 4u << p.bits1, stream, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(embed_sort1_kernel, dim3(p.tiles), dim3(kThreads), lds1, stream, p);
+  hipLaunchKernelGGL(embed_sort1_kernel<ROUNDS>, dim3(p.tiles), dim3(kThreads), lds1, stream, p);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t pieces = (p.D + 3) / 4, count = p.base == p.dtable ? 0 : p.V * pieces;
   const int64_t wgs = (count + kThreads * kFillPieces - 1) / (kThreads * kFillPieces);
   if (p.V * p.D * 4 > kNtBytes)
-    hipLaunchKernelGGL((embed_sort2_kernel<FULL, true>), dim3((uint32_t)(p.tiles + wgs)), dim3(kThreads), lds2, stream, p,
+    hipLaunchKernelGGL((embed_sort2_kernel<ROUNDS, FULL, true>), dim3((uint32_t)(p.tiles + wgs)), dim3(kThreads), lds2, stream, p,
                        (uint32_t)pieces);
   else
-    hipLaunchKernelGGL((embed_sort2_kernel<FULL, false>), dim3((uint32_t)(p.tiles + wgs)), dim3(kThreads), lds2, stream, p,
+    hipLaunchKernelGGL((embed_sort2_kernel<ROUNDS, FULL, false>), dim3((uint32_t)(p.tiles + wgs)), dim3(kThreads), lds2, stream, p,
                        (uint32_t)pieces);
   return hipGetLastError();
 }
@@ -389,13 +441,16 @@ template <bool FULL> hipError_t sort_and_fill(const EmbedParams& p, hipStream_t 
 // One slice's gradient.
 template <typename T> hipError_t backward(const EmbedParams& p, hipStream_t stream) {
   constexpr int V = kPiece<T>;
-  hipError_t e = p.D % 4 == 0 ? sort_and_fill<true>(p, stream) : sort_and_fill<false>(p, stream);
+  static_assert(kEmbedTile == 4 * 64 * kWaves && kEmbedLargeTile == 16 * 64 * kWaves, "rounds of a wave");
+  hipError_t e;
+  if (p.tile == kEmbedTile) e = full(p, 4) ? sort_and_fill<4, true>(p, stream) : sort_and_fill<4, false>(p, stream);
+  else e = full(p, 4) ? sort_and_fill<16, true>(p, stream) : sort_and_fill<16, false>(p, stream);
   if (e != hipSuccess) return e;
-  e = p.D % V == 0 ? sums<T, true>(p, stream) : sums<T, false>(p, stream);
+  e = full(p, V) ? sums<T, true>(p, stream) : sums<T, false>(p, stream);
   if (e != hipSuccess || p.chunks < 3) return e;   // (a run in parts spans a whole chunk and its neighbours)
   const int32_t per = (p.chunks + 127) / 128;
   const dim3 grid((uint32_t)((p.D + 255) / 256), (uint32_t)((p.chunks + per - 1) / per));
-  if (p.D % 4 == 0) hipLaunchKernelGGL(embed_join_kernel<true>, grid, dim3(kThreads), 0, stream, p, per);
+  if (full(p, 4)) hipLaunchKernelGGL(embed_join_kernel<true>, grid, dim3(kThreads), 0, stream, p, per);
   else hipLaunchKernelGGL(embed_join_kernel<false>, grid, dim3(kThreads), 0, stream, p, per);
   return hipGetLastError();
 }
@@ -408,9 +463,9 @@ size_t embed_plan(EmbedParams& p, int64_t tokens, unsigned char* ws) {
   p.bits1 = (bits + 1) / 2;
   p.bits2 = bits - p.bits1;
   p.n = tokens;
-  p.tile = tokens <= 65536 ? 1024 : 4096;
+  p.tile = tokens <= 65536 ? kEmbedTile : kEmbedLargeTile;
   p.tiles = (int32_t)((tokens + p.tile - 1) / p.tile);
-  p.chunk = 16;
+  p.chunk = tokens <= 8192 ? 8 : 16;   // (few tokens: more groups of lanes)
   while (p.chunk * 4096 < tokens) p.chunk *= 2;
   p.chunks = (int32_t)((tokens + p.chunk - 1) / p.chunk);
   size_t off = 0;
