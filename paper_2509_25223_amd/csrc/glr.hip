@@ -313,7 +313,7 @@ __device__ __forceinline__ void stretch_forward(const GlrParams& p, const Place&
 // tokens.  SUMMARY: the chunk's pair only.
 // ---------------------------------------------------------------------------
 template <typename T, bool HAS_I, bool HAS_Z, bool NORM, bool SUMMARY, bool WHOLE>
-__global__ __launch_bounds__(kGlrThreads) void glr_fwd_kernel(GlrParams p, uint32_t blocks, int save) {
+__global__ __launch_bounds__(kGlrThreads, sizeof(T) == 2 ? 4 : 2) void glr_fwd_kernel(GlrParams p, uint32_t blocks, int save) {
   __shared__ GlrLds lds;
   if (blockIdx.x >= blocks * p.nchunk) {
     copy_empty(p, p.h0, p.hfin, blockIdx.x - p.nchunk * blocks);
@@ -652,12 +652,15 @@ template <typename F> hipError_t with(const GlrParams& p, bool bf16, bool i, boo
 void glr_plan(GlrParams& p, bool packed) {
   const int64_t blocks = blocks_of(p), ntok = p.map.ntok;
   constexpr int64_t tile = kTile;
-  constexpr int64_t fill = 256;   // workgroups that fill the card
-  const int64_t want = max((int64_t)1, fill / blocks);
+  // Whole sequences where they give every CU a workgroup: then no pass before is needed.  Else chunks, for two
+  // workgroups a CU (16384 x 2048: 124 us, one a CU 139; 4 sequences of 4096 x 4096 with gradients 447, cut in
+  // two each 775).
+  constexpr int64_t cus = 256;
+  const int64_t apart = max((int64_t)1, cus / blocks), want = max((int64_t)1, 2 * cus / blocks);
   p.apart = 0;
-  if (!packed && p.map.nseq >= want) {   // whole sequences
+  if (!packed && p.map.nseq >= apart) {
     const int64_t T = max(p.map.T, (int64_t)1), each = max(p.map.nseq / want, (tile + T - 1) / T);
-    p.L = each * p.map.T;
+    p.L = max(each, (int64_t)1) * p.map.T;
     p.apart = 1;
   } else {
     const int64_t n = max((int64_t)1, min(want, (ntok + tile - 1) / tile));
