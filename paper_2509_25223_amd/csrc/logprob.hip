@@ -9,7 +9,8 @@
 //
 // Alternatives: values are compared as whole numbers in their order (0: none, -inf or NaN).
 // Of a wave's 64 lanes' largest values the q-th is a bound that q values of the wave reach (its upper
-// 16 bits are enough), and the r-th of the waves' bounds one that q r >= `top` values of the row do; values from the bound on are collected in LDS by
+// 16 bits are enough), and the r-th of the waves' bounds one that q r >= `top` values of the row do (or any wave's
+// `top`-th); values from the bound on are collected in LDS by
 // the few lanes whose largest reaches it, and ranked by counting, (value, place) being different
 // for each.  Where more reach the bound than LDS has room for (equal or neighbouring large
 // logits), it is raised by bisection until exactly `top` do.
@@ -79,7 +80,7 @@ struct Candidate {
 template <int L> constexpr int kRoom = L > 64 ? 256 : 128;
 
 template <int L> struct TopLds {
-  uint32_t bound[L / 64];
+  uint32_t bound[L / 64], whole[L / 64];   // of each wave: its q-th, its `want`-th
   int32_t count, sums[2][L / 64];
   Candidate list[kRoom<L>];
 };
@@ -244,16 +245,27 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads, !TOP && L == 1024 && N
   // (a wave's q-th; the workgroup's: the r-th of its waves', so that r waves have q each)
   const int q = (want + max(W / 2, 1) - 1) / max(W / 2, 1);
   uint32_t bound = 0;
-  if constexpr (TOP) bound = bound_of_lanes(order_key(own), q);
+  uint32_t whole = 0;
+  if constexpr (TOP) {
+    bound = bound_of_lanes(order_key(own), q);
+    if (L > 64) whole = bound_of_lanes(order_key(own), want);
+  }
   if ((threadIdx.x & 63) == 0) {
     slots[0][sub][w] = mx;
-    if (TOP) top.bound[w] = bound;
+    if (TOP) {
+      top.bound[w] = bound;
+      top.whole[w] = whole;
+    }
   }
   if (TOP && lane == 0) top.count = 0;
   row_barrier<L>();
   if constexpr (L > 64) {
     mx = over(slots[0][0], Max());
-    if constexpr (TOP) bound = bound_of_lanes((threadIdx.x & 63) < W ? top.bound[threadIdx.x & 63 & (W - 1)] : 0u, (want + q - 1) / q);
+    if constexpr (TOP) {
+      bound = bound_of_lanes((threadIdx.x & 63) < W ? top.bound[threadIdx.x & (W - 1)] : 0u, (want + q - 1) / q);
+#pragma unroll
+      for (int i = 0; i < W; ++i) bound = max(bound, top.whole[i]);   // (few waves have any: a grammar's tokens)
+    }
   }
 
   if constexpr (TOP) {

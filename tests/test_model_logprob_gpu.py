@@ -303,3 +303,21 @@ def test_refused_gradients(device):
     wide = lref.strided(x, 1)
     with pytest.raises(ValueError, match="out"):
         f(wide, lse, y, lse, out=wide)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("V", [20000, 131072])
+@pytest.mark.parametrize("allowed", [3, 40, 400, 3000])
+def test_few_allowed(device, dtype, V, allowed):
+    """A stretch of the vocabulary is allowed, the rest -inf: fewer than the alternatives asked
+    for, a few lanes' worth, a few waves' worth."""
+    g = torch.Generator(device).manual_seed(allowed)
+    x = torch.full((6, V), NEG, dtype=TYPES[dtype], device=device)
+    first = [0, 7, V // 2, V - allowed, 1024, 8191]
+    for r, a in enumerate(first):
+        x[r, a:a + allowed] = (3 * torch.randn(allowed, device=device, generator=g)).to(TYPES[dtype])
+    y = torch.tensor(first, device=device)
+    y[1] = 0
+    for top in (1, 20, 64):
+        got = rla.rla_logprob_forward(x, y, entropy=True, top=top)
+        check_forward(got, ref.logprob(x.cpu().double(), y.cpu(), 1.0, top), top)
