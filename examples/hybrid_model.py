@@ -2,18 +2,18 @@
 
 One residual stream (fp32) and two mixing blocks on it:
 
-  n, r = addnorm(embedding)
+  n, r = addnorm(embed(tokens))
   block 1   q, k, v, gate, four gates = n W1;  q, k, v through a short convolution;
             Residual Delta Net;  gated norm per head;  x = .. W2
   n, r = addnorm(x, r)
   block 2   u, delta, z, B, C = n W3;  u through a short convolution;  selective
             scan;  gated norm;  x = .. W4
-  n, r = addnorm(x, r);  logits = n W5
+  n, r = addnorm(x, r);  logits = n W5;  loss: their log probabilities of the next tokens
 
 `Model.forward` takes a batch [B, T] or packed sequences [T] with their offsets, and
 returns each sequence's state; `Model.decode` carries such states one token on, in
-place; `Model.gradients` is the training step's backward.  The projections and the
-loss are torch; what is between them are the package's calls.
+place; `Model.gradients` is the training step's backward.  The projections are torch;
+what is between them, the lookup of the tokens and the loss are the package's calls.
 
   python examples/hybrid_model.py [--steps 400]
 
@@ -77,7 +77,7 @@ class Model:
         """(logits, state) of tokens [B, T], or packed [T]; `state`: the one that the
         sequences continue.  With save, also what `gradients` needs."""
         p, n_of = self.p, (lambda s, key: None if s is None else s[key])
-        x0 = self._cast("embed")[tokens]
+        x0 = rla.rla_embed_forward(tokens, p["embed"], out_dtype=self.dtype)
         n1, r1 = rla.rla_addnorm_forward(x0, p["norm1"])
         p1 = n1 @ self._cast("w1")
         (q, k, v, gate), gates = self._split1(p1)
@@ -119,7 +119,7 @@ class Model:
     def decode(self, tokens, state):
         """Logits [B, vocab] of the token behind tokens [B]; `state` moves on in place."""
         p = self.p
-        n1, r = rla.rla_addnorm_forward(self._cast("embed")[tokens][:, None], p["norm1"])
+        n1, r = rla.rla_addnorm_forward(rla.rla_embed_forward(tokens[:, None], p["embed"], out_dtype=self.dtype), p["norm1"])
         (q, k, v, gate), gates = self._split1(n1 @ self._cast("w1"))
         mixed = []
         for i, t in enumerate((q, k, v)):
@@ -142,10 +142,13 @@ class Model:
 
     def loss(self, logits, targets):
         """Mean cross entropy, and its gradient by the logits."""
-        flat = torch.log_softmax(logits.flatten(0, -2), -1)
-        at = targets.reshape(-1, 1)
-        grad = flat.exp().scatter_add(1, at, torch.full_like(at, -1, dtype=flat.dtype)) / at.numel()
-        return -flat.gather(1, at).mean(), grad.view_as(logits)
+        if logits.dtype == torch.float64:   # (for differences: the definition)
+            lp = torch.log_softmax(logits, -1)
+            p = lp.exp().scatter_add(-1, targets[..., None], torch.full_like(lp[..., :1], -1))
+            return -lp.gather(-1, targets[..., None]).mean(), p / targets.numel()
+        f = rla.rla_logprob_forward(logits, targets)
+        up = torch.full_like(f["lse"], -1.0 / targets.numel())
+        return -f["logprob"].mean(), rla.rla_logprob_backward(logits, f["lse"], targets, up)
 
     def gradients(self, dlogits, s):
         """Gradients of every parameter, from the gradient by the logits and what
@@ -190,7 +193,7 @@ class Model:
         dn1 = through("w1", s["n1"], torch.cat(dx + [dgate] + dgates, -1))
         b = rla.rla_addnorm_backward(dn1, s["r1"], p["norm1"], dresidual_out=dr)
         g["norm1"] = b["dweight"]
-        g["embed"] = torch.zeros_like(p["embed"]).index_add_(0, s["tokens"].reshape(-1), b["dx"].flatten(0, -2).float())
+        g["embed"] = rla.rla_embed_backward(s["tokens"], b["dx"], self.vocab)
         return g
 
 
@@ -210,8 +213,8 @@ def train(model, steps, batch=16, length=128, rate=3e-3, seed=1, report=None):
     v = {n: torch.zeros_like(t) for n, t in model.p.items()}
     for i in range(1, steps + 1):
         data = periodic(model.vocab, batch, length + 1, gen).to(model.device)
-        logits, _, saved = model.forward(data[:, :-1], save=True)
-        loss, dlogits = model.loss(logits, data[:, 1:])
+        logits, _, saved = model.forward(data[:, :-1].contiguous(), save=True)
+        loss, dlogits = model.loss(logits, data[:, 1:].contiguous())
         for n, grad in model.gradients(dlogits, saved).items():
             m[n].lerp_(grad, 0.1)
             v[n].lerp_(grad * grad, 0.02)
@@ -224,18 +227,22 @@ def train(model, steps, batch=16, length=128, rate=3e-3, seed=1, report=None):
     return losses
 
 
+def likeliest(logits):
+    return rla.rla_logprob_forward(logits, top=1)["top_ids"][..., 0]
+
+
 def generate(model, prompts, count):
     """The `count` likeliest tokens behind each prompt: the prompts packed in one call,
     then a token of each at a time."""
     ends = torch.tensor([0] + [len(t) for t in prompts]).cumsum(0)
     cu = ends.to(model.device, torch.int32)
     logits, state = model.forward(torch.cat(prompts).to(model.device), cu_seqlens=cu)
-    token = logits[(ends[1:] - 1).to(model.device)].argmax(-1)
+    token = likeliest(logits[(ends[1:] - 1).to(model.device)])
     out = [token]
     for _ in range(count - 1):
-        token = model.decode(token, state).argmax(-1)
+        token = likeliest(model.decode(token, state))
         out.append(token)
-    return torch.stack(out, 1).cpu()
+    return torch.stack(out, 1).long().cpu()
 
 
 def main():
