@@ -80,7 +80,7 @@ typedef struct {
   int32_t index;             /* rla_index of the tokens */
   int32_t dtype;             /* rla_dtype of logits, dlogits */
   int32_t top;               /* alternatives a row, 0 to 64, <= V */
-  float scale;               /* inverse temperature: > 0, finite */
+  float scale;               /* inverse temperature: > 0, scale log2 e finite */
 } rla_logprob_problem;
 
 /* Bytes of the forward's workspace (0: none is needed, or an invalid problem). */

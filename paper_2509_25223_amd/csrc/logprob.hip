@@ -423,7 +423,7 @@ __global__ __launch_bounds__(kThreads) void logprob_bwd_kernel(LogprobParams p, 
   const int64_t id = first + (int64_t)blockIdx.x * kSub + threadIdx.x / L;
   const int64_t row = id / segs;
   if (row >= p.n) return;
-  const int64_t c0 = (id - row * segs) * (L * N * V) + (threadIdx.x % L) * V;
+  const int64_t seg = id - row * segs, c0 = seg * (L * N * V) + (threadIdx.x % L) * V;
   const T* x = reinterpret_cast<const T*>(p.x) + row * p.xs;
   T* dx = reinterpret_cast<T*>(p.dx) + row * p.V;
   float in[N][V];
@@ -446,32 +446,43 @@ __global__ __launch_bounds__(kThreads) void logprob_bwd_kernel(LogprobParams p, 
   }
   const bool none = lse == -kInf;
   float mx = 0.f, ln = lse;
-  if (__builtin_fabsf(lse) > kFarLse && __builtin_fabsf(lse) < kInf) far_row<T, L>(p, x, mx, ln);
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const int64_t c = c0 + j * (L * V);
+  auto write = [&](int64_t c, float (&v)[V]) {
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      const float d = __builtin_fmaf(in[j][e] - mx, p.scale, -ln);   // log p
+      const float d = __builtin_fmaf(v[e] - mx, p.scale, -ln);   // log p
       const float pr = __builtin_amdgcn_exp2f(d * kLog2e);
       float t = -pr * __builtin_fmaf(de, fmaxf(d, -1000.f) + H, g);
       if (c + e == y) t += g;
-      in[j][e] = none ? 0.f : t * p.scale;
+      v[e] = none ? 0.f : t * p.scale;
     }
-    store_piece<T, V, false, NT>(dx + c, (int)min(p.V - c, (int64_t)V), in[j]);
+    store_piece<T, V, false, NT>(dx + c, (int)min(p.V - c, (int64_t)V), v);
+  };
+  if (__builtin_fabsf(lse) > kFarLse && __builtin_fabsf(lse) < kInf) {
+    // by its first lanes alone: in place, others would write what these read again
+    if (seg > 0) return;
+    far_row<T, L>(p, x, mx, ln);
+    for (int64_t c = threadIdx.x % L * V; c < p.V; c += L * V) {
+      float v[V];
+      load_piece<T, V>(x + c, (int)min(p.V - c, (int64_t)V), v);
+      write(c, v);
+    }
+    return;
   }
+#pragma unroll
+  for (int j = 0; j < N; ++j) write(c0 + j * (L * V), in[j]);
 }
 
 // ---------------------------------------------------------------------------
 // launches
 // ---------------------------------------------------------------------------
-constexpr int64_t kMaxGrid = (int64_t)1 << 23;   // workgroups a launch
+constexpr int64_t kMaxLanes = (int64_t)1 << 31;   // of a launch
 
 template <typename T, int L, int N> hipError_t forward(const LogprobParams& p, hipStream_t stream) {
   const int64_t sub = L > kThreads ? 1 : kThreads / L, wgs = (p.n * p.parts + sub - 1) / sub;
   const dim3 threads(L > kThreads ? L : kThreads);
-  for (int64_t w = 0; w < wgs; w += kMaxGrid) {
-    const dim3 grid((uint32_t)min(wgs - w, kMaxGrid));
+  constexpr int64_t most = kMaxLanes / (L > kThreads ? L : kThreads);
+  for (int64_t w = 0; w < wgs; w += most) {
+    const dim3 grid((uint32_t)min(wgs - w, most));
     if (p.top) hipLaunchKernelGGL((logprob_fwd_kernel<T, L, N, true>), grid, threads, 0, stream, p, w * sub);
     else hipLaunchKernelGGL((logprob_fwd_kernel<T, L, N, false>), grid, threads, 0, stream, p, w * sub);
     const hipError_t e = hipGetLastError();
@@ -519,8 +530,9 @@ template <typename T, int L, int N> hipError_t backward(const LogprobParams& p, 
   constexpr int V = kPiece<T>;
   const int64_t sub = kThreads / L, segs = (p.V + L * N * V - 1) / (L * N * V), wgs = (p.n * segs + sub - 1) / sub;
   const bool nt = p.n * p.V * (int64_t)sizeof(T) > kNtBytes;
-  for (int64_t w = 0; w < wgs; w += kMaxGrid) {
-    const dim3 grid((uint32_t)min(wgs - w, kMaxGrid));
+  constexpr int64_t most = kMaxLanes / kThreads;
+  for (int64_t w = 0; w < wgs; w += most) {
+    const dim3 grid((uint32_t)min(wgs - w, most));
     if (nt) hipLaunchKernelGGL((logprob_bwd_kernel<T, L, N, true>), grid, dim3(kThreads), 0, stream, p, w * sub, (uint32_t)segs);
     else hipLaunchKernelGGL((logprob_bwd_kernel<T, L, N, false>), grid, dim3(kThreads), 0, stream, p, w * sub, (uint32_t)segs);
     const hipError_t e = hipGetLastError();

@@ -101,7 +101,7 @@ rla_status check_logprob(const rla_logprob_problem* q, LogprobParams& p) {
       q->top > q->vocab)
     return RLA_ERR_SHAPE;
   if (!stride(q->logits_stride, q->vocab, p.xs) || times(times(q->rows, p.xs), 4) < 0) return RLA_ERR_SHAPE;
-  if (!(q->scale > 0.f) || isinf(q->scale)) return RLA_ERR_VALUE;
+  if (!(q->scale > 0.f) || isinf(q->scale * 1.4426950408889634f)) return RLA_ERR_VALUE;   // (kernels use scale log2 e)
   p.n = q->rows;
   p.V = q->vocab;
   p.scale = q->scale;

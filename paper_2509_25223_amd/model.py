@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import operator
 
 from . import layer as _layer
 from .layer import _check, _code, _cu, _device, _elsewhere, _gradients, _need, _new, _ok, _ptr, _rows, _space, _tokens
@@ -81,7 +82,7 @@ def _stream(stream, index):
     return _layer._stream_handle(stream, index)
 
 
-# problems by their sizes (never changed after): building one costs as much as passing it
+# problems by their sizes (numbers, never changed after): building one costs as much as passing it
 _embed_problem = functools.lru_cache(256)(rla_embed_problem)
 _logprob_problem = functools.lru_cache(256)(rla_logprob_problem)
 _glr_problem = functools.lru_cache(256)(rla_glr_problem)
@@ -103,7 +104,7 @@ def _embed(ids, vocab, width, dtype, table_dtype, scale, dout=None):
     index = _device("ids", ids)
     kind = _ids("ids", ids, index)
     ds = 0 if dout is None else _rows("dout", dout, index, ids.shape + (width,), ids.dim(), dout.dtype)
-    return _embed_problem(ids.numel(), vocab, width, ds, kind, dtype, table_dtype, scale), index
+    return _embed_problem(ids.numel(), vocab, width, ds, kind, dtype, table_dtype, float(scale)), index
 
 
 def make_embed_problem(ids, table, scale=1.0) -> rla_embed_problem:
@@ -149,7 +150,7 @@ def rla_embed_backward(ids, dout, vocab, scale=1.0, base=None, dtable=None, work
         _need(ids=ids, dout=dout, vocab=vocab)
     if dout.dim() != ids.dim() + 1:
         raise ValueError("dout must be [.., width]")
-    D = dout.shape[-1]
+    D, vocab = dout.shape[-1], operator.index(vocab)
     code = _code("dout", dout.dtype)
     problem, index = _embed(ids, vocab, D, code, code, scale, dout)
     _check("base", base, index, (vocab, D), torch.float32)
@@ -178,13 +179,13 @@ def _logprob(logits, targets, top, scale):
     lead = shape[:-1]
     stride = _rows("logits", logits, index, shape, len(lead), logits.dtype)
     kind = RLA_INDEX_I64 if targets is None else _ids("targets", targets, index, lead)
-    return _logprob_problem(lead.numel(), V, stride, kind, dtype, top, scale), index, lead
+    return _logprob_problem(lead.numel(), V, stride, kind, dtype, top, float(scale)), index, lead
 
 
 def make_logprob_problem(logits, top=0, scale=1.0) -> rla_logprob_problem:
     """rla_logprob_problem for logits [.., vocab]."""
     _lib()
-    return rla_logprob_problem.from_buffer_copy(_logprob(logits, None, top, scale)[0])
+    return rla_logprob_problem.from_buffer_copy(_logprob(logits, None, operator.index(top), scale)[0])
 
 
 def rla_logprob_workspace_size(problem: rla_logprob_problem) -> int:
@@ -203,6 +204,7 @@ def rla_logprob_forward(logits, targets=None, scale=1.0, entropy=False, top=0, o
     None for what is not asked for.  `out`, `lse`, `entropy_out`, `top_logprobs`,
     `top_ids` are written into if given."""
     lib = _lib()
+    top = operator.index(top)
     problem, index, lead = _logprob(logits, targets, top, scale)
     if not 0 <= top <= 64 or top > logits.shape[-1]:
         raise ValueError("top must be 0 to 64, and at most the vocabulary; got %d" % top)

@@ -156,3 +156,10 @@ def test_sizes_beyond_a_launch(lib):
     for batch, want in ((1 << 29, SHAPE), (1 << 26, NULL)):
         p = rla.rla_glr_problem(batch=batch, seq_len=1, channels=64, normalize=1, dtype=rla.RLA_BF16)
         assert lib.rla_glr_decode(p, FAKE, FAKE, FAKE, None, None, FAKE, None, FAKE, None) == want
+
+
+def test_scale_in_base_2(lib):
+    """A scale that times log2 e leaves fp32 is refused."""
+    for scale, want in ((3e38, VALUE), (2e38, NULL)):
+        p = rla.rla_logprob_problem(rows=1, vocab=5, index=1, dtype=rla.RLA_F32, top=0, scale=scale)
+        assert lib.rla_logprob_forward(p, None, FAKE, FAKE, None, None, None, None, None, 0, None) == want

@@ -183,3 +183,13 @@ def test_refused_gradients(device):
     for bad in (dict(vocab=0), dict(vocab=1 << 22), dict(vocab=5, scale=float("nan"))):
         with pytest.raises((rla.RLAError, ValueError)):
             f(ids, torch.zeros(10, 1, device=device), **bad, dtable=None)
+
+
+def test_numbers_in_tensors(device):
+    """A scale given as a tensor counts as what it holds when the call is made."""
+    table, ids = torch.randn(10, 8, device=device), torch.arange(10, device=device)
+    scale = torch.tensor(0.5)
+    assert torch.equal(rla.rla_embed_forward(ids, table, scale), 0.5 * table)
+    scale.fill_(2.0)
+    assert torch.equal(rla.rla_embed_forward(ids, table, scale), 2 * table)
+    assert torch.equal(rla.rla_embed_backward(ids, table, torch.tensor(10), scale), 2 * table)

@@ -321,3 +321,46 @@ def test_few_allowed(device, dtype, V, allowed):
     for top in (1, 20, 64):
         got = rla.rla_logprob_forward(x, y, entropy=True, top=top)
         check_forward(got, ref.logprob(x.cpu().double(), y.cpu(), 1.0, top), top)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("V", [50, 700, 20001, 200003])
+def test_far_rows_in_place(device, dtype, V):
+    """Rows that are read again are not read where their gradient already stands."""
+    x, y, gen = rows(40, V, dtype, seed=V)
+    x[::2] += 30000.0
+    x[1::4] = torch.finfo(TYPES[dtype]).min
+    g, e = torch.randn(40, generator=gen).to(device), torch.randn(40, generator=gen).to(device)
+    f = rla.rla_logprob_forward(x, y, entropy=True)
+    want = rla.rla_logprob_backward(x, f["lse"], y, g, f["entropy"], e)
+    got = rla.rla_logprob_backward(x, f["lse"], y, g, f["entropy"], e, out=x)
+    assert got is x and torch.equal(got, want)
+
+
+def test_numbers_in_tensors(device):
+    """A scale and a count given as tensors count as what they hold when the call is made."""
+    x, y, _ = rows(4, 100, "f32")
+    scale, top = torch.tensor(0.5), torch.tensor(3)
+    first = rla.rla_logprob_forward(x, y, scale=scale, top=top)
+    scale.fill_(2.0)
+    top.fill_(5)
+    second = rla.rla_logprob_forward(x, y, scale=scale, top=top)
+    for got, s, n in ((first, 0.5, 3), (second, 2.0, 5)):
+        check_forward(got, ref.logprob(x.cpu().double(), y.cpu(), s, n), n, entropy=False)
+
+
+def test_more_long_rows_than_a_launch(device):
+    """Rows that a workgroup of 1024 lanes takes each, beyond the lanes of one launch."""
+    n, V = (1 << 22) + 3, 12289
+    if torch.cuda.mem_get_info()[0] < 2 * n * V + (4 << 30):
+        pytest.skip("needs 107 GB")
+    x = torch.zeros(n, V, dtype=torch.bfloat16, device=device)
+    some = [0, (1 << 21) - 1, 1 << 21, 1 << 22, n - 1]
+    near, y, _ = rows(len(some), V, "bf16")
+    x[some] = near
+    targets = torch.zeros(n, dtype=torch.int32, device=device)
+    targets[some] = y.int()
+    f = rla.rla_logprob_forward(x, targets)
+    check_forward({k: f[k][some] for k in ("lse", "logprob")}, ref.logprob(near.cpu().double(), y.cpu(), 1.0, 0), 0, entropy=False)
+    f["lse"][some] = f["lse"][1].item()
+    assert (f["lse"] == f["lse"][1]).all()
