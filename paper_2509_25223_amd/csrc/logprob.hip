@@ -9,11 +9,12 @@
 //
 // Alternatives: values are compared as whole numbers in their order (0: none, -inf or NaN).
 // Of a wave's 64 lanes' largest values the q-th is a bound that q values of the wave reach (its upper
-// 16 bits are enough), and the r-th of the waves' bounds one that q r >= `top` values of the row do (or any wave's
-// `top`-th); values from the bound on are collected in LDS by
-// the few lanes whose largest reaches it, and ranked by counting, (value, place) being different
-// for each.  Where more reach the bound than LDS has room for (equal or neighbouring large
-// logits), it is raised by bisection until exactly `top` do.
+// 16 bits are enough), and the r-th of the waves' bounds one that q r >= `top` values of the row do;
+// values from the bound on are collected in LDS by the few lanes whose largest reaches it, and
+// ranked by counting, (value, place) being different for each.  Where more reach the bound than LDS
+// has room for, the row is read again: first with the largest of the waves' `top`-th lanes as the bound
+// (a few hundred neighbouring tokens allowed), then, if that does not do (equal large logits), by
+// bisection until exactly `top` reach it.
 #include "model.hpp"
 
 namespace rla {
@@ -80,7 +81,7 @@ struct Candidate {
 template <int L> constexpr int kRoom = L > 64 ? 256 : 128;
 
 template <int L> struct TopLds {
-  uint32_t bound[L / 64], whole[L / 64];   // of each wave: its q-th, its `want`-th
+  uint32_t bound[L / 64];   // of each wave
   int32_t count, sums[2][L / 64];
   Candidate list[kRoom<L>];
 };
@@ -103,22 +104,44 @@ template <int L> __device__ __forceinline__ void collect(TopLds<L>& s, uint32_t 
   if (j < kRoom<L>) s.list[j] = Candidate{key, at};
 }
 
-// More than fit were collected: the largest bound that `want` values reach, of the values equal to
-// it those up to the place that leaves `want`, collected anew.  for_each(f) hands all of the lane's
-// (key, place) to f.
-template <int L, typename Each> __device__ __forceinline__ void collect_exactly(int want, TopLds<L>& s, Each for_each) {
+// More than fit were collected: anew, from the largest of the waves' own bounds on, if a wave has `want`
+// lanes of values (a mask that leaves a stretch of tokens; `own`: the lane's largest key).
+template <int L, typename Each> __device__ __forceinline__ void collect_stretch(int want, uint32_t own, TopLds<L>& s, Each for_each) {
+  const uint32_t wave = bound_of_lanes(own, want);
+  __syncthreads();   // (all have read the count)
+  if ((threadIdx.x & 63) == 0) s.bound[threadIdx.x >> 6] = wave;
+  if (threadIdx.x == 0) s.count = 0;
+  __syncthreads();
+  uint32_t bound = kLowestKey;
+#pragma unroll
+  for (int w = 0; w < L / 64; ++w) bound = max(bound, s.bound[w]);
+  for_each([&](uint32_t k, int at) {
+    if (k >= bound) collect(s, k, at);
+  });
+  __syncthreads();
+}
+
+// Still more: the largest bound that `want` values reach (the row's largest key `most`, if that many
+// equal it), of the values equal to it those up to the place that leaves `want`, collected anew.
+// for_each(f) hands all of the lane's (key, place < places) to f.
+template <int L, typename Each>
+__device__ __forceinline__ void collect_exactly(int want, uint32_t most, int places, TopLds<L>& s, Each for_each) {
   int turn = 0;
   auto reach = [&](uint32_t t) {
     int c = 0;
     for_each([&](uint32_t k, int) { c += k >= t ? 1 : 0; });
     return row_count<L>(c, s, turn++);
   };
-  uint32_t t = 0;
-  for (uint32_t bit = 0x80000000u; bit; bit >>= 1)
-    if (reach(t | bit) >= want) t |= bit;
-  const int above = t == 0xffffffffu ? 0 : reach(t + 1);
+  uint32_t t = most;
+  int above = 0;
+  if (reach(most) < want) {
+    t = 0;
+    for (uint32_t bit = 0x80000000u; bit; bit >>= 1)
+      if (reach(t | bit) >= want) t |= bit;
+    above = reach(t + 1);
+  }
   int32_t last = 0;   // fewer than want - above equal values lie before it
-  for (int32_t bit = 1 << 30; bit; bit >>= 1) {
+  for (int32_t bit = 1 << (31 - __builtin_clz(places)); bit; bit >>= 1) {
     int c = 0;
     const int32_t upto = last | bit;
     for_each([&](uint32_t k, int at) { c += k == t && at < upto ? 1 : 0; });
@@ -245,27 +268,16 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads, !TOP && L == 1024 && N
   // (a wave's q-th; the workgroup's: the r-th of its waves', so that r waves have q each)
   const int q = (want + max(W / 2, 1) - 1) / max(W / 2, 1);
   uint32_t bound = 0;
-  uint32_t whole = 0;
-  if constexpr (TOP) {
-    bound = bound_of_lanes(order_key(own), q);
-    if (L > 64) whole = bound_of_lanes(order_key(own), want);
-  }
+  if constexpr (TOP) bound = bound_of_lanes(order_key(own), q);
   if ((threadIdx.x & 63) == 0) {
     slots[0][sub][w] = mx;
-    if (TOP) {
-      top.bound[w] = bound;
-      top.whole[w] = whole;
-    }
+    if (TOP) top.bound[w] = bound;
   }
   if (TOP && lane == 0) top.count = 0;
   row_barrier<L>();
   if constexpr (L > 64) {
     mx = over(slots[0][0], Max());
-    if constexpr (TOP) {
-      bound = bound_of_lanes((threadIdx.x & 63) < W ? top.bound[threadIdx.x & (W - 1)] : 0u, (want + q - 1) / q);
-#pragma unroll
-      for (int i = 0; i < W; ++i) bound = max(bound, top.whole[i]);   // (few waves have any: a grammar's tokens)
-    }
+    if constexpr (TOP) bound = bound_of_lanes((threadIdx.x & 63) < W ? top.bound[threadIdx.x & (W - 1)] : 0u, (want + q - 1) / q);
   }
 
   if constexpr (TOP) {
@@ -312,10 +324,12 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads, !TOP && L == 1024 && N
     else *reinterpret_cast<floatx4*>(p.stat + id * 4) = floatx4{mx, s, ent, 0.f};
   }
   if constexpr (TOP) {
-    if (top.count > kRoom<L>)
-      collect_exactly<L>(want, top, [&](auto&& f) {   // (read again: rare, and registers are few)
-        for (int i = lane; i < width; i += L) f(order_key(to_f<T>(x[i])), i);
-      });
+    auto again = [&](auto&& f) {   // (read again: rare, and registers are few)
+      for (int i = lane; i < width; i += L) f(order_key(to_f<T>(x[i])), i);
+    };
+    if constexpr (L > 64)
+      if (top.count > kRoom<L>) collect_stretch<L>(want, order_key(own), top, again);
+    if (top.count > kRoom<L>) collect_exactly<L>(want, order_key(mx), width, top, again);
     const int64_t base = id * p.top;
     rank_collected<L>(want, top, [&](int rank, uint32_t key, int at) {
       if (p.parts == 1) {
@@ -334,36 +348,46 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads, !TOP && L == 1024 && N
   }
 }
 
-// A wave a row: its parts merged.
+// A wave a row: its parts merged.  What the lane's first part, its first alternative and the row's
+// token need is loaded at once, before anything waits.
 template <typename T, bool TOP> __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobParams p) {
   __shared__ TopLds<64> tops[TOP ? kWaves : 1];
   const int64_t row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
   if (row >= p.n) return;
   const int lane = threadIdx.x & 63;
   const float k = p.scale * kLog2e;
-  float mx = -kInf, s = 0.f, e = 0.f;
-  for (int64_t j = lane; j < p.parts; j += 64) mx = fmaxf(mx, p.stat[(row * p.parts + j) * 4]);
+  const int64_t count = TOP ? p.parts * p.top : 0;
+  auto stat = [&](int64_t j) { return *reinterpret_cast<const floatx4*>(p.stat + (row * p.parts + min(j, p.parts - 1)) * 4); };
+  const floatx4 t0 = stat(lane);
+  float x0 = 0.f;
+  int32_t at0 = -1;
+  if (TOP) {
+    const int64_t j = row * count + min((int64_t)lane, count - 1);
+    x0 = p.cand_x[j];
+    at0 = p.cand_i[j];
+  }
+  bool there = false;
+  const float given = p.logprob ? given_logit<T>(p, row, there) : 0.f;
+  float mx = t0[0], s = 0.f, e = 0.f;
+  for (int64_t j = lane + 64; j < p.parts; j += 64) mx = fmaxf(mx, stat(j)[0]);
   mx = wave_max(mx);
   const float m0 = mx == -kInf ? 0.f : mx;
-  for (int64_t j = lane; j < p.parts; j += 64) {
-    const floatx4 t = *reinterpret_cast<const floatx4*>(p.stat + (row * p.parts + j) * 4);
+  auto add = [&](const floatx4& t) {
     const float d = t[0] == -kInf ? -1000.f : (t[0] - m0) * k, f = __builtin_amdgcn_exp2f(d);
     s = __builtin_fmaf(t[1], f, s);
     e = __builtin_fmaf(__builtin_fmaf(t[1], fmaxf(d, -1000.f), t[2]), f, e);
-  }
+  };
+  if (lane < p.parts) add(t0);
+  for (int64_t j = lane + 64; j < p.parts; j += 64) add(stat(j));
   s = wave_sum(s);
   e = wave_sum(e);
   const RowResult r(m0, s, p.scale);
-  if (lane == 0) {
-    bool there = false;
-    const float given = p.logprob ? given_logit<T>(p, row, there) : 0.f;
-    write_row(p, row, r, s, e, given, there);
-  }
+  if (lane == 0) write_row(p, row, r, s, e, given, there);
   if constexpr (TOP) {
     TopLds<64>& top = tops[threadIdx.x >> 6];
-    const int64_t count = p.parts * p.top;
     auto each = [&](auto&& f) {
-      for (int64_t j = lane; j < count; j += 64) {
+      if (lane < count) f(at0 < 0 ? 0u : order_key(x0), at0);
+      for (int64_t j = lane + 64; j < count; j += 64) {
         const int32_t at = p.cand_i[row * count + j];
         f(at < 0 ? 0u : order_key(p.cand_x[row * count + j]), at);
       }
@@ -380,7 +404,7 @@ template <typename T, bool TOP> __global__ __launch_bounds__(kThreads) void logp
       if (key >= bound) collect(top, key, at);
     });
     row_barrier<64>();
-    if (top.count > kRoom<64>) collect_exactly<64>(p.top, top, each);
+    if (top.count > kRoom<64>) collect_exactly<64>(p.top, order_key(mx), (int)p.V, top, each);
     rank_collected<64>(p.top, top, [&](int rank, uint32_t key, int at) {
       p.top_lp[row * p.top + rank] = key ? r.of(from_order_key(key)) : r.ln == r.ln ? -kInf : r.ln;
       p.top_ids[row * p.top + rank] = key ? at : -1;
