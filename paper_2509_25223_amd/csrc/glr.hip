@@ -8,17 +8,24 @@
 //
 // Two tokens' steps are one, (a2, b2) (a1, b1) = (a2 a1, a2 b1 + b2), so a stretch of tokens is
 // a pair (P, S): h behind it is P h + S.  A workgroup takes 64 channels (128 bytes of
-// bf16: whole lines of the caches) of a chunk of tokens, a tile at a time: a thread 4
-// channels of kTok tokens in registers, the stretches of a wave (4) by exchanges between lanes,
-// those of the workgroup's waves one after the other in LDS, where the state is carried from
-// tile to tile.  Then each thread goes through its tokens from the state before
-// them.  Everything is read once and written once.  The backward goes through the tiles
-// from the last one; it takes h anew from the state before each tile, which the forward
-// kept (or which is computed again), and carries l the other way.
+// bf16: whole lines of the caches) of a chunk of tokens, a tile of 128 at a time: a thread 2
+// channels of 8 tokens in registers, the two stretches of a wave by an exchange between its halves.  The
+// 8 waves' pairs go to LDS, and after the tile's one barrier each wave goes through all of them
+// for itself, so that none waits for another's state; the carried state is every wave's own.  Then
+// each thread goes through its tokens from the state before them.  Everything is read once
+// and written once.  The backward goes through the tiles from the last one; it takes h anew from the
+// state before each tile, which the forward kept (or which is computed again), and carries l the
+// other way.
 // Sequences lie side by side along one axis of tokens, dense ones too: where one
 // starts, the state is its own, whatever came before (never a factor 0: NaN and
-// infinities of a sequence stay there).  Few channels: the tokens are cut into chunks, and a pass
-// before leaves each chunk's pair.
+// infinities of a sequence stay there).  Too few workgroups: the tokens are cut into chunks, and a
+// pass before leaves each chunk's pair, at the price of reading x, r, i (backward: r, dO, z) twice.
+//
+// What bounds it: HBM and the vector ALU together.  bf16, both gates, normalized, 4 x 4096 x 4096:
+// forward 178 us (671 MB, 3.8 TB/s; vector ALUs busy 55 % of the time), backward 279 (1.2 GB, 4.3 TB/s),
+// whose 2 channels x 8 tokens x 7 values take 256 registers: two waves a SIMD.  Measured there and not kept:
+// 16 waves a workgroup and loads a tile further ahead (the same time), 16 tokens a stretch (spills).
+// Loads behind branches, in turn waited for one by one, had cost three times as much (1283 us, now 447).
 #include <math.h>
 
 #include "model.hpp"
@@ -101,8 +108,8 @@ template <bool WHOLE> struct Channels {
 };
 
 // Workgroups are dealt to the 8 XCDs in turn.  Each takes adjacent blocks of channels: the lines of a row
-// lie in all channels of its L2, where every eighth block's would share two of them (16384 x 2048: the
-// forward %s).
+// lie in all channels of its L2, where every eighth block's would share two of them (16384 x 2048
+// forward 139 us, before 147; 3001 x 514 of fp32 with gradients 45, before 49).
 constexpr uint32_t kXcds = 8;
 __device__ __forceinline__ uint32_t work_of(uint32_t wg, uint32_t count) {
   const uint32_t xcd = wg % kXcds, each = count / kXcds, more = count % kXcds;
@@ -115,8 +122,10 @@ template <bool WHOLE> struct Work {
   Channels<WHOLE> ch;
   int64_t t0, end, channel;   // (channel: the lane's own, of the states that waves carry)
   bool owner;                 // the first wave's lanes write what there is one of per channel
-  __device__ __forceinline__ Work(const GlrParams& p, uint32_t blocks) : Work(p, blocks, work_of(blockIdx.x, blocks * p.nchunk)) {}
-  __device__ __forceinline__ Work(const GlrParams& p, uint32_t blocks, uint32_t id) : chunk(id / blocks), ch(p.D, id - chunk * blocks) {
+  __device__ __forceinline__ Work(const GlrParams& p, uint32_t blocks)
+      : Work(p, blocks, work_of(blockIdx.x, blocks * p.nchunk)) {}
+  __device__ __forceinline__ Work(const GlrParams& p, uint32_t blocks, uint32_t id)
+      : chunk(id / blocks), ch(p.D, id - chunk * blocks) {
     t0 = chunk * p.L;
     end = min(t0 + p.L, p.map.ntok);
     channel = ch.c + (threadIdx.x & 63) / kLanes;
@@ -310,7 +319,7 @@ __device__ __forceinline__ void stretch_forward(const GlrParams& p, const Place&
 
 // ---------------------------------------------------------------------------
 // forward.  Behind the chunks' workgroups those that copy the states of sequences without
-// tokens.  SUMMARY: the chunk's pair only.
+// tokens.  SUMMARY: the chunk's pair only (16384 x 2048, bf16: 50 us, then 72 for the rest).
 // ---------------------------------------------------------------------------
 template <typename T, bool HAS_I, bool HAS_Z, bool NORM, bool SUMMARY, bool WHOLE>
 __global__ __launch_bounds__(kGlrThreads, sizeof(T) == 2 ? 4 : 2) void glr_fwd_kernel(GlrParams p, uint32_t blocks, int save) {
@@ -585,7 +594,8 @@ __global__ __launch_bounds__(kGlrThreads) __attribute__((amdgpu_waves_per_eu(2, 
 }
 
 // Single tokens: a thread owns 4 channels of a sequence, whose state it reads before it
-// writes (in place works: a row's last piece is its own, in part).
+// writes (in place works: a row's last piece is its own, in part).  256 x 4096, bf16: 5.3 us for 18.9 MB, in
+// most part a launch and one trip to memory.
 constexpr int kDecV = 4;
 template <typename T, bool HAS_I, bool HAS_Z, bool NORM, bool FULL>
 __global__ __launch_bounds__(kThreads) void glr_decode_kernel(GlrParams p, uint32_t pieces, uint32_t count) {
