@@ -1,23 +1,25 @@
 // Embedding lookup, out_t = scale table[id_t], and the table's gradient: row v gets
 // scale times the sum, in the order of t, of dout_t where id_t = v.
 //
-// The gradient sorts (id, t) by id, stably, in two passes of a counting sort over
-// the id's low and high bits, and sums stretches of equal ids: every row of the table is
+// The gradient sorts (id, t) by id, stably, and sums stretches of equal ids: every row of the table is
 // written once, in one order of summation, and nothing is added by atomics (they count
-// tokens only).  Ids without a row sort behind the others and are dropped.
+// tokens and mark rows only).  Ids without a row sort behind the others and are dropped.  Few tokens:
+//   embed_rank    counts for each token those before it, and marks the rows that have one
+// More, in two passes of a counting sort over the id's low and high bits:
 //   embed_count   a tile of tokens counts its low digits; clears what is counted later
 //   embed_sort    a tile moves its tokens to their places among all: the counts of smaller
 //                 digits, of the same digit in earlier tiles, and in the tile itself
 //                 (first pass: also counts the high digits by the tile that a token lands in,
 //                 and marks the rows that have a token)
 //   embed_sort    second pass; other workgroups write the rows without a token
+// Then:
 //   embed_sums    a group of lanes takes `chunk` sorted tokens and writes the sums of the ids
 //                 that start there and end there or in the next chunk; of longer runs
-//                 each chunk leaves its part
+//                 each chunk leaves its part (few tokens: other workgroups write the rows without one)
 //   embed_join    adds these parts
 // 16384 tokens as frequent as words, 32768 x 2048, bf16 rows into an fp32 table, us: 4.7, 8.9, 43.7 (224 MB of
 // zeros at 5.1 TB/s, the second pass beside them), 27 (67 MB read at random, 45 written), 6.3; all bytes
-// at 5.0 TB/s would take 67.  Few tokens of a narrow table are bound by the five launches.
+// at 5.0 TB/s would take 67.  Few tokens of a narrow table are bound by the launches, two to three.
 #include "model.hpp"
 
 namespace rla {
@@ -203,16 +205,11 @@ template <int ROUNDS> __global__ __launch_bounds__(kThreads) void embed_sort1_ke
   sort_tile<false, ROUNDS>(p, blockIdx.x, lds);
 }
 
-constexpr int kFillPieces = 8;   // 16-byte pieces a thread of the workgroups that write rows without a token
+// Rows without a token, by workgroup.
+constexpr int kFillPieces = 8;   // 16-byte pieces a thread
 
-template <int ROUNDS, bool FULL, bool NT>
-__global__ __launch_bounds__(kThreads) void embed_sort2_kernel(EmbedParams p, uint32_t pieces) {
-  extern __shared__ int32_t lds[];
-  if ((int)blockIdx.x < p.tiles) {
-    sort_tile<true, ROUNDS>(p, blockIdx.x, lds);
-    return;
-  }
-  const int64_t first = ((int64_t)blockIdx.x - p.tiles) * (kThreads * kFillPieces) + threadIdx.x;
+template <bool FULL, bool NT> __device__ __forceinline__ void fill_rows(const EmbedParams& p, uint32_t pieces, int64_t wg) {
+  const int64_t first = wg * (kThreads * kFillPieces) + threadIdx.x;
 #pragma unroll
   for (int j = 0; j < kFillPieces; ++j) {
     const int64_t id = first + j * kThreads;
@@ -223,6 +220,86 @@ __global__ __launch_bounds__(kThreads) void embed_sort2_kernel(EmbedParams p, ui
     if (p.base) load_piece<float, 4, FULL>(p.base + v * p.D + c, left, x);
     store_piece<float, 4, FULL, NT>(p.dtable + v * p.D + c, left, x);
   }
+}
+
+template <int ROUNDS, bool FULL, bool NT>
+__global__ __launch_bounds__(kThreads) void embed_sort2_kernel(EmbedParams p, uint32_t pieces) {
+  extern __shared__ int32_t lds[];
+  if ((int)blockIdx.x < p.tiles) sort_tile<true, ROUNDS>(p, blockIdx.x, lds);
+  else fill_rows<FULL, NT>(p, pieces, (int64_t)blockIdx.x - p.tiles);
+}
+
+// Up to kRankTokens: a token's place is the number of tokens before it in the order, counted over all of
+// them, kRanked tokens a workgroup, 8 lanes each.  The same workgroups find the rows that have a
+// token, kRankWords words of bits each.  One launch for three, whose 2 n^2 operations are 2.3 us of the
+// card's at 6144 tokens.  The whole gradient, us, against the counting sort: 6 tokens 10.3 (15.5), 600 13.9 (20.1),
+// 3000 16.2 (21.7; 32768 x 1024: 34.5, 42.6), 6000 42.5 (44.6), 8000 26.7 (25.6).
+constexpr int kRankTokens = 6144, kRanked = 32, kRankWords = 1024;
+__global__ __launch_bounds__(kThreads) void embed_rank_kernel(EmbedParams p) {
+  __shared__ uint4 keys[kRankTokens / 4];
+  __shared__ uint32_t bits[kRankWords];
+  __shared__ int32_t counts[kThreads / kRanked][kRanked];
+  uint32_t* key = reinterpret_cast<uint32_t*>(keys);
+  const int tid = threadIdx.x, n = (int)p.n, slices = kThreads / kRanked;
+  const int all = (n + 4 * slices - 1) / (4 * slices) * (4 * slices);   // (whole reads of 4 for each slice; past n: behind all)
+  const uint32_t word0 = blockIdx.x * kRankWords;
+  for (int i = tid; i < kRankWords; i += kThreads) bits[i] = 0;
+  __syncthreads();
+  auto load = [&](auto type) {
+    typedef decltype(type) Id;
+    const Id* ids = reinterpret_cast<const Id*>(p.ids.p);
+    constexpr int kAhead = 8;
+    for (int i0 = tid; i0 < all; i0 += kAhead * kThreads) {
+      Id id[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) id[u] = ids[min(i0 + u * kThreads, n - 1)];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int i = i0 + u * kThreads;
+        const bool row = id[u] >= 0 && id[u] < p.V;
+        const uint32_t k = row ? (uint32_t)id[u] : (uint32_t)p.V, word = (k >> 5) - word0;
+        if (i < all) key[i] = i < n ? k : 0xffffffffu;
+        if (row && word < kRankWords) atomicOr(&bits[word], 1u << (k & 31u));   // (past n: the last again)
+      }
+    }
+  };
+  if (p.ids.wide) load(int64_t());
+  else load(int32_t());
+  __syncthreads();
+  const int first = blockIdx.x * kRanked, i = first + tid % kRanked, slice = tid / kRanked;
+  const uint32_t own = first < n ? key[min(i, n - 1)] : 0u;
+  int count = 0;
+  if (first < n) {
+    // (of equal keys the earlier tokens)
+    const int each = all / (4 * slices), g0 = slice * each, block = first / 4;
+#pragma unroll 4
+    for (int g = g0; g < g0 + each; ++g) {
+      const uint4 k = keys[g];
+      const uint32_t below = own + (g < block ? 1u : 0u);
+      count += k.x < below ? 1 : 0;
+      count += k.y < below ? 1 : 0;
+      count += k.z < below ? 1 : 0;
+      count += k.w < below ? 1 : 0;
+    }
+    static_assert(kRanked == 4 * (kThreads / kRanked), "a read of 4 for each slice");
+    const int g = block + slice, j = 4 * g;
+    if (j < i) {
+      const uint4 k = keys[g];
+      count += k.x == own ? 1 : 0;
+      count += k.y == own && j + 1 < i ? 1 : 0;
+      count += k.z == own && j + 2 < i ? 1 : 0;
+      count += k.w == own && j + 3 < i ? 1 : 0;
+    }
+    counts[slice][tid % kRanked] = count;
+  }
+  __syncthreads();
+  if (tid < kRanked && i < n) {
+    int rank = 0;
+    for (int v = 0; v < slices; ++v) rank += counts[v][tid];
+    p.key[rank] = (int32_t)own;
+    p.pos[rank] = i;
+  }
+  for (int64_t w = tid; w < kRankWords && word0 + w <= p.V / 32; w += kThreads) p.present[word0 + w] = bits[w];
 }
 
 // ---------------------------------------------------------------------------
@@ -238,9 +315,16 @@ __device__ __forceinline__ bool ends_next(const EmbedParams& p, int64_t i1, int3
 
 // L lanes a chunk of sorted tokens, a piece of the columns a lane (blockIdx.y: which L pieces).
 // BASE: what the sums are added to is loaded with the rows, for each token (those of one run hit the caches).
+// From workgroup `fill` on (0: none) others write the rows without a token.
 template <typename T, int L, bool FULL, bool BASE>
-__global__ __launch_bounds__(kThreads) void embed_sums_kernel(EmbedParams p) {
+__global__ __launch_bounds__(kThreads) void embed_sums_kernel(EmbedParams p, uint32_t fill, uint32_t pieces, bool nt) {
   constexpr int V = kPiece<T>, kAhead = BASE ? 4 : 8;
+  if (fill && blockIdx.x >= fill) {
+    const int64_t wg = (int64_t)(blockIdx.x - fill) * gridDim.y + blockIdx.y;
+    if (nt) fill_rows<FULL, true>(p, pieces, wg);
+    else fill_rows<FULL, false>(p, pieces, wg);
+    return;
+  }
   const int64_t c = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
   if (c >= p.chunks) return;
   const int64_t piece = (int64_t)blockIdx.y * L + threadIdx.x % L, col = piece_col<V, FULL>(piece, p.D);
@@ -406,11 +490,21 @@ template <typename X, typename T> hipError_t forward(const EmbedParams& p, hipSt
   return full(p, kPiece<T>) ? forward<X, T, true>(p, stream) : forward<X, T, false>(p, stream);
 }
 
+// Workgroups that write the rows without a token (in place: none).
+int64_t fill_wgs(const EmbedParams& p) {
+  const int64_t pieces = (p.D + 3) / 4, count = p.base == p.dtable ? 0 : p.V * pieces;
+  return (count + kThreads * kFillPieces - 1) / (kThreads * kFillPieces);
+}
+bool nt_table(const EmbedParams& p) { return p.V * p.D * 4 > kNtBytes; }
+
 template <typename T, int L, bool FULL> hipError_t sums(const EmbedParams& p, hipStream_t stream) {
   constexpr int V = kPiece<T>, sub = kThreads / L;
-  const dim3 grid((uint32_t)((p.chunks + sub - 1) / sub), (uint32_t)((p.D + L * V - 1) / (L * V)));
-  if (p.base) hipLaunchKernelGGL((embed_sums_kernel<T, L, FULL, true>), grid, dim3(kThreads), 0, stream, p);
-  else hipLaunchKernelGGL((embed_sums_kernel<T, L, FULL, false>), grid, dim3(kThreads), 0, stream, p);
+  dim3 grid((uint32_t)((p.chunks + sub - 1) / sub), (uint32_t)((p.D + L * V - 1) / (L * V)));
+  const uint32_t fill = p.n <= kRankTokens ? grid.x : 0;
+  if (fill) grid.x += (uint32_t)((fill_wgs(p) + grid.y - 1) / grid.y);
+  const uint32_t pieces = (uint32_t)((p.D + 3) / 4);
+  if (p.base) hipLaunchKernelGGL((embed_sums_kernel<T, L, FULL, true>), grid, dim3(kThreads), 0, stream, p, fill, pieces, nt_table(p));
+  else hipLaunchKernelGGL((embed_sums_kernel<T, L, FULL, false>), grid, dim3(kThreads), 0, stream, p, fill, pieces, nt_table(p));
   return hipGetLastError();
 }
 template <typename T, bool FULL> hipError_t sums(const EmbedParams& p, hipStream_t stream) {
@@ -431,14 +525,15 @@ template <int ROUNDS, bool FULL> hipError_t sort_and_fill(const EmbedParams& p, 
   hipLaunchKernelGGL(embed_sort1_kernel<ROUNDS>, dim3(p.tiles), dim3(kThreads), lds1, stream, p);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int64_t pieces = (p.D + 3) / 4, count = p.base == p.dtable ? 0 : p.V * pieces;
-  const int64_t wgs = (count + kThreads * kFillPieces - 1) / (kThreads * kFillPieces);
-  if (p.V * p.D * 4 > kNtBytes)
-    hipLaunchKernelGGL((embed_sort2_kernel<ROUNDS, FULL, true>), dim3((uint32_t)(p.tiles + wgs)), dim3(kThreads), lds2, stream, p,
-                       (uint32_t)pieces);
-  else
-    hipLaunchKernelGGL((embed_sort2_kernel<ROUNDS, FULL, false>), dim3((uint32_t)(p.tiles + wgs)), dim3(kThreads), lds2, stream, p,
-                       (uint32_t)pieces);
+  const dim3 grid((uint32_t)(p.tiles + fill_wgs(p)));
+  const uint32_t pieces = (uint32_t)((p.D + 3) / 4);
+  if (nt_table(p)) hipLaunchKernelGGL((embed_sort2_kernel<ROUNDS, FULL, true>), grid, dim3(kThreads), lds2, stream, p, pieces);
+  else hipLaunchKernelGGL((embed_sort2_kernel<ROUNDS, FULL, false>), grid, dim3(kThreads), lds2, stream, p, pieces);
+  return hipGetLastError();
+}
+hipError_t rank(const EmbedParams& p, hipStream_t stream) {
+  const int64_t words = p.V / 32 + 1, wgs = max((p.n + kRanked - 1) / kRanked, (words + kRankWords - 1) / kRankWords);
+  hipLaunchKernelGGL(embed_rank_kernel, dim3((uint32_t)wgs), dim3(kThreads), 0, stream, p);
   return hipGetLastError();
 }
 
@@ -447,7 +542,8 @@ template <typename T> hipError_t backward(const EmbedParams& p, hipStream_t stre
   constexpr int V = kPiece<T>;
   static_assert(kEmbedTile == 4 * 64 * kWaves && kEmbedLargeTile == 16 * 64 * kWaves, "rounds of a wave");
   hipError_t e;
-  if (p.tile == kEmbedTile) e = full(p, 4) ? sort_and_fill<4, true>(p, stream) : sort_and_fill<4, false>(p, stream);
+  if (p.n <= kRankTokens) e = rank(p, stream);
+  else if (p.tile == kEmbedTile) e = full(p, 4) ? sort_and_fill<4, true>(p, stream) : sort_and_fill<4, false>(p, stream);
   else e = full(p, 4) ? sort_and_fill<16, true>(p, stream) : sort_and_fill<16, false>(p, stream);
   if (e != hipSuccess) return e;
   e = full(p, V) ? sums<T, true>(p, stream) : sums<T, false>(p, stream);
@@ -469,7 +565,8 @@ size_t embed_plan(EmbedParams& p, int64_t tokens, unsigned char* ws) {
   p.n = tokens;
   p.tile = tokens <= 65536 ? kEmbedTile : kEmbedLargeTile;
   p.tiles = (int32_t)((tokens + p.tile - 1) / p.tile);
-  p.chunk = tokens <= 8192 ? 8 : 16;   // (few tokens: more groups of lanes)
+  // (few tokens: more groups of lanes; up to 64 in two chunks, which leave no parts to be added)
+  p.chunk = tokens <= 64 ? 32 : tokens <= 8192 ? 8 : 16;
   while (p.chunk * 4096 < tokens) p.chunk *= 2;
   p.chunks = (int32_t)((tokens + p.chunk - 1) / p.chunk);
   size_t off = 0;
@@ -478,10 +575,13 @@ size_t embed_plan(EmbedParams& p, int64_t tokens, unsigned char* ws) {
     off += (bytes + 255) / 256 * 256;
     return at;
   };
-  p.count1 = reinterpret_cast<int32_t*>(take(4 * ((size_t)p.tiles << p.bits1)));
-  p.count2 = reinterpret_cast<int32_t*>(take(4 * ((size_t)p.tiles << p.bits2)));
   p.present = reinterpret_cast<uint32_t*>(take(4 * (size_t)(p.V / 32 + 1)));
-  for (int32_t** a : {&p.key1, &p.pos1, &p.key, &p.pos}) *a = reinterpret_cast<int32_t*>(take(4 * (size_t)tokens));
+  for (int32_t** a : {&p.key, &p.pos}) *a = reinterpret_cast<int32_t*>(take(4 * (size_t)tokens));
+  if (tokens > kRankTokens) {
+    p.count1 = reinterpret_cast<int32_t*>(take(4 * ((size_t)p.tiles << p.bits1)));
+    p.count2 = reinterpret_cast<int32_t*>(take(4 * ((size_t)p.tiles << p.bits2)));
+    for (int32_t** a : {&p.key1, &p.pos1}) *a = reinterpret_cast<int32_t*>(take(4 * (size_t)tokens));
+  }
   p.part = reinterpret_cast<float*>(take(p.chunks < 3 ? 0 : 8 * (size_t)p.chunks * (size_t)p.D));
   return off;
 }

@@ -193,3 +193,26 @@ def test_numbers_in_tensors(device):
     scale.fill_(2.0)
     assert torch.equal(rla.rla_embed_forward(ids, table, scale), 2 * table)
     assert torch.equal(rla.rla_embed_backward(ids, table, torch.tensor(10), scale), 2 * table)
+
+
+@pytest.mark.parametrize("wide", [True, False])
+@pytest.mark.parametrize("V", [1, 5, 40000, (1 << 22) - 1])
+@pytest.mark.parametrize("n", [1, 31, 33, 64, 65, 129, 2047, 6144, 6145])
+def test_places(device, n, V, wide):
+    """Few tokens, whose places are counted, and the first that are sorted: sums are of whole
+    numbers, so that any order gives the same."""
+    D = 3 if V > 50000 else 12
+    g = torch.Generator(device).manual_seed(n + V)
+    ids = torch.randint(-1, V + 1, (n,), device=device, generator=g)
+    ids[n // 2:] = torch.where(torch.rand(n - n // 2, device=device, generator=g) < 0.3, ids[n // 2], ids[n // 2:])
+    dout = torch.randint(-8, 9, (n, D), device=device, generator=g).float()
+    there = (ids >= 0) & (ids < V)
+    want = torch.zeros(V, D, dtype=torch.float64, device=device).index_add_(0, ids[there], dout[there].double()).float()
+    given = ids if wide else ids.int()
+    table = torch.full((V, D), float("nan"), device=device)
+    assert torch.equal(rla.rla_embed_backward(given, dout, V, dtable=table), want)
+    base = torch.randint(-99, 99, (V, D), device=device, generator=g).float()
+    assert torch.equal(rla.rla_embed_backward(given, dout.bfloat16(), V, base=base), want + base)
+    assert torch.equal(rla.rla_embed_backward(given, dout, V, scale=2.0, base=base, dtable=base.clone()), 2 * want + base)
+    same = base.clone()
+    assert torch.equal(rla.rla_embed_backward(given, dout, V, base=same, dtable=same), want + base)
