@@ -234,28 +234,28 @@ __global__ __launch_bounds__(kThreads) void embed_sort2_kernel(EmbedParams p, ui
 // token, kRankWords words of bits each.  One launch for three, whose 2 n^2 operations are 2.3 us of the
 // card's at 6144 tokens.  The whole gradient, us, against the counting sort: 6 tokens 10.3 (15.5), 600 13.9 (20.1),
 // 3000 16.2 (21.7; 32768 x 1024: 34.5, 42.6), 6000 42.5 (44.6), 8000 26.7 (25.6).
-constexpr int kRankTokens = 6144, kRanked = 32, kRankWords = 1024;
-__global__ __launch_bounds__(kThreads) void embed_rank_kernel(EmbedParams p) {
+constexpr int kRankTokens = 8192, kRankThreads = 1024, kRanked = 32, kRankWords = 1024;
+__global__ __launch_bounds__(kRankThreads) void embed_rank_kernel(EmbedParams p) {
   __shared__ uint4 keys[kRankTokens / 4];
   __shared__ uint32_t bits[kRankWords];
-  __shared__ int32_t counts[kThreads / kRanked][kRanked];
+  __shared__ int32_t counts[kRankThreads / kRanked][kRanked];
   uint32_t* key = reinterpret_cast<uint32_t*>(keys);
-  const int tid = threadIdx.x, n = (int)p.n, slices = kThreads / kRanked;
+  const int tid = threadIdx.x, n = (int)p.n, slices = kRankThreads / kRanked;
   const int all = (n + 4 * slices - 1) / (4 * slices) * (4 * slices);   // (whole reads of 4 for each slice; past n: behind all)
   const uint32_t word0 = blockIdx.x * kRankWords;
-  for (int i = tid; i < kRankWords; i += kThreads) bits[i] = 0;
+  for (int i = tid; i < kRankWords; i += kRankThreads) bits[i] = 0;
   __syncthreads();
   auto load = [&](auto type) {
     typedef decltype(type) Id;
     const Id* ids = reinterpret_cast<const Id*>(p.ids.p);
-    constexpr int kAhead = 8;
-    for (int i0 = tid; i0 < all; i0 += kAhead * kThreads) {
+    constexpr int kAhead = 4;
+    for (int i0 = tid; i0 < all; i0 += kAhead * kRankThreads) {
       Id id[kAhead];
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) id[u] = ids[min(i0 + u * kThreads, n - 1)];
+      for (int u = 0; u < kAhead; ++u) id[u] = ids[min(i0 + u * kRankThreads, n - 1)];
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        const int i = i0 + u * kThreads;
+        const int i = i0 + u * kRankThreads;
         const bool row = id[u] >= 0 && id[u] < p.V;
         const uint32_t k = row ? (uint32_t)id[u] : (uint32_t)p.V, word = (k >> 5) - word0;
         if (i < all) key[i] = i < n ? k : 0xffffffffu;
@@ -281,9 +281,9 @@ __global__ __launch_bounds__(kThreads) void embed_rank_kernel(EmbedParams p) {
       count += k.z < below ? 1 : 0;
       count += k.w < below ? 1 : 0;
     }
-    static_assert(kRanked == 4 * (kThreads / kRanked), "a read of 4 for each slice");
+    static_assert(kRanked <= 4 * (kRankThreads / kRanked), "the workgroup's own tokens: a read of 4 a slice");
     const int g = block + slice, j = 4 * g;
-    if (j < i) {
+    if (j < i) {   // (slices behind the workgroup's tokens: never)
       const uint4 k = keys[g];
       count += k.x == own ? 1 : 0;
       count += k.y == own && j + 1 < i ? 1 : 0;
@@ -299,7 +299,7 @@ __global__ __launch_bounds__(kThreads) void embed_rank_kernel(EmbedParams p) {
     p.key[rank] = (int32_t)own;
     p.pos[rank] = i;
   }
-  for (int64_t w = tid; w < kRankWords && word0 + w <= p.V / 32; w += kThreads) p.present[word0 + w] = bits[w];
+  for (int64_t w = tid; w < kRankWords && word0 + w <= p.V / 32; w += kRankThreads) p.present[word0 + w] = bits[w];
 }
 
 // ---------------------------------------------------------------------------
@@ -533,7 +533,7 @@ template <int ROUNDS, bool FULL> hipError_t sort_and_fill(const EmbedParams& p, 
 }
 hipError_t rank(const EmbedParams& p, hipStream_t stream) {
   const int64_t words = p.V / 32 + 1, wgs = max((p.n + kRanked - 1) / kRanked, (words + kRankWords - 1) / kRankWords);
-  hipLaunchKernelGGL(embed_rank_kernel, dim3((uint32_t)wgs), dim3(kThreads), 0, stream, p);
+  hipLaunchKernelGGL(embed_rank_kernel, dim3((uint32_t)wgs), dim3(kRankThreads), 0, stream, p);
   return hipGetLastError();
 }
 

@@ -197,7 +197,7 @@ def test_numbers_in_tensors(device):
 
 @pytest.mark.parametrize("wide", [True, False])
 @pytest.mark.parametrize("V", [1, 5, 40000, (1 << 22) - 1])
-@pytest.mark.parametrize("n", [1, 31, 33, 64, 65, 129, 2047, 6144, 6145])
+@pytest.mark.parametrize("n", [1, 31, 33, 64, 65, 129, 2047, 6144, 6145, 8192, 8193])
 def test_places(device, n, V, wide):
     """Few tokens, whose places are counted, and the first that are sorted: sums are of whole
     numbers, so that any order gives the same."""
