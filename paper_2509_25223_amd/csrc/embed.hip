@@ -15,7 +15,7 @@
 // Then:
 //   embed_sums    a group of lanes takes `chunk` sorted tokens and writes the sums of the ids
 //                 that start there and end there or in the next chunk; of longer runs
-//                 each chunk leaves its part (few tokens: other workgroups write the rows without one)
+//                 each chunk leaves its part (few tokens: others write the rows without one)
 //   embed_join    adds these parts
 // 16384 tokens as frequent as words, 32768 x 2048, bf16 rows into an fp32 table, us: 4.7, 8.9, 43.7 (224 MB of
 // zeros at 5.1 TB/s, the second pass beside them), 27 (67 MB read at random, 45 written), 6.3; all bytes
@@ -230,10 +230,11 @@ __global__ __launch_bounds__(kThreads) void embed_sort2_kernel(EmbedParams p, ui
 }
 
 // Up to kRankTokens: a token's place is the number of tokens before it in the order, counted over all of
-// them, kRanked tokens a workgroup, 8 lanes each.  The same workgroups find the rows that have a
-// token, kRankWords words of bits each.  One launch for three, whose 2 n^2 operations are 2.3 us of the
-// card's at 6144 tokens.  The whole gradient, us, against the counting sort: 6 tokens 10.3 (15.5), 600 13.9 (20.1),
-// 3000 16.2 (21.7; 32768 x 1024: 34.5, 42.6), 6000 42.5 (44.6), 8000 26.7 (25.6).
+// them, kRanked tokens a workgroup, 32 lanes each.  The same workgroups find the rows that have a
+// token, kRankWords words of bits each.  One launch for three, whose 2 n^2 operations are 4 us of the
+// card's at 8192 tokens (4099: 6.1 us in all).  The whole gradient, us, against the counting sort: 6 tokens
+// 10.3 (15.5), 600 of 64 values 14.3 (20.1), 3000 14.4 (21.7), 8000 17.7 (25.5), 8192 of 1024 40 (46); on from
+// there, 64 tokens a workgroup: 12288 of 1024 53 (50), 16384 60 (52).
 constexpr int kRankTokens = 8192, kRankThreads = 1024, kRanked = 32, kRankWords = 1024;
 __global__ __launch_bounds__(kRankThreads) void embed_rank_kernel(EmbedParams p) {
   __shared__ uint4 keys[kRankTokens / 4];
