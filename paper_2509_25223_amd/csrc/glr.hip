@@ -24,7 +24,8 @@
 // What bounds it: HBM and the vector ALU together.  bf16, both gates, normalized, 4 x 4096 x 4096:
 // forward 178 us (671 MB, 3.8 TB/s; vector ALUs busy 55 % of the time), backward 279 (1.2 GB, 4.3 TB/s),
 // whose 2 channels x 8 tokens x 7 values take 256 registers: two waves a SIMD.  Measured there and not kept:
-// 16 waves a workgroup and loads a tile further ahead (the same time), 16 tokens a stretch (spills).
+// 16 waves a workgroup and loads a tile further ahead (the same time), 16 tokens a stretch (spills), two
+// workgroups a CU of 32 channels each, half lines (forward 205 us, backward 336).
 // Loads behind branches, in turn waited for one by one, had cost three times as much (1283 us, now 447).
 #include <math.h>
 
