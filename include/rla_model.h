@@ -69,7 +69,9 @@ rla_status rla_embed_backward(const rla_embed_problem *problem, const void *ids,
  *   top      the `top` largest logits, equal ones by their place, as log
  *            probabilities and ids; -inf and -1 where fewer have a probability
  * -inf is a logit without a probability.  A row of nothing else has lse = -inf,
- * entropy 0 and log probability -inf.  NaN or +inf in a row gives that row NaN
+ * entropy 0, log probability -inf and a gradient of zeros.  Where scale times finite
+ * logits leaves fp32, lse alone is infinite: everything else is taken from the
+ * logits' differences.  NaN or +inf in a row gives that row NaN
  * (lse, log probability, entropy and those of its alternatives; which ids they
  * have is then not said).
  * ------------------------------------------------------------------------ */

@@ -426,7 +426,8 @@ template <typename T, bool TOP> __global__ __launch_bounds__(kThreads) void logp
 // ---------------------------------------------------------------------------
 // The log probability z - lse is off by half a step of lse: 1.5e-5 at 256.  Rows farther out
 // (large logits, a row at the type's lowest value) are read once more for their largest value and
-// the logarithm of the sum beside it.
+// the logarithm of the sum beside it; among them those whose lse is infinite, be it that scale times
+// finite logits is, or that they hold nothing but -inf (then mx is).
 constexpr float kFarLse = 256.f;
 template <typename T, int L> __device__ __forceinline__ void far_row(const LogprobParams& p, const T* x, float& mx, float& ln) {
   __shared__ float slots[2][kWaves];
@@ -439,7 +440,8 @@ template <typename T, int L> __device__ __forceinline__ void far_row(const Logpr
     __syncthreads();
     m = over(slots[0], Max());
   }
-  for (int64_t j = threadIdx.x % L; j < p.V; j += L) s += __builtin_amdgcn_exp2f((to_f<T>(x[j]) - m) * k);
+  const float m0 = m == -kInf ? 0.f : m;
+  for (int64_t j = threadIdx.x % L; j < p.V; j += L) s += __builtin_amdgcn_exp2f((to_f<T>(x[j]) - m0) * k);
   s = wave_sum(s);
   if constexpr (L > 64) {
     if ((threadIdx.x & 63) == 0) slots[1][threadIdx.x >> 6] = s;
@@ -477,7 +479,7 @@ __global__ __launch_bounds__(kThreads) void logprob_bwd_kernel(LogprobParams p, 
     de = p.dentropy[row];
     H = p.entropy_in[row];
   }
-  const bool none = lse == -kInf;
+  bool none = false;   // nothing but -inf
   float mx = 0.f, ln = lse;
   auto write = [&](int64_t c, float (&v)[V]) {
 #pragma unroll
@@ -490,10 +492,11 @@ __global__ __launch_bounds__(kThreads) void logprob_bwd_kernel(LogprobParams p, 
     }
     store_piece<T, V, false, NT>(dx + c, (int)min(p.V - c, (int64_t)V), v);
   };
-  if (__builtin_fabsf(lse) > kFarLse && __builtin_fabsf(lse) < kInf) {
+  if (__builtin_fabsf(lse) > kFarLse) {
     // by its first lanes alone: in place, others would write what these read again
     if (seg > 0) return;
     far_row<T, L>(p, x, mx, ln);
+    none = mx == -kInf;
     for (int64_t c = threadIdx.x % L * V; c < p.V; c += L * V) {
       float v[V];
       load_piece<T, V>(x + c, (int)min(p.V - c, (int64_t)V), v);

@@ -364,3 +364,30 @@ def test_more_long_rows_than_a_launch(device):
     check_forward({k: f[k][some] for k in ("lse", "logprob")}, ref.logprob(near.cpu().double(), y.cpu(), 1.0, 0), 0, entropy=False)
     f["lse"][some] = f["lse"][1].item()
     assert (f["lse"] == f["lse"][1]).all()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("V", [50, 3000, 20001, 200003])
+@pytest.mark.parametrize("scale", [1.43, 2.0])
+def test_gradient_where_lse_overflows(device, dtype, V, scale):
+    """Finite logits whose lse, times the scale, leaves fp32: the probabilities are those of the
+    differences, as in the forward; rows without any keep their zeros."""
+    x, y, gen = rows(6, V, dtype, seed=V)
+    least, most = torch.finfo(TYPES[dtype]).min, torch.finfo(TYPES[dtype]).max
+    x[0] = least
+    x[1] = most
+    x[2, 1:], x[2, 0] = most, 0.0
+    x[3, 1:], x[3, 0] = NEG, least
+    x[4] = NEG
+    y[2], y[3] = 0, 0
+    g, e = torch.randn(6, generator=gen).to(device), torch.randn(6, generator=gen).to(device)
+    f = rla.rla_logprob_forward(x, y, scale=scale, entropy=True)
+    assert (f["lse"][[0, 3, 4]] == NEG).all() and (f["lse"][[1, 2]] == -NEG).all()
+    # (the rows shifted to a maximum of 0; values 1e4 below have no probability)
+    near = (x.double() - x.double().amax(-1, keepdim=True)).clamp(min=-1e4)
+    near[4] = NEG
+    want, allowed = gradient(near, y, scale, g, e)
+    want[4] = 0
+    allowed += 2.0 ** -8 * want.abs() if dtype == "bf16" else 0
+    close("dlogits", rla.rla_logprob_backward(x, f["lse"], y, g, f["entropy"], e, scale=scale), want, allowed)
+    close("in place", rla.rla_logprob_backward(x, f["lse"], y, g, f["entropy"], e, scale=scale, out=x), want, allowed)
