@@ -97,7 +97,8 @@ rla_status rla_logprob_forward(const rla_logprob_problem *problem, const void *l
                                void *workspace, size_t workspace_bytes, void *stream);
 
 /* dlogits [n, V]: gradients of <dlogprob, logprob> + <dentropy, entropy> from the
- * lse and entropy that the forward wrote:
+ * lse and entropy that the forward wrote (fp32: what rounding lse costs p is made
+ * good from the row, where it has more than 20480 logits if |lse| > 32):
  *   scale * (dlogprob (1[j = y] - p_j) - dentropy p_j (z_j - lse + entropy))
  * with a row's first part 0 where it is left out.  dlogprob (then targets) and
  * dentropy (then entropy) may be NULL: zeros.  dlogits may be logits (in place,

@@ -19,6 +19,8 @@
 // (a few hundred neighbouring tokens allowed), then, if that does not do (equal large logits), by
 // bisection until exactly `top` reach it (64 rows of 131072, eight alternatives: 16 us; 500 allowed
 // tokens in each 30; all equal 135).
+//
+// The gradient recomputes p from lse, and holds a row in the same way (below).
 #include "model.hpp"
 
 namespace rla {
@@ -421,91 +423,167 @@ template <typename T, bool TOP> __global__ __launch_bounds__(kThreads) void logp
 }
 
 // ---------------------------------------------------------------------------
-// Gradient: L lanes a row, or N pieces a lane of one.  16384 x 32768 of bf16: 430 us, 2.15 GB at the
-// 5.0 TB/s of a large copy (rows from the last one on, for what the forward left in the caches: no gain).
+// Gradient.  lse is rounded to fp32, so e^(z - lse) is off by up to half a step of it: 1.9e-6 at 63,
+// 7.6e-6 at 255.  The row's own sum of these, by which they are divided, takes that out, and what the
+// shift c and the factor k are off by.  Rows farther out (large logits, a row at the type's lowest
+// value; an infinite lse: scale times finite logits is, or there is nothing but -inf) take the
+// differences from their largest value instead.
 // ---------------------------------------------------------------------------
-// The log probability z - lse is off by half a step of lse: 1.5e-5 at 256.  Rows farther out
-// (large logits, a row at the type's lowest value) are read once more for their largest value and
-// the logarithm of the sum beside it; among them those whose lse is infinite, be it that scale times
-// finite logits is, or that they hold nothing but -inf (then mx is).
 constexpr float kFarLse = 256.f;
-template <typename T, int L> __device__ __forceinline__ void far_row(const LogprobParams& p, const T* x, float& mx, float& ln) {
-  __shared__ float slots[2][kWaves];
-  const float k = p.scale * kLog2e;
-  float m = -kInf, s = 0.f;
-  for (int64_t j = threadIdx.x % L; j < p.V; j += L) m = fmaxf(m, to_f<T>(x[j]));
-  m = wave_max(m);
-  if constexpr (L > 64) {
-    if ((threadIdx.x & 63) == 0) slots[0][threadIdx.x >> 6] = m;
-    __syncthreads();
-    m = over(slots[0], Max());
+// Of one row: log2 p = (x - b) k - c - log2 s.  g and de hold the factor `scale`, and in gs, des that of 1 / s.
+struct RowGradient {
+  float lse, k, b = 0.f, c, g = 0.f, gs, de = 0.f, des, H = 0.f;
+  int y = -1;
+  bool far, entropy;
+  __device__ __forceinline__ RowGradient(const LogprobParams& p, int64_t row)
+      : lse(p.lse_in[row]), k(p.scale * kLog2e), c(lse * kLog2e), far(__builtin_fabsf(lse) > kFarLse), entropy(p.dentropy) {
+    if (p.dlogprob) {
+      const int64_t t = p.targets[row];
+      if (t >= 0 && t < p.V) {
+        y = (int)t;
+        g = p.dlogprob[row] * p.scale;
+      }
+    }
+    if (entropy) {
+      de = p.dentropy[row] * p.scale;
+      H = p.entropy_in[row];
+    }
+    gs = g;
+    des = de;
   }
-  const float m0 = m == -kInf ? 0.f : m;
-  for (int64_t j = threadIdx.x % L; j < p.V; j += L) s += __builtin_amdgcn_exp2f((to_f<T>(x[j]) - m0) * k);
-  s = wave_sum(s);
-  if constexpr (L > 64) {
-    if ((threadIdx.x & 63) == 0) slots[1][threadIdx.x >> 6] = s;
-    __syncthreads();
-    s = over(slots[1], Add());
+  __device__ __forceinline__ void from(float mx) {
+    b = mx;
+    c = 0.f;
+    if (mx == -kInf) b = g = gs = de = des = 0.f;   // nothing but -inf
   }
-  mx = m;
-  ln = logf(s);
+  __device__ __forceinline__ float log2_of(float x) const { return __builtin_fmaf(x - b, k, -c); }
+  __device__ __forceinline__ float term(float x) const { return __builtin_amdgcn_exp2f(log2_of(x)); }
+  // The row's sum of terms.  Further from 1 than the roundings (lse, k and c a step each at most, the sum
+  // 128 half steps), the lse given is not of this row alone, and stands.
+  __device__ __forceinline__ void divide(float s) {
+    if (s == 0.f || (!far && !(__builtin_fabsf(s - 1.f) <= __builtin_fmaf(__builtin_fabsf(lse), 0x1p-21f, 0x1p-17f)))) return;
+    gs = g / s;
+    des = de / s;
+    H -= logf(s);   // (what is added to log p)
+  }
+  template <typename T, int V, typename Raw>
+  __device__ __forceinline__ void write(T* dx, int col, int width, Raw raw, int nt) const {
+    float d[V];
+    if (entropy) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float t = log2_of(to_f<T>(raw[e]));
+        d[e] = -__builtin_amdgcn_exp2f(t) * __builtin_fmaf(des, __builtin_fmaf(fmaxf(t, -1000.f), kLn2, H), gs);   // (0 times -inf)
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e) d[e] = -term(to_f<T>(raw[e])) * gs;
+    }
+    const uint32_t at = (uint32_t)(y - col);
+    if (at < (uint32_t)V)
+#pragma unroll
+      for (int e = 0; e < V; ++e) d[e] += (uint32_t)e == at ? g : 0.f;
+    if (nt) store_piece<T, V, false, true>(dx + col, width - col, d);
+    else store_piece<T, V, false, false>(dx + col, width - col, d);
+  }
+};
+template <int L, typename Op> __device__ __forceinline__ float over_row(float a, float* slots, Op op) {
+  if constexpr (L > 64) {
+    if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = a;
+    __syncthreads();
+    a = slots[0];
+#pragma unroll
+    for (int w = 1; w < L / 64; ++w) a = op(a, slots[w]);
+  }
+  return a;
 }
 
-template <typename T, int L, int N, bool NT>
-__global__ __launch_bounds__(kThreads) void logprob_bwd_kernel(LogprobParams p, int64_t first, uint32_t segs) {
-  constexpr int V = kPiece<T>, kSub = kThreads / L;
-  const int64_t id = first + (int64_t)blockIdx.x * kSub + threadIdx.x / L;
-  const int64_t row = id / segs;
-  if (row >= p.n) return;
-  const int64_t seg = id - row * segs, c0 = seg * (L * N * V) + (threadIdx.x % L) * V;
+// L lanes a row, which they hold, N pieces each: read once, written once.
+template <typename T, int L, int N>
+__global__ __launch_bounds__(L > kThreads ? L : kThreads, L == 1024 ? 8 : 1)
+void logprob_bwd_kernel(LogprobParams p, int64_t first, int nt) {
+  constexpr int V = kPiece<T>, kSub = L > kThreads ? 1 : kThreads / L;
+  __shared__ float slots[2][L / 64];
+  const int lane = threadIdx.x % L, width = (int)p.V;
+  const int64_t row = first + (int64_t)blockIdx.x * kSub + threadIdx.x / L;
+  if (row >= p.n) return;   // (whole rows of lanes)
+  Part<T, L, N> v;
+  v.load(reinterpret_cast<const T*>(p.x) + row * p.xs, width, lane);
+  RowGradient r(p, row);
+  if (r.far) {
+    float mx = -kInf;
+    v.each([&](int, int, float z) { mx = fmaxf(mx, z); });
+    r.from(over_row<L>(wave_max(mx), slots[0], Max()));
+  }
+  float s = 0.f;
+  v.again();
+  v.each([&](int, int, float z) { s += r.term(z); });
+  r.divide(over_row<L>(wave_sum(s), slots[1], Add()));
+  v.again();
+  T* dx = reinterpret_cast<T*>(p.dx) + row * p.V;
+#pragma unroll
+  for (int j = 0; j < N; ++j) r.write<T, V>(dx, v.col(j, lane), width, v.raw[j], nt);
+}
+
+// Longer rows: a workgroup a piece a lane, many a row, which trust its lse as far as it costs no more than
+// the exponents' own rounding (fp32: to 32, half a step 9.5e-7) or the outputs' (bf16: to 256, 2^-8 of theirs).  Any
+// other row is left to one of its workgroups (in place, others would write what it reads again; not to the
+// first, which for 8 n workgroups a row would all lie on one XCD), and read twice, far out three times.
+constexpr int kLongLanes = 1024;
+template <typename T> constexpr float kTrustedLse = sizeof(T) == 4 ? 32.f : kFarLse;
+template <typename T> __global__ __launch_bounds__(kLongLanes, 8) void logprob_bwd_long_kernel(LogprobParams p, int64_t first, uint32_t segs, int nt) {
+  constexpr int L = kLongLanes, V = kPiece<T>, kSpan = L * V, kAhead = 4;
+  typedef typename RowVec<T, V>::type Vec;
+  __shared__ float slots[2][L / 64];
+  const int64_t id = first + blockIdx.x, row = id / segs;
+  const int seg = (int)(id - row * segs), width = (int)p.V, lane = threadIdx.x;
   const T* x = reinterpret_cast<const T*>(p.x) + row * p.xs;
   T* dx = reinterpret_cast<T*>(p.dx) + row * p.V;
-  float in[N][V];
+  // the lane's N pieces from column c0 on, -inf past the row's end (loads without branches: there its last piece)
+  auto load = [&](int c0, auto& raw) {
+    constexpr int N = sizeof(raw) / sizeof(Vec);
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const int64_t c = c0 + j * (L * V);
-    load_piece<T, V>(x + c, (int)min(p.V - c, (int64_t)V), in[j]);
-  }
-  const float lse = p.lse_in[row];
-  int64_t y = -1;
-  float g = 0.f, de = 0.f, H = 0.f;
-  if (p.dlogprob) {
-    y = p.targets[row];
-    if (y >= 0 && y < p.V) g = p.dlogprob[row];
-    else y = -1;
-  }
-  if (p.dentropy) {
-    de = p.dentropy[row];
-    H = p.entropy_in[row];
-  }
-  bool none = false;   // nothing but -inf
-  float mx = 0.f, ln = lse;
-  auto write = [&](int64_t c, float (&v)[V]) {
+    for (int u = 0; u < N; ++u) raw[u] = *reinterpret_cast<const Vec*>(x + min(c0 + u * kSpan, width - V));
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const float d = __builtin_fmaf(v[e] - mx, p.scale, -ln);   // log p
-      const float pr = __builtin_amdgcn_exp2f(d * kLog2e);
-      float t = -pr * __builtin_fmaf(de, fmaxf(d, -1000.f) + H, g);
-      if (c + e == y) t += g;
-      v[e] = none ? 0.f : t * p.scale;
+    for (int u = 0; u < N; ++u) {
+      const int c = c0 + u * kSpan, left = width - c;
+      if (left >= V) continue;
+#pragma unroll
+      for (int e = 0; e < V; ++e) raw[u][e] = e < left ? x[c + e] : from_f<T>(-kInf);
     }
-    store_piece<T, V, false, NT>(dx + c, (int)min(p.V - c, (int64_t)V), v);
   };
-  if (__builtin_fabsf(lse) > kFarLse) {
-    // by its first lanes alone: in place, others would write what these read again
-    if (seg > 0) return;
-    far_row<T, L>(p, x, mx, ln);
-    none = mx == -kInf;
-    for (int64_t c = threadIdx.x % L * V; c < p.V; c += L * V) {
-      float v[V];
-      load_piece<T, V>(x + c, (int)min(p.V - c, (int64_t)V), v);
-      write(c, v);
-    }
+  Vec raw[1];
+  const int own = seg * kSpan + lane * V;
+  load(own, raw);
+  RowGradient r(p, row);
+  if (!(__builtin_fabsf(r.lse) > kTrustedLse<T>)) {
+    r.write<T, V>(dx, own, width, raw[0], nt);
     return;
   }
+  if (seg != (int)(row % segs)) return;
+  auto all = [&](auto f) {
+    for (int c0 = lane * V; c0 < width; c0 += kAhead * kSpan) {
+      Vec z[kAhead];
+      load(c0, z);
 #pragma unroll
-  for (int j = 0; j < N; ++j) write(c0 + j * (L * V), in[j]);
+      for (int u = 0; u < kAhead; ++u) f(c0 + u * kSpan, z[u]);
+    }
+  };
+  if (r.far) {
+    float mx = -kInf;
+    all([&](int, Vec z) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) mx = fmaxf(mx, to_f<T>(z[e]));
+    });
+    r.from(over_row<L>(wave_max(mx), slots[0], Max()));
+  }
+  float s = 0.f;
+  all([&](int, Vec z) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) s += r.term(to_f<T>(z[e]));
+  });
+  r.divide(over_row<L>(wave_sum(s), slots[1], Add()));
+  all([&](int c, Vec z) { r.write<T, V>(dx, c, width, z, nt); });
 }
 
 // ---------------------------------------------------------------------------
@@ -562,23 +640,51 @@ template <typename T> hipError_t forward(const LogprobParams& p, hipStream_t str
   return hipGetLastError();
 }
 
-template <typename T, int L, int N> hipError_t backward(const LogprobParams& p, hipStream_t stream) {
-  constexpr int V = kPiece<T>;
-  const int64_t sub = kThreads / L, segs = (p.V + L * N * V - 1) / (L * N * V), wgs = (p.n * segs + sub - 1) / sub;
-  const bool nt = p.n * p.V * (int64_t)sizeof(T) > kNtBytes;
-  constexpr int64_t most = kMaxLanes / kThreads;
+// `launch` for all of `wgs` workgroups, from workgroup w on: as many as a launch holds at a time.
+template <typename F> hipError_t backward_launches(int64_t wgs, int64_t threads, F launch) {
+  const int64_t most = kMaxLanes / threads;
   for (int64_t w = 0; w < wgs; w += most) {
-    const dim3 grid((uint32_t)min(wgs - w, most));
-    if (nt) hipLaunchKernelGGL((logprob_bwd_kernel<T, L, N, true>), grid, dim3(kThreads), 0, stream, p, w * sub, (uint32_t)segs);
-    else hipLaunchKernelGGL((logprob_bwd_kernel<T, L, N, false>), grid, dim3(kThreads), 0, stream, p, w * sub, (uint32_t)segs);
+    launch(dim3((uint32_t)min(wgs - w, most)), w);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
+template <typename T, int L, int N> hipError_t backward(const LogprobParams& p, int nt, hipStream_t stream) {
+  constexpr int threads = L > kThreads ? L : kThreads, sub = threads / L;
+  return backward_launches((p.n + sub - 1) / sub, threads, [&](dim3 grid, int64_t w) {
+    hipLaunchKernelGGL((logprob_bwd_kernel<T, L, N>), grid, dim3(threads), 0, stream, p, w * sub, nt);
+  });
+}
+// Lanes of a row, as many as hold it in registers for two rows of 1024 on a CU (fp32: 20480 logits, bf16: 40960); of
+// few rows more, for latency.  us: 16384 x 32768 of bf16 415 (2.15 GB, the 5.2 TB/s of a large copy), rows at 400 422;
+// 3000 x 20003 of fp32 76 and 77.  Longer: 4001 x 50001 of bf16 157, at 400 309; 2000 x 151936 of fp32 387, at 100 665, at
+// 400 816; 1 x 131072 of fp32 2.4, 18, 22.
 template <typename T> hipError_t backward(const LogprobParams& p, hipStream_t stream) {
   const int64_t pieces = (p.V + kPiece<T> - 1) / kPiece<T>;
-  return pieces <= 128 ? backward<T, 64, 1>(p, stream) : backward<T, 256, 4>(p, stream);
+  const int nt = p.n * p.V * (int64_t)sizeof(T) > kNtBytes;
+  const bool few = p.n <= kFewRows;
+  if (pieces <= 64) return backward<T, 64, 1>(p, nt, stream);
+  if (!few && pieces <= 128) return backward<T, 64, 2>(p, nt, stream);
+  if (!few && pieces <= 256) return backward<T, 64, 4>(p, nt, stream);
+  if (pieces <= 256) return backward<T, 256, 1>(p, nt, stream);
+  if (pieces <= 512) return backward<T, 256, 2>(p, nt, stream);
+  if (!few && pieces <= 1024) return backward<T, 256, 4>(p, nt, stream);
+  if (!few && pieces <= 1536) return backward<T, 256, 6>(p, nt, stream);
+  // (a few rows of bf16, whose digits are the outputs': sooner done by several workgroups each, 1 x 32768 2.7, not 4.7)
+  if (!few || sizeof(T) == 4) {
+    if constexpr (sizeof(T) == 4)
+      if (pieces <= 1024) return backward<T, 1024, 1>(p, nt, stream);
+    if (pieces <= 2048) return backward<T, 1024, 2>(p, nt, stream);
+    if (pieces <= 3072) return backward<T, 1024, 3>(p, nt, stream);
+    if (pieces <= 4096) return backward<T, 1024, 4>(p, nt, stream);
+    if (pieces <= 5120) return backward<T, 1024, 5>(p, nt, stream);
+  }
+  constexpr int64_t span = kLongLanes * kPiece<T>;
+  const int64_t segs = (p.V + span - 1) / span;
+  return backward_launches(p.n * segs, kLongLanes, [&](dim3 grid, int64_t w) {
+    hipLaunchKernelGGL((logprob_bwd_long_kernel<T>), grid, dim3(kLongLanes), 0, stream, p, w, (uint32_t)segs, nt);
+  });
 }
 
 }  // namespace

@@ -391,3 +391,53 @@ def test_gradient_where_lse_overflows(device, dtype, V, scale):
     allowed += 2.0 ** -8 * want.abs() if dtype == "bf16" else 0
     close("dlogits", rla.rla_logprob_backward(x, f["lse"], y, g, f["entropy"], e, scale=scale), want, allowed)
     close("in place", rla.rla_logprob_backward(x, f["lse"], y, g, f["entropy"], e, scale=scale, out=x), want, allowed)
+
+
+def exact_gradient(x, y, scale, g, e):
+    """(gradient, bound) in 64 bits from the definition.  Half steps of p: of the exponent's three roundings (its
+    factor's two, its own) 3 |log p|, of those of the row's sum 3 H, e^t, 1 / s and products 10, and of the
+    terms added one after the other at most 4 pieces of 8, then 6 in a wave and 16 waves: 54.  log p is off by
+    as much, H by the half step that it is given with, the bracket by rounding."""
+    z = x.cpu().double() * scale
+    lp = z - torch.logsumexp(z, -1, keepdim=True)
+    p, H = lp.exp(), -(lp.exp() * lp).sum(-1, keepdim=True)
+    g, e = g.cpu().double()[:, None], e.cpu().double()[:, None]
+    at = (torch.arange(x.shape[1]) == y.cpu()[:, None]).double()
+    want = scale * (g * (at - p) - e * p * (lp + H))
+    steps = HALF * (64 + 3 * lp.abs() + 3 * H)
+    allowed = scale * p * (steps * (g.abs() + e.abs() * (lp + H).abs()) + e.abs() * (steps + HALF * (2 * H + 2 * lp.abs())))
+    return want, allowed + 4 * HALF * (want.abs() + scale * g.abs() * at), H[:, 0]
+
+
+@pytest.mark.parametrize("V,rows_", [(50, 600), (300, 300), (3000, 60), (20003, 40), (30011, 24)])
+@pytest.mark.parametrize("spread,scale", [(1.0, 1.0), (6.0, 0.75)])
+def test_digits_of_large_lse(device, V, rows_, spread, scale):
+    """A gradient's digits do not go with its row's lse: rows at 30 to 255 and below -30, as exact as near 0 (half a
+    step of lse is up to 128 half steps of p)."""
+    x, y, gen = rows(rows_, V, "f32", seed=V, spread=spread)
+    lse = torch.logsumexp(x.cpu().double() * scale, -1)
+    to = torch.empty(rows_, dtype=torch.float64).uniform_(34, 250, generator=gen) * torch.where(torch.arange(rows_) % 4 == 3, -1, 1)
+    x += ((to - lse) / scale)[:, None].float().to(device)
+    g, e = torch.randn(rows_, generator=gen).to(device), torch.randn(rows_, generator=gen).to(device)
+    want, allowed, H = exact_gradient(x, y, scale, g, e)
+    f = rla.rla_logprob_forward(x, y, scale=scale)
+    assert f["lse"].abs().min() > 32 and f["lse"].abs().max() < 256
+    got = rla.rla_logprob_backward(x, f["lse"], y, g, H.float().to(device), e, scale=scale)
+    close("dlogits", got, want, allowed)
+
+
+def test_part_of_a_vocabulary(device):
+    """The formula's lse stands where it is not the row's own: each half of the columns, with the lse of
+    both, gives its part of the gradient."""
+    x, y, gen = rows(40, 6000, "f32", seed=3)
+    g = torch.randn(40, generator=gen).to(device)
+    f = rla.rla_logprob_forward(x, y)
+    whole = rla.rla_logprob_backward(x, f["lse"], y, g)
+    for a, b in ((0, 2500), (2500, 6000)):
+        own = torch.where((y >= a) & (y < b), y - a, -1)
+        got = rla.rla_logprob_backward(x[:, a:b], f["lse"], own, torch.where(own < 0, 0.0, g))
+        rest = rla.rla_logprob_backward(x[:, a:b], f["lse"], torch.zeros_like(y), torch.where(own < 0, g, 0.0))
+        rest[:, 0] -= torch.where(own < 0, g, 0.0)   # (a row whose token lies elsewhere: the probabilities' part)
+        want = whole[:, a:b].cpu().double()
+        # lse < 16: off by half a step, 2^-21, and 64 more of p's half steps
+        close("part", got + rest, want, 2 ** -20 * want.abs() + HALF * 64 * g.cpu().double().abs()[:, None])
