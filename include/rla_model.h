@@ -154,8 +154,8 @@ rla_status rla_glr_backward(const rla_glr_problem *problem, const void *x, const
                             int use_saved, void *workspace, size_t workspace_bytes, void *stream);
 
 /* T new tokens (a few) of B sequences: h_out [B, D], which may be h_in (in place;
- * h_in NULL: zeros).  No workspace; dense only (RLA_ERR_UNSUPPORTED with
- * cu_seqlens). */
+ * h_in NULL: zeros), as o may be x, r, i or z with rows next to each other.  No
+ * workspace; dense only (RLA_ERR_UNSUPPORTED with cu_seqlens). */
 rla_status rla_glr_decode(const rla_glr_problem *problem, const void *x, const void *r,
                           const float *A, const void *i, const void *z, const float *h_in,
                           void *o, float *h_out, void *stream);

@@ -15,6 +15,33 @@ namespace {
 bool is_index(int32_t t) { return t == RLA_INDEX_I32 || t == RLA_INDEX_I64; }
 size_t index_size(int32_t t) { return t == RLA_INDEX_I64 ? 8 : 4; }
 
+// `n` rows of `width` bytes, `step` apart.
+struct Bytes {
+  const void* at;
+  size_t width, n = 1, step = 0;
+};
+Bytes rows_of(const void* at, int64_t n, int64_t D, int64_t stride, size_t el) {
+  return {at, (size_t)D * el, (size_t)n, (size_t)stride * el};
+}
+// They meet `out` (one piece).
+bool meet(const Bytes& in, const Bytes& out) {
+  if (in.n <= 1 || in.step == in.width) return overlap(in.at, in.n * in.width, out.at, out.width);
+  if (!in.at || !out.at || out.width == 0) return false;
+  const uintptr_t a = (uintptr_t)in.at, o = (uintptr_t)out.at;
+  const size_t k = o < a + in.width ? 0 : (o - a - in.width) / in.step + 1;   // the first row that ends behind its start
+  return k < in.n && a + k * in.step < o + out.width;
+}
+// No output (one piece each) lies over an input or another output.
+template <size_t N, size_t M> bool apart(const Bytes (&outs)[N], const Bytes (&ins)[M]) {
+  for (size_t i = 0; i < N; ++i) {
+    for (size_t j = 0; j < i; ++j)
+      if (meet(outs[j], outs[i])) return false;
+    for (const Bytes& in : ins)
+      if (meet(in, outs[i])) return false;
+  }
+  return true;
+}
+
 // ---------------------------------------------------------------------------
 // embedding
 // ---------------------------------------------------------------------------
@@ -130,11 +157,13 @@ extern "C" rla_status rla_logprob_forward(const rla_logprob_problem* q, const vo
   if (p.n == 0) return RLA_OK;
   if (!logits || (logprob && !targets) || (p.top > 0 && (!top_logprobs || !top_ids))) return RLA_ERR_NULL_ARG;
   if (!aligned(logits, elem(q->dtype)) || !aligned(targets, index_size(q->index))) return RLA_ERR_VALUE;
-  const size_t in = logits_bytes(q, p), row = 4 * (size_t)p.n;
-  const struct { const void* at; size_t bytes; } outs[] = {
+  const size_t row = 4 * (size_t)p.n;
+  const Bytes ins[] = {{logits, logits_bytes(q, p)}, {logprob ? targets : nullptr, index_size(q->index) * (size_t)p.n}};
+  const Bytes outs[] = {
       {logprob, row}, {lse, row}, {entropy, row}, {p.top ? top_logprobs : nullptr, row * p.top}, {p.top ? top_ids : nullptr, row * p.top}};
-  for (const auto& o : outs)
-    if (!aligned(o.at, 4) || overlap(logits, in, o.at, o.bytes)) return RLA_ERR_VALUE;
+  for (const Bytes& o : outs)
+    if (!aligned(o.at, 4)) return RLA_ERR_VALUE;
+  if (!apart(outs, ins)) return RLA_ERR_VALUE;
   unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
   st = check_workspace(logprob_plan(p, q->dtype == RLA_BF16, ws), workspace, workspace_bytes);
   if (st != RLA_OK) return st;
@@ -238,6 +267,16 @@ rla_status glr_inputs(const rla_glr_problem* q, GlrParams& p, const void* x, con
   p.x = x; p.r = r; p.A = A; p.i = i; p.z = z; p.h0 = h0;
   return RLA_OK;
 }
+// Outputs over nothing that is read, or each other.
+template <size_t N>
+bool glr_apart(const rla_glr_problem* q, const GlrParams& p, const void* dO, const float* dh_final, const Bytes (&outs)[N]) {
+  const size_t el = elem(q->dtype), sbytes = (size_t)p.map.nseq * (size_t)p.D * 4;
+  const Bytes ins[] = {rows_of(p.x, p.map.ntok, p.D, p.xs, el), rows_of(p.r, p.map.ntok, p.D, p.rs, el),
+                       rows_of(p.i, p.map.ntok, p.D, p.is, el), rows_of(p.z, p.map.ntok, p.D, p.zs, el),
+                       rows_of(dO, p.map.ntok, p.D, p.dos, el), {p.A, (size_t)p.D * 4}, {p.h0, sbytes}, {dh_final, sbytes},
+                       {q->cu_seqlens, ((size_t)p.map.nseq + 1) * 4}};
+  return apart(outs, ins);
+}
 size_t state_bytes(const GlrParams& p) { return (size_t)p.map.nseq * (size_t)p.D * 4; }
 
 hipError_t copy_states(const void* from, void* to, size_t bytes, hipStream_t stream) {
@@ -266,6 +305,8 @@ extern "C" rla_status rla_glr_forward(const rla_glr_problem* q, const void* x, c
   const GlrPlan w = plan_glr(q, p, save != 0);
   st = check_workspace(w.total, workspace, workspace_bytes);
   if (st != RLA_OK) return st;
+  const Bytes outs[] = {{o, (size_t)p.map.ntok * p.D * elem(q->dtype)}, {h_final, sbytes}};
+  if (!glr_apart(q, p, nullptr, nullptr, outs)) return RLA_ERR_VALUE;
   hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);
   if (p.map.ntok == 0) return to_status(copy_states(h_init, h_final, sbytes, stream));
   unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
@@ -296,6 +337,10 @@ extern "C" rla_status rla_glr_backward(const rla_glr_problem* q, const void* x, 
   const GlrPlan w = plan_glr(q, p, true);
   st = check_workspace(w.total, workspace, workspace_bytes);
   if (st != RLA_OK) return st;
+  const size_t tbytes = (size_t)p.map.ntok * p.D * el;
+  const Bytes outs[] = {{dx, tbytes}, {dr, tbytes}, {i ? di : nullptr, tbytes}, {z ? dz : nullptr, tbytes},
+                        {dA, (size_t)p.D * 4}, {dh_init, sbytes}};
+  if (!glr_apart(q, p, dO, dh_final, outs)) return RLA_ERR_VALUE;
   hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);
   const bool bf16 = q->dtype == RLA_BF16;
   unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
@@ -328,6 +373,15 @@ extern "C" rla_status rla_glr_decode(const rla_glr_problem* q, const void* x, co
   const size_t sbytes = state_bytes(p);
   if (!aligned(o, elem(q->dtype)) || !aligned(h_out, 4) || (h_in != h_out && overlap(h_in, sbytes, h_out, sbytes)))
     return RLA_ERR_VALUE;
+  // (in place: a thread reads what it writes)
+  GlrParams in = p;
+  if (in.h0 == h_out) in.h0 = nullptr;
+  if (in.x == o && in.xs == p.D) in.x = nullptr;
+  if (in.r == o && in.rs == p.D) in.r = nullptr;
+  if (in.i == o && in.is == p.D) in.i = nullptr;
+  if (in.z == o && in.zs == p.D) in.z = nullptr;
+  const Bytes outs[] = {{o, (size_t)p.map.ntok * p.D * elem(q->dtype)}, {h_out, sbytes}};
+  if (!glr_apart(q, in, nullptr, nullptr, outs)) return RLA_ERR_VALUE;
   p.o = o;
   p.hfin = h_out;
   return to_status(launch_glr_decode(p, q->dtype == RLA_BF16, reinterpret_cast<hipStream_t>(stream)));

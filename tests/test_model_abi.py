@@ -163,3 +163,72 @@ def test_scale_in_base_2(lib):
     for scale, want in ((3e38, VALUE), (2e38, NULL)):
         p = rla.rla_logprob_problem(rows=1, vocab=5, index=1, dtype=rla.RLA_F32, top=0, scale=scale)
         assert lib.rla_logprob_forward(p, None, FAKE, FAKE, None, None, None, None, None, 0, None) == want
+
+
+def overlaps(call, outputs, inputs):
+    """Each output over each input, at its start and its last value, and over each other output: refused.  (All calls
+    here are: none reaches the GPU with these addresses.)"""
+    for out, el in outputs:
+        for other, offset in [(n, o) for n, last in inputs for o in {0, last}] + [(n, 0) for n, _ in outputs if n != out]:
+            assert call(**{out: (other, offset)}) == VALUE, (out, other, offset)
+
+
+def test_glr_overlaps(lib):
+    """Outputs of the recurrence over what it reads, or over each other, strided rows and packed offsets among
+    them."""
+    names = ("x", "r", "A", "i", "z", "h", "dO", "dh", "cu", "o", "f", "dx", "dr", "dA", "di", "dz", "dh0")
+    base = {n: at(k) for k, n in enumerate(names)}
+    tokens, D, S, N = 10, 24, 40, 3
+    last = 2 * ((tokens - 1) * S + D - 1)   # bytes to the last value of strided rows
+
+    def call(which, **over):
+        where = dict(base)
+        for n, (other, offset) in over.items():
+            where[n] = base[other] + offset
+        a = where.__getitem__
+        p = rla.rla_glr_problem(batch=1, seq_len=tokens, channels=D, num_seqs=N, cu_seqlens=a("cu"), x_stride=S, r_stride=S,
+                                i_stride=S, z_stride=S, do_stride=S, normalize=1, dtype=rla.RLA_BF16)
+        ws = (FAKE >> 1, 1 << 40)
+        if which == "forward":
+            return lib.rla_glr_forward(p, a("x"), a("r"), a("A"), a("i"), a("z"), a("h"), a("o"), a("f"), 0, *ws, None)
+        return lib.rla_glr_backward(p, a("x"), a("r"), a("A"), a("i"), a("z"), a("h"), a("dO"), a("dh"), a("dx"), a("dr"),
+                                    a("dA"), a("di"), a("dz"), a("dh0"), 0, *ws, None)
+
+    read = [("x", last), ("r", last), ("i", last), ("z", last), ("A", 4 * (D - 1)), ("h", 4 * (N * D - 1)), ("cu", 4 * N)]
+    overlaps(lambda **o: call("forward", **o), [("o", 2), ("f", 4)], [(n, t & ~3) for n, t in read])
+    overlaps(lambda **o: call("backward", **o), [(n, 4) for n in ("dx", "dr", "dA", "di", "dz", "dh0")],
+             [(n, t & ~3) for n, t in read + [("dO", last), ("dh", 4 * (N * D - 1))]])
+    # from the front: an output that ends in an input's first value
+    assert call("forward", o=("x", 4 - 2 * tokens * D)) == VALUE and call("forward", f=("r", 4 - 4 * N * D)) == VALUE
+
+
+def test_glr_decode_overlaps(lib):
+    B, D = 5, 24
+
+    def call(x=at(0), r=at(1), A=at(2), i=at(3), z=at(4), h=at(5), o=at(6), out=at(7), S=D):
+        p = rla.rla_glr_problem(batch=B, seq_len=1, channels=D, x_stride=S, r_stride=S, i_stride=S, z_stride=S, normalize=1,
+                                dtype=rla.RLA_BF16)
+        return lib.rla_glr_decode(p, x, r, A, i, z, h, o, out, None)
+
+    for k in (0, 1, 3, 4):
+        assert call(o=at(k) + 2) == VALUE and call(o=at(k), S=40) == VALUE and call(out=at(k)) == VALUE
+        assert call(o=at(k) - 2 * B * D + 2) == VALUE
+    for o in (2, 5, 7):
+        assert call(o=at(o)) == VALUE
+    assert call(out=at(2)) == VALUE and call(out=at(5) + 4) == VALUE
+
+
+def test_logprob_overlaps(lib):
+    """Outputs of the log probabilities over the tokens, or over each other."""
+    names = ("y", "lp", "lse", "H", "tl", "ti")
+    base = {n: at(k + 1) for k, n in enumerate(names)}
+    p = rla.rla_logprob_problem(rows=6, vocab=50, index=1, dtype=rla.RLA_F32, top=3, scale=1.0)
+
+    def call(**over):
+        where = dict(base)
+        for n, (other, offset) in over.items():
+            where[n] = base[other] + offset
+        a = where.__getitem__
+        return lib.rla_logprob_forward(p, at(0), a("y"), a("lp"), a("lse"), a("H"), a("tl"), a("ti"), None, 0, None)
+
+    overlaps(call, [(n, 4) for n in names[1:]], [("y", 8 * 6 - 4)])

@@ -276,3 +276,30 @@ def test_refused_gradients(device):
     h = torch.zeros(3, 64, device=device)
     with pytest.raises(rla.RLAError):   # states that overlap in part
         rla.rla_glr_decode(*args, h_in=h[:2], h_out=h[1:])
+
+
+def test_in_place_and_between(device):
+    """Single tokens' outputs over their own inputs; outputs between the rows of an input; an output over an
+    input that others read is refused."""
+    g = torch.Generator(device).manual_seed(1)
+    x, r, i, z = torch.randn(4, 7, 2, 90, device=device, generator=g).unbind(0)
+    A, h = -torch.rand(90, device=device, generator=g), torch.randn(7, 90, device=device, generator=g)
+    want, state = rla.rla_glr_decode(x, r, A, i=i, z=z, h_in=h)
+    for k in range(4):
+        t = [v.clone() for v in (x, r, i, z)]
+        got, end = rla.rla_glr_decode(t[0], t[1], A, i=t[2], z=t[3], h_in=h, out=t[k])
+        assert got is t[k] and torch.equal(got, want) and torch.equal(end, state)
+    wide = torch.zeros(1, 7, 5 * 90 * 7, device=device)
+    wide[..., :90] = x[:, 0]
+    between = wide.view(-1)[90:90 * 8].view(1, 7, 90)
+    r, i = r[:, 0][None].contiguous(), i[:, 0][None].contiguous()
+    want, state = rla.rla_glr_forward(wide[..., :90].contiguous(), r, A, i=i)
+    got, end = rla.rla_glr_forward(wide[..., :90], r, A, i=i, out=between)
+    assert torch.equal(got, want) and torch.equal(end, state)
+    assert torch.equal(rla.rla_glr_decode(wide[..., :90], r, A, i=i, out=between)[0], want)
+    for out in (r, i):
+        with pytest.raises(rla.RLAError):
+            rla.rla_glr_forward(wide[..., :90], r, A, i=i, out=out)
+    grads = rla.rla_glr_backward(x, x, A, x)
+    with pytest.raises(rla.RLAError):
+        rla.rla_glr_backward(x, x, A, x, grads=dict(grads, dx=grads["dr"]))
