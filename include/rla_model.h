@@ -11,7 +11,8 @@
  * asynchronous on `stream`, argument errors returned as an rla_status before any
  * HIP call, no call aborts or throws; token rows contiguous, *_stride elements
  * apart (0: next to each other), every other array contiguous; arrays aligned to
- * their elements, workspaces to 256 bytes; activations fp32 or bf16, rounded
+ * their elements, workspaces to 256 bytes (the size for a problem is enough for one
+ * of fewer tokens or rows, sequences and alternatives, everything else equal); activations fp32 or bf16, rounded
  * once; sums, states and statistics in fp32; outputs overlap neither inputs nor
  * each other, except where an entry point says so; equal calls give equal
  * bits (atomics count tokens, none adds values).

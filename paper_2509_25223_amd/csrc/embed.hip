@@ -570,6 +570,9 @@ size_t embed_plan(EmbedParams& p, int64_t tokens, unsigned char* ws) {
   p.chunk = tokens <= 64 ? 32 : tokens <= 8192 ? 8 : 16;
   while (p.chunk * 4096 < tokens) p.chunk *= 2;
   p.chunks = (int32_t)((tokens + p.chunk - 1) / p.chunk);
+  // Room for as many tiles and chunks as any call of up to this many tokens has: a workspace serves smaller calls too.
+  const int64_t tiles = max((int64_t)p.tiles, min((tokens + kEmbedTile - 1) / kEmbedTile, (int64_t)65536 / kEmbedTile));
+  const int64_t chunks = tokens <= kRankTokens ? p.chunks : max((int64_t)kRankTokens / 8, min((tokens + 15) / 16, (int64_t)4096));
   size_t off = 0;
   auto take = [&](size_t bytes) {
     unsigned char* at = ws + off;
@@ -579,11 +582,11 @@ size_t embed_plan(EmbedParams& p, int64_t tokens, unsigned char* ws) {
   p.present = reinterpret_cast<uint32_t*>(take(4 * (size_t)(p.V / 32 + 1)));
   for (int32_t** a : {&p.key, &p.pos}) *a = reinterpret_cast<int32_t*>(take(4 * (size_t)tokens));
   if (tokens > kRankTokens) {
-    p.count1 = reinterpret_cast<int32_t*>(take(4 * ((size_t)p.tiles << p.bits1)));
-    p.count2 = reinterpret_cast<int32_t*>(take(4 * ((size_t)p.tiles << p.bits2)));
+    p.count1 = reinterpret_cast<int32_t*>(take(4 * ((size_t)tiles << p.bits1)));
+    p.count2 = reinterpret_cast<int32_t*>(take(4 * ((size_t)tiles << p.bits2)));
     for (int32_t** a : {&p.key1, &p.pos1}) *a = reinterpret_cast<int32_t*>(take(4 * (size_t)tokens));
   }
-  p.part = reinterpret_cast<float*>(take(p.chunks < 3 ? 0 : 8 * (size_t)p.chunks * (size_t)p.D));
+  p.part = reinterpret_cast<float*>(take(p.chunks < 3 ? 0 : 8 * (size_t)chunks * (size_t)p.D));
   return off;
 }
 

@@ -682,6 +682,13 @@ void glr_plan(GlrParams& p, bool packed) {
   p.nchunk = (int32_t)n;
   p.tiles = (int32_t)((p.L + tile - 1) / tile);
   if (n <= 1) p.apart = 1;
+  // Room in the workspace for as many as any call of up to this many tokens has, cut this way or that, so that it serves
+  // smaller calls too.  Chunks of a tile or more: `all` at most; whole sequences: fewer than 2 want, since
+  // each >= nseq / want rounded down.  A chunk has up to 1 + all / apart tiles, one of them begun.
+  const int64_t all = (ntok + tile - 1) / tile;
+  p.room_sum = want > 1 && all > 1 ? min(want, all) : 0;
+  p.room_chunks = min(2 * want, all);
+  p.room_tiles = all == 0 ? 0 : all + p.room_chunks + (all + apart - 1) / apart + 2;
 }
 
 int64_t glr_decode_wgs(const GlrParams& p) { return ((p.D + kDecV - 1) / kDecV * p.map.nseq + kThreads - 1) / kThreads; }

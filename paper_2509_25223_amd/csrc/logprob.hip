@@ -698,14 +698,15 @@ size_t logprob_plan(LogprobParams& p, bool bf16, unsigned char* ws) {
   if (p.n * parts < cus) parts = max(parts, min(cus / max(p.n, (int64_t)1), p.V / least));
   p.width = ((p.V + parts - 1) / parts + piece - 1) / piece * piece;
   p.parts = (p.V + p.width - 1) / p.width;
-  if (p.parts == 1) return 0;
+  // Room for as many parts as any call of up to this many rows has: a workspace serves smaller calls too.
+  const int64_t base = (p.V + most - 1) / most, few = max(base, p.V / least);
+  const size_t all = (size_t)max(base > 1 ? p.n * base : 0, few > 1 ? min(cus, p.n * few) : 0);
   size_t off = 0;
   auto take = [&](size_t bytes) {
     unsigned char* at = ws + off;
     off += (bytes + 255) / 256 * 256;
     return at;
   };
-  const size_t all = (size_t)p.n * (size_t)p.parts;
   p.stat = reinterpret_cast<float*>(take(16 * all));
   p.cand_x = reinterpret_cast<float*>(take(4 * all * (size_t)p.top));
   p.cand_i = reinterpret_cast<int32_t*>(take(4 * all * (size_t)p.top));

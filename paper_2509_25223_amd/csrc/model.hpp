@@ -89,6 +89,7 @@ struct GlrParams {
   int64_t L = 0;
   int32_t nchunk = 0, tiles = 0;
   int32_t apart = 0;                   // every chunk starts with a sequence: none needs another's state
+  int64_t room_sum = 0, room_chunks = 0, room_tiles = 0;   // rows of D that the workspace has for sum (two each), pA, ck
   float* sum = nullptr;                // [nchunk][2][D]: a chunk's decay and state from zeros (forward, then backward)
   float* ck = nullptr;                 // [nchunk][tiles][D]: states before the tiles
   float* pA = nullptr;                 // [nchunk][D]

@@ -242,12 +242,12 @@ GlrPlan plan_glr(const rla_glr_problem* q, const GlrParams& p, bool backward) {
     off = up(off + bytes);
     return at;
   };
-  const size_t D = (size_t)p.D, nc = (size_t)p.nchunk;
+  const size_t D = (size_t)p.D;
   if (q->cu_seqlens) w.map = take(token_map_bytes(p.map.ntok, p.map.nseq));
-  if (!p.apart) w.sum = take(8 * nc * D);
+  w.sum = take(8 * (size_t)p.room_sum * D);
   if (backward) {
-    w.ck = take(4 * nc * (size_t)p.tiles * D);
-    w.pA = take(4 * nc * D);
+    w.ck = take(4 * (size_t)p.room_tiles * D);
+    w.pA = take(4 * (size_t)p.room_chunks * D);
   }
   w.total = off;
   return w;

@@ -232,3 +232,28 @@ def test_logprob_overlaps(lib):
         return lib.rla_logprob_forward(p, at(0), a("y"), a("lp"), a("lse"), a("H"), a("tl"), a("ti"), None, 0, None)
 
     overlaps(call, [(n, 4) for n in names[1:]], [("y", 8 * 6 - 4)])
+
+
+def test_workspaces_serve_smaller_calls(lib):
+    """A workspace sized for a call is enough for one of fewer tokens or rows, however each is cut up."""
+    def grows(sizes):
+        return all(a <= b for a, b in zip(sizes, sizes[1:]))
+
+    tokens = sorted({*range(1, 200), *range(8150, 8230), *range(65500, 65570), *range(200, 70000, 333), 1 << 17, 1 << 20, 1 << 22})
+    for V, D in ((50001, 770), (32768, 2048), (100, 3)):
+        assert grows([rla.rla_embed_workspace_size(rla.rla_embed_problem(tokens=n, vocab=V, width=D, index=1, dtype=0,
+                                                                         table_dtype=0, scale=1.0)) for n in tokens])
+    for V in (50000, 65536, 131072, 200003):
+        for dtype in (rla.RLA_F32, rla.RLA_BF16):
+            for top in (0, 8):
+                assert grows([rla.rla_logprob_workspace_size(rla.rla_logprob_problem(rows=n, vocab=V, index=1, dtype=dtype, top=top,
+                                                                                     scale=1.0)) for n in range(0, 600)])
+    for D in (64, 514, 4096, 12800):
+        for op in (rla.RLA_GLR_FORWARD, rla.RLA_GLR_BACKWARD):
+            def size(**kw):
+                return rla.rla_glr_workspace_size(rla.rla_glr_problem(channels=D, normalize=1, dtype=rla.RLA_BF16, **kw), op)
+
+            assert grows([size(batch=1, seq_len=n) for n in tokens])
+            assert grows([size(batch=1, seq_len=n, cu_seqlens=FAKE, num_seqs=5) for n in tokens])
+            for T in (1, 100, 2048, 4096):
+                assert grows([size(batch=b, seq_len=T) for b in range(0, 700)])
