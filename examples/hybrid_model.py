@@ -77,6 +77,7 @@ class Model:
         """(logits, state) of tokens [B, T], or packed [T]; `state`: the one that the
         sequences continue.  With save, also what `gradients` needs."""
         p, n_of = self.p, (lambda s, key: None if s is None else s[key])
+        tokens = tokens.contiguous()   # (slices of a batch)
         x0 = rla.rla_embed_forward(tokens, p["embed"], out_dtype=self.dtype)
         n1, r1 = rla.rla_addnorm_forward(x0, p["norm1"])
         p1 = n1 @ self._cast("w1")
@@ -119,7 +120,8 @@ class Model:
     def decode(self, tokens, state):
         """Logits [B, vocab] of the token behind tokens [B]; `state` moves on in place."""
         p = self.p
-        n1, r = rla.rla_addnorm_forward(rla.rla_embed_forward(tokens[:, None], p["embed"], out_dtype=self.dtype), p["norm1"])
+        x0 = rla.rla_embed_forward(tokens.contiguous()[:, None], p["embed"], out_dtype=self.dtype)
+        n1, r = rla.rla_addnorm_forward(x0, p["norm1"])
         (q, k, v, gate), gates = self._split1(n1 @ self._cast("w1"))
         mixed = []
         for i, t in enumerate((q, k, v)):
@@ -146,6 +148,7 @@ class Model:
             lp = torch.log_softmax(logits, -1)
             p = lp.exp().scatter_add(-1, targets[..., None], torch.full_like(lp[..., :1], -1))
             return -lp.gather(-1, targets[..., None]).mean(), p / targets.numel()
+        logits, targets = logits.contiguous(), targets.contiguous()
         f = rla.rla_logprob_forward(logits, targets)
         up = torch.full_like(f["lse"], -1.0 / targets.numel())
         return -f["logprob"].mean(), rla.rla_logprob_backward(logits, f["lse"], targets, up)
@@ -213,8 +216,8 @@ def train(model, steps, batch=16, length=128, rate=3e-3, seed=1, report=None):
     v = {n: torch.zeros_like(t) for n, t in model.p.items()}
     for i in range(1, steps + 1):
         data = periodic(model.vocab, batch, length + 1, gen).to(model.device)
-        logits, _, saved = model.forward(data[:, :-1].contiguous(), save=True)
-        loss, dlogits = model.loss(logits, data[:, 1:].contiguous())
+        logits, _, saved = model.forward(data[:, :-1], save=True)
+        loss, dlogits = model.loss(logits, data[:, 1:])
         for n, grad in model.gradients(dlogits, saved).items():
             m[n].lerp_(grad, 0.1)
             v[n].lerp_(grad * grad, 0.02)

@@ -88,3 +88,20 @@ def test_training(device):
     losses = hybrid.train(m, 240)
     assert all(torch.isfinite(torch.tensor(losses)))
     assert sum(losses[-5:]) / 5 < 0.5 * losses[0]
+
+
+def test_slices_of_a_batch(device):
+    """Tokens and targets as a training loop has them, slices of one batch: the same as their copies."""
+    m = model(device, torch.float32)
+    data = torch.randint(m.vocab, (3, 41), generator=torch.Generator().manual_seed(4)).to(device)
+    tokens, targets = data[:, :-1], data[:, 1:]
+    logits, state, saved = m.forward(tokens, save=True)
+    want, same, kept = m.forward(tokens.contiguous(), save=True)
+    assert torch.equal(logits, want)
+    loss, grad = m.loss(logits, targets)
+    assert torch.equal(loss, m.loss(logits, targets.contiguous())[0])
+    apart = m.loss(logits.transpose(0, 1), targets.t())[1]
+    assert torch.equal(apart.transpose(0, 1), grad)
+    got, twin = m.gradients(grad, saved), m.gradients(grad, kept)
+    assert all(torch.equal(got[n], twin[n]) for n in got)
+    assert torch.equal(m.decode(data[:, 40], state), m.decode(data[:, 40].contiguous(), same))
