@@ -23,7 +23,8 @@
 //
 // What bounds it: HBM and the vector ALU together.  bf16, both gates, normalized, 4 x 4096 x 4096:
 // forward 178 us (671 MB, 3.8 TB/s; vector ALUs busy 55 % of the time), backward 279 (1.2 GB, 4.3 TB/s),
-// whose 2 channels x 8 tokens x 7 values take 256 registers: two waves a SIMD.  Measured there and not kept:
+// whose 2 channels x 8 tokens x 6 values take 248 registers, with both gates, two waves a SIMD, and what they do not
+// hold lies in LDS, each thread's own (96 KB; fp32 with both gates: all 256, and 24 spilled).  Measured there and not kept:
 // 16 waves a workgroup and loads a tile further ahead (the same time), 16 tokens a stretch (spills), two
 // workgroups a CU of 32 channels each, half lines (forward 205 us, backward 336).
 // Loads behind branches, in turn waited for one by one, had cost three times as much (1283 us, now 447).
@@ -404,6 +405,14 @@ __global__ __launch_bounds__(kGlrThreads, sizeof(T) == 2 ? 4 : 2) void glr_fwd_k
   if (SUMMARY && w.owner) write_pair(p, w.chunk, w.channel, pair);
 }
 
+// A gate's s = sigmoid(z), and 1 - s with all its digits (from s alone it has an error of 6e-8, which for an open
+// gate is most of it: 1e-3 at z = 10, all at 17).
+__device__ __forceinline__ float gate(float z, float& rest) {
+  const float e = __expf(-z), s = __builtin_amdgcn_rcpf(1.f + e);
+  rest = fminf(e * s, 1.f);   // (infinity times 0: 1)
+  return s;
+}
+
 // Computed here, not moved behind what follows.
 __device__ __forceinline__ void here(float& x) { asm volatile("" : "+v"(x)); }
 // Every second token: keeps the scheduler from taking the tokens' independent chains all at once,
@@ -420,6 +429,9 @@ __device__ __forceinline__ void few_registers(int k) {
 template <typename T, bool HAS_I, bool HAS_Z, bool NORM, bool SUMMARY, bool WHOLE>
 __global__ __launch_bounds__(kGlrThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void glr_bwd_kernel(GlrParams p, uint32_t blocks) {
   __shared__ GlrLds fwd, rev;
+  // what a thread has no registers for, two tokens a slot: 1 - s of the gates, the output gate's slope
+  constexpr int kRestI = 1, kSlope = 1 + HAS_I, kParked = SUMMARY ? 0 : 1 + HAS_I + HAS_Z;
+  __shared__ floatx4 parked[kParked ? kParked : 1][kTok / 2][kParked ? kGlrThreads : 1];
   if (blockIdx.x >= blocks * p.nchunk) {
     copy_empty(p, p.dhfin, p.dh0, blockIdx.x - p.nchunk * blocks);
     return;
@@ -454,30 +466,44 @@ __global__ __launch_bounds__(kGlrThreads) __attribute__((amdgpu_waves_per_eu(2, 
       if (!SUMMARY) x.put(q.in, 0.f);
       if (HAS_I && !SUMMARY) i.put(q.in, 0.f);
     }
-    // slope: dO SiLU'(z)
-    float a[kTok][kV], m[kTok][kV], sr[kTok][kV], si[kTok][kV], g[kTok][kV], slope[kTok][kV], h[kV], u[kV];
+    // closed, closed_i: 1 - s of the gates; slope: dO SiLU'(z); of two tokens
+    float a[kTok][kV], m[kTok][kV], sr[kTok][kV], si[kTok][kV], g[kTok][kV], h[kV], u[kV];
     Step own[kV], before[kV], behind[kV];
+    floatx4 closed, closed_i, slope;
+    static_assert(2 * kV == 4, "two tokens a slot");
 #pragma unroll
     for (int k = 0; k < kTok; ++k) {
       few_registers(k);
 #pragma unroll
       for (int e = 0; e < kV; ++e) {
-        sr[k][e] = sigmoid_fast(r.at(k, e));
+        float rest;
+        sr[k][e] = gate(r.at(k, e), rest);
+        if (!SUMMARY) closed[k % 2 * kV + e] = rest;
         decay<NORM && !SUMMARY>(A[e] * kLog2e * sr[k][e], a[k][e], m[k][e]);
-        if (HAS_I && !SUMMARY) si[k][e] = sigmoid_fast(i.at(k, e));
-        else si[k][e] = 1.f;
+        if (HAS_I && !SUMMARY) {
+          si[k][e] = gate(i.at(k, e), rest);
+          closed_i[k % 2 * kV + e] = rest;
+        } else {
+          si[k][e] = 1.f;
+        }
         g[k][e] = d.at(k, e);
         if (HAS_Z) {
           float silu;
-          slope[k][e] = silu_grad_f(z.at(k, e), silu) * g[k][e];
+          slope[k % 2 * kV + e] = silu_grad_f(z.at(k, e), silu) * g[k][e];
           g[k][e] *= silu;
-          here(slope[k][e]);
         }
         here(a[k][e]);
         here(m[k][e]);
         here(sr[k][e]);
         here(g[k][e]);
         if (HAS_I && !SUMMARY) here(si[k][e]);
+      }
+      if constexpr (!SUMMARY) {
+        if (k % 2) {
+          parked[0][k / 2][threadIdx.x] = closed;
+          if constexpr (HAS_I) parked[kRestI][k / 2][threadIdx.x] = closed_i;
+          if constexpr (HAS_Z) parked[kSlope][k / 2][threadIdx.x] = slope;
+        }
       }
     }
     if (n > 0) load(tile - kTile);
@@ -530,19 +556,25 @@ __global__ __launch_bounds__(kGlrThreads) __attribute__((amdgpu_waves_per_eu(2, 
       for (int k = 0; k < kTok; ++k) {
         few_registers(k);
         if (!PLAIN && ((q.starts >> k) & 1u)) w.ch.state(p.h0, q.seq(p, k), p.D, h);
+        if constexpr (HAS_Z)
+          if (k % 2 == 0) slope = parked[kSlope][k / 2][threadIdx.x];
         float dz[kV];
 #pragma unroll
         for (int e = 0; e < kV; ++e) {
           const float b = m[k][e] * si[k][e] * x.at(k, e);
           prev[k][e] = h[e];
           h[e] = __builtin_fmaf(a[k][e], h[e], b);
-          if (HAS_Z) dz[e] = slope[k][e] * h[e];
+          if (HAS_Z) dz[e] = slope[k % 2 * kV + e] * h[e];
         }
         if (HAS_Z && (PLAIN || ((q.there >> k) & 1u))) store_row<T>(p, p.dz, tile, k, w, dz);
       }
 #pragma unroll
       for (int k = kTok - 1; k >= 0; --k) {
         few_registers(k);
+        if (k % 2) {
+          closed = parked[0][k / 2][threadIdx.x];
+          if constexpr (HAS_I) closed_i = parked[kRestI][k / 2][threadIdx.x];
+        }
         if (!PLAIN) {
           if (!((q.there >> k) & 1u)) continue;
           if ((q.ends >> k) & 1u) w.ch.state(p.dhfin, q.seq(p, k), p.D, u);
@@ -560,8 +592,8 @@ __global__ __launch_bounds__(kGlrThreads) __attribute__((amdgpu_waves_per_eu(2, 
           u[e] = a[k][e] * l;
           dlog *= u[e] * sr[k][e];
           dx[e] = into;
-          di[e] = into * x.at(k, e) * (1.f - si[k][e]);
-          dr[e] = dlog * A[e] * (1.f - sr[k][e]);
+          if (HAS_I) di[e] = into * x.at(k, e) * closed_i[k % 2 * kV + e];
+          dr[e] = dlog * A[e] * closed[k % 2 * kV + e];
           dA[e] += dlog;
         }
         store_row<T>(p, p.dx, tile, k, w, dx);

@@ -10,6 +10,7 @@ pytestmark = pytest.mark.gpu
 TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
 ROWS = ("x", "r", "i", "z", "dO")
 INPUTS = ("x", "r", "A", "i", "z", "h0")
+HALF = 2.0 ** -24
 
 
 def make(device, where, D, dtype, opts="izhn", wide=False, seed=0):
@@ -303,3 +304,48 @@ def test_in_place_and_between(device):
     grads = rla.rla_glr_backward(x, x, A, x)
     with pytest.raises(rla.RLAError):
         rla.rla_glr_backward(x, x, A, x, grads=dict(grads, dx=grads["dr"]))
+
+
+@pytest.mark.parametrize("normalize", [True, False])
+@pytest.mark.parametrize("z", [False, True])
+def test_digits_of_gates_and_decays(device, normalize, z):
+    """dr, di and dA of open and closed gates and of slow decays: each value to its own digits, not to those of the
+    largest.  Half steps: an exponential e^-v of a gate 2 |v| + 4 (its argument's two roundings and its own step), so a gate
+    or its complement 2 |v| + 12; a decay and m, which have r's, 8 more; sums of the states' and the messages' parts
+    over four tokens, whose signs differ, count by the parts' sizes; products."""
+    T, D = 4, 4 * 13 * 6
+    gen = torch.Generator().manual_seed(21)
+    A = -torch.tensor([1e-6, 1e-4, 1e-2, 1.0]).repeat_interleave(D // 4)
+    gate = torch.linspace(-30, 30, 13).repeat(D // 13)
+    x, dO, r, i = (torch.randn(1, T, D, generator=gen) for _ in range(4))
+    r = r * 0.1 + gate
+    i = i * 0.1 + gate[torch.randperm(D, generator=gen)]
+    zz = torch.randn(1, T, D, generator=gen) if z else None
+    h0 = torch.randn(1, D, generator=gen)
+    dev = [None if t is None else t.to(device) for t in (x, r, A, dO, i, zz, h0)]
+    got = rla.rla_glr_backward(dev[0], dev[1], dev[2], dev[3], i=dev[4], z=dev[5], normalize=normalize, h0=dev[6])
+    x, r, i, dO = (t[0].double() for t in (x, r, i, dO))
+    A, h0, s = A.double(), h0[0].double(), torch.sigmoid
+    sr, si, cr, ci = s(r), s(i), s(-r), s(-i)
+    log_a = A * sr
+    a, m = torch.exp(log_a), torch.sqrt(-torch.expm1(2 * log_a)) if normalize else torch.ones_like(r)
+    g = dO if zz is None else dO * zz[0].double() * s(zz[0].double())
+    h, size, prev, prev_size = h0, h0.abs(), [], []
+    for t in range(T):
+        prev.append(h)
+        prev_size.append(size)
+        h, size = a[t] * h + m[t] * si[t] * x[t], a[t] * size + m[t] * si[t] * x[t].abs()
+    u, usize, l, lsize = torch.zeros(D).double(), torch.zeros(D).double(), [None] * T, [None] * T
+    for t in reversed(range(T)):
+        l[t], lsize[t] = g[t] + u, g[t].abs() + usize
+        u, usize = a[t] * l[t], a[t] * lsize[t]
+    prev, prev_size, l, lsize = map(torch.stack, (prev, prev_size, l, lsize))
+    curve = si * x * a / m if normalize else torch.zeros_like(x)   # minus dm / d(log a), a factor a taken out
+    dlog, dlog_size = l * a * (prev - curve), lsize * a * (prev_size + curve.abs())
+    steps = HALF * (4 * r.abs().max(0).values + 4 * i.abs().max(0).values + 120)
+    for n, want, size in (("dr", dlog * A * sr * cr, dlog_size * A.abs() * sr * cr),
+                          ("di", l * m * x * si * ci, lsize * m * x.abs() * si * ci),
+                          ("dA", (dlog * sr).sum(0), (dlog_size * sr).sum(0)),
+                          ("dx", l * m * si, lsize * m * si)):
+        off = (got[n].cpu().double().reshape(want.shape) - want).abs() - steps * size
+        assert off.max().item() <= 0, (n, off.max().item(), (off / size).max().item() / HALF)
