@@ -466,8 +466,8 @@ struct RowGradient {
     des = de / s;
     H -= logf(s);   // (what is added to log p)
   }
-  template <typename T, int V, typename Raw>
-  __device__ __forceinline__ void write(T* dx, int col, int width, Raw raw, int nt) const {
+  template <typename T, int V>
+  __device__ __forceinline__ void write(T* dx, int col, int width, const typename RowVec<T, V>::type& raw, int nt) const {
     float d[V];
     if (entropy) {
 #pragma unroll
@@ -530,6 +530,20 @@ void logprob_bwd_kernel(LogprobParams p, int64_t first, int nt) {
 // other row is left to one of its workgroups (in place, others would write what it reads again; not to the
 // first, which for 8 n workgroups a row would all lie on one XCD), and read twice, far out three times.
 constexpr int kLongLanes = 1024;
+// A lane's N pieces from column c0 on, -inf past the row's end (loads without branches: there its last piece).
+template <typename T, int N>
+__device__ __forceinline__ void load_ahead(const T* x, int c0, int width, typename RowVec<T, kPiece<T>>::type (&raw)[N]) {
+  constexpr int V = kPiece<T>, kSpan = kLongLanes * V;
+#pragma unroll
+  for (int u = 0; u < N; ++u) raw[u] = *reinterpret_cast<const typename RowVec<T, V>::type*>(x + min(c0 + u * kSpan, width - V));
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    const int c = c0 + u * kSpan, left = width - c;
+    if (left >= V) continue;
+#pragma unroll
+    for (int e = 0; e < V; ++e) raw[u][e] = e < left ? x[c + e] : from_f<T>(-kInf);
+  }
+}
 template <typename T> constexpr float kTrustedLse = sizeof(T) == 4 ? 32.f : kFarLse;
 template <typename T> __global__ __launch_bounds__(kLongLanes, 8) void logprob_bwd_long_kernel(LogprobParams p, int64_t first, uint32_t segs, int nt) {
   constexpr int L = kLongLanes, V = kPiece<T>, kSpan = L * V, kAhead = 4;
@@ -539,22 +553,9 @@ template <typename T> __global__ __launch_bounds__(kLongLanes, 8) void logprob_b
   const int seg = (int)(id - row * segs), width = (int)p.V, lane = threadIdx.x;
   const T* x = reinterpret_cast<const T*>(p.x) + row * p.xs;
   T* dx = reinterpret_cast<T*>(p.dx) + row * p.V;
-  // the lane's N pieces from column c0 on, -inf past the row's end (loads without branches: there its last piece)
-  auto load = [&](int c0, auto& raw) {
-    constexpr int N = sizeof(raw) / sizeof(Vec);
-#pragma unroll
-    for (int u = 0; u < N; ++u) raw[u] = *reinterpret_cast<const Vec*>(x + min(c0 + u * kSpan, width - V));
-#pragma unroll
-    for (int u = 0; u < N; ++u) {
-      const int c = c0 + u * kSpan, left = width - c;
-      if (left >= V) continue;
-#pragma unroll
-      for (int e = 0; e < V; ++e) raw[u][e] = e < left ? x[c + e] : from_f<T>(-kInf);
-    }
-  };
   Vec raw[1];
   const int own = seg * kSpan + lane * V;
-  load(own, raw);
+  load_ahead<T, 1>(x, own, width, raw);
   RowGradient r(p, row);
   if (!(__builtin_fabsf(r.lse) > kTrustedLse<T>)) {
     r.write<T, V>(dx, own, width, raw[0], nt);
@@ -564,26 +565,26 @@ template <typename T> __global__ __launch_bounds__(kLongLanes, 8) void logprob_b
   auto all = [&](auto f) {
     for (int c0 = lane * V; c0 < width; c0 += kAhead * kSpan) {
       Vec z[kAhead];
-      load(c0, z);
+      load_ahead<T, kAhead>(x, c0, width, z);
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) f(c0 + u * kSpan, z[u]);
     }
   };
   if (r.far) {
     float mx = -kInf;
-    all([&](int, Vec z) {
+    all([&](int, const Vec& z) {
 #pragma unroll
       for (int e = 0; e < V; ++e) mx = fmaxf(mx, to_f<T>(z[e]));
     });
     r.from(over_row<L>(wave_max(mx), slots[0], Max()));
   }
   float s = 0.f;
-  all([&](int, Vec z) {
+  all([&](int, const Vec& z) {
 #pragma unroll
     for (int e = 0; e < V; ++e) s += r.term(to_f<T>(z[e]));
   });
   r.divide(over_row<L>(wave_sum(s), slots[1], Add()));
-  all([&](int c, Vec z) { r.write<T, V>(dx, c, width, z, nt); });
+  all([&](int c, const Vec& z) { r.write<T, V>(dx, c, width, z, nt); });
 }
 
 // ---------------------------------------------------------------------------
