@@ -592,14 +592,13 @@ template <typename T> __global__ __launch_bounds__(kLongLanes, 8) void logprob_b
 // ---------------------------------------------------------------------------
 constexpr int64_t kMaxLanes = (int64_t)1 << 31;   // of a launch
 
-template <typename T, int L, int N> hipError_t forward(const LogprobParams& p, hipStream_t stream) {
+template <typename T, int L, int N, bool TOP> hipError_t forward(const LogprobParams& p, hipStream_t stream) {
   const int64_t sub = L > kThreads ? 1 : kThreads / L, wgs = (p.n * p.parts + sub - 1) / sub;
   const dim3 threads(L > kThreads ? L : kThreads);
   constexpr int64_t most = kMaxLanes / (L > kThreads ? L : kThreads);
   for (int64_t w = 0; w < wgs; w += most) {
     const dim3 grid((uint32_t)min(wgs - w, most));
-    if (p.top) hipLaunchKernelGGL((logprob_fwd_kernel<T, L, N, true>), grid, threads, 0, stream, p, w * sub);
-    else hipLaunchKernelGGL((logprob_fwd_kernel<T, L, N, false>), grid, threads, 0, stream, p, w * sub);
+    hipLaunchKernelGGL((logprob_fwd_kernel<T, L, N, TOP>), grid, threads, 0, stream, p, w * sub);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -610,30 +609,36 @@ template <typename T, int L, int N> hipError_t forward(const LogprobParams& p, h
 // (256 of 16 pieces) 167 (189), with five alternatives 257 (232); 4001 x 49152 with five on 1024 lanes (512
 // of 12) 90 (114).
 constexpr int64_t kFewRows = 512;
-template <typename T, int L> hipError_t forward_pieces(const LogprobParams& p, int64_t n, hipStream_t stream) {
-  if (n <= 1) return forward<T, L, 1>(p, stream);
-  if (n <= 2) return forward<T, L, 2>(p, stream);
-  if constexpr (L == 64) return forward<T, L, 4>(p, stream);
+template <typename T, int L, bool TOP> hipError_t forward_pieces(const LogprobParams& p, int64_t n, hipStream_t stream) {
+  if (n <= 1) return forward<T, L, 1, TOP>(p, stream);
+  if (n <= 2) return forward<T, L, 2, TOP>(p, stream);
+  if constexpr (L == 64) return forward<T, L, 4, TOP>(p, stream);
   else {
-    if (n <= 4) return forward<T, L, 4>(p, stream);
-    if (n <= 5) return forward<T, L, 5>(p, stream);
-    if (n <= 6) return forward<T, L, 6>(p, stream);
-    if (n <= 7) return forward<T, L, 7>(p, stream);
-    if (n <= 8) return forward<T, L, 8>(p, stream);
-    if (n <= 10) return forward<T, L, 10>(p, stream);
-    if (n <= 13) return forward<T, L, 13>(p, stream);
-    return forward<T, L, 16>(p, stream);
+    if (n <= 4) return forward<T, L, 4, TOP>(p, stream);
+    if (n <= 5) return forward<T, L, 5, TOP>(p, stream);
+    if constexpr (L == 256 && !TOP) return forward<T, L, 6, TOP>(p, stream);
+    else {
+      if (n <= 6) return forward<T, L, 6, TOP>(p, stream);
+      if (n <= 7) return forward<T, L, 7, TOP>(p, stream);
+      if (n <= 8) return forward<T, L, 8, TOP>(p, stream);
+      if (n <= 10) return forward<T, L, 10, TOP>(p, stream);
+      if (n <= 13) return forward<T, L, 13, TOP>(p, stream);
+      return forward<T, L, 16, TOP>(p, stream);
+    }
   }
 }
-template <typename T> hipError_t forward(const LogprobParams& p, hipStream_t stream) {
+template <typename T, bool TOP> hipError_t forward_lanes(const LogprobParams& p, hipStream_t stream) {
   constexpr int V = kPiece<T>;
   const int64_t pieces = (p.width + V - 1) / V;
   const bool few = p.n * p.parts <= kFewRows;
-  const int64_t lanes = pieces <= 64 * (few ? 1 : 4) ? 64 : pieces <= 256 * (few ? 1 : p.top ? 16 : 6) ? 256 : 1024;
+  const int64_t lanes = pieces <= 64 * (few ? 1 : 4) ? 64 : pieces <= 256 * (few ? 1 : TOP ? 16 : 6) ? 256 : 1024;
   const int64_t n = (pieces + lanes - 1) / lanes;
-  hipError_t e = lanes == 64    ? forward_pieces<T, 64>(p, n, stream)
-                 : lanes == 256 ? forward_pieces<T, 256>(p, n, stream)
-                                : forward_pieces<T, 1024>(p, n, stream);
+  return lanes == 64    ? forward_pieces<T, 64, TOP>(p, n, stream)
+         : lanes == 256 ? forward_pieces<T, 256, TOP>(p, n, stream)
+                        : forward_pieces<T, 1024, TOP>(p, n, stream);
+}
+template <typename T> hipError_t forward(const LogprobParams& p, hipStream_t stream) {
+  const hipError_t e = p.top ? forward_lanes<T, true>(p, stream) : forward_lanes<T, false>(p, stream);
   if (e != hipSuccess || p.parts == 1) return e;
   const dim3 grid((uint32_t)((p.n + kWaves - 1) / kWaves));
   if (p.top) hipLaunchKernelGGL((logprob_join_kernel<T, true>), grid, dim3(kThreads), 0, stream, p);
