@@ -21,13 +21,13 @@
 // infinities of a sequence stay there).  Too few workgroups: the tokens are cut into chunks, and a
 // pass before leaves each chunk's pair, at the price of reading x, r, i (backward: r, dO, z) twice.
 //
-// What bounds it: HBM and the vector ALU together.  bf16, both gates, normalized, 4 x 4096 x 4096:
-// forward 178 us (671 MB, 3.8 TB/s; vector ALUs busy 55 % of the time), backward 279 (1.2 GB, 4.3 TB/s),
-// whose 2 channels x 8 tokens x 6 values take 248 registers, with both gates, two waves a SIMD, and what they do not
-// hold lies in LDS, each thread's own (96 KB; fp32 with both gates: all 256, and 24 spilled).  Measured there and not kept:
-// 16 waves a workgroup and loads a tile further ahead (the same time), 16 tokens a stretch (spills), two
-// workgroups a CU of 32 channels each, half lines (forward 205 us, backward 336).
-// Loads behind branches, in turn waited for one by one, had cost three times as much (1283 us, now 447).
+// What bounds it: HBM and the vector ALU together.  bf16, both gates, normalized, 4 x 4096 x 4096: forward 168 to
+// 184 us from card to card (671 MB, 3.6 to 4.0 TB/s; vector ALUs busy 53 % of the time), backward 282 to 290 (1.2 GB,
+// 4.2 TB/s, 56 %).  Its 2 channels x 8 tokens x 6 values take 252 registers with both gates, two waves a SIMD; what they do
+// not hold lies in LDS, each thread's own (96 KB).  fp32 with both gates spills 30 of them (116 bytes a lane), the bf16
+// forward with both gates 2.  Measured there and not kept: 16 waves a workgroup and loads a tile further ahead (the same
+// time), 16 tokens a stretch (spills), two workgroups a CU of 32 channels each, half lines (forward 205 us, backward 336).
+// Loads behind branches, in turn waited for one by one, had cost three times as much (1283 us, now 455).
 #include <math.h>
 
 #include "model.hpp"
@@ -409,7 +409,7 @@ __global__ __launch_bounds__(kGlrThreads, sizeof(T) == 2 ? 4 : 2) void glr_fwd_k
 // gate is most of it: 1e-3 at z = 10, all at 17).
 __device__ __forceinline__ float gate(float z, float& rest) {
   const float e = __expf(-z), s = __builtin_amdgcn_rcpf(1.f + e);
-  rest = fminf(e * s, 1.f);   // (infinity times 0: 1)
+  rest = __builtin_amdgcn_fmed3f(e * s, 0.f, 1.f);   // (infinity times 0: 0, and s is a factor of all that it is used for)
   return s;
 }
 
@@ -429,8 +429,10 @@ __device__ __forceinline__ void few_registers(int k) {
 template <typename T, bool HAS_I, bool HAS_Z, bool NORM, bool SUMMARY, bool WHOLE>
 __global__ __launch_bounds__(kGlrThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void glr_bwd_kernel(GlrParams p, uint32_t blocks) {
   __shared__ GlrLds fwd, rev;
-  // what a thread has no registers for, two tokens a slot: 1 - s of the gates, the output gate's slope
-  constexpr int kRestI = 1, kSlope = 1 + HAS_I, kParked = SUMMARY ? 0 : 1 + HAS_I + HAS_Z;
+  // What a thread has no registers for, two tokens a slot: 1 - s of the gates and, with both, r's s, read where the
+  // gradients are written (the output gate's slope instead of s, read right behind the barrier: 296 us, not 286).
+  constexpr bool kParkS = HAS_I && HAS_Z;
+  constexpr int kRestI = 1, kS = 2, kParked = SUMMARY ? 0 : 1 + HAS_I + kParkS;
   __shared__ floatx4 parked[kParked ? kParked : 1][kTok / 2][kParked ? kGlrThreads : 1];
   if (blockIdx.x >= blocks * p.nchunk) {
     copy_empty(p, p.dhfin, p.dh0, blockIdx.x - p.nchunk * blocks);
@@ -466,10 +468,10 @@ __global__ __launch_bounds__(kGlrThreads) __attribute__((amdgpu_waves_per_eu(2, 
       if (!SUMMARY) x.put(q.in, 0.f);
       if (HAS_I && !SUMMARY) i.put(q.in, 0.f);
     }
-    // closed, closed_i: 1 - s of the gates; slope: dO SiLU'(z); of two tokens
-    float a[kTok][kV], m[kTok][kV], sr[kTok][kV], si[kTok][kV], g[kTok][kV], h[kV], u[kV];
+    // closed, closed_i: 1 - s of the gates, of two tokens; slope: dO SiLU'(z)
+    float a[kTok][kV], m[kTok][kV], sr[kTok][kV], si[kTok][kV], g[kTok][kV], slope[kTok][kV], h[kV], u[kV];
     Step own[kV], before[kV], behind[kV];
-    floatx4 closed, closed_i, slope;
+    floatx4 closed, closed_i;
     static_assert(2 * kV == 4, "two tokens a slot");
 #pragma unroll
     for (int k = 0; k < kTok; ++k) {
@@ -489,8 +491,9 @@ __global__ __launch_bounds__(kGlrThreads) __attribute__((amdgpu_waves_per_eu(2, 
         g[k][e] = d.at(k, e);
         if (HAS_Z) {
           float silu;
-          slope[k % 2 * kV + e] = silu_grad_f(z.at(k, e), silu) * g[k][e];
+          slope[k][e] = silu_grad_f(z.at(k, e), silu) * g[k][e];
           g[k][e] *= silu;
+          here(slope[k][e]);
         }
         here(a[k][e]);
         here(m[k][e]);
@@ -502,7 +505,7 @@ __global__ __launch_bounds__(kGlrThreads) __attribute__((amdgpu_waves_per_eu(2, 
         if (k % 2) {
           parked[0][k / 2][threadIdx.x] = closed;
           if constexpr (HAS_I) parked[kRestI][k / 2][threadIdx.x] = closed_i;
-          if constexpr (HAS_Z) parked[kSlope][k / 2][threadIdx.x] = slope;
+          if constexpr (kParkS) parked[kS][k / 2][threadIdx.x] = floatx4{sr[k - 1][0], sr[k - 1][1], sr[k][0], sr[k][1]};
         }
       }
     }
@@ -556,25 +559,29 @@ __global__ __launch_bounds__(kGlrThreads) __attribute__((amdgpu_waves_per_eu(2, 
       for (int k = 0; k < kTok; ++k) {
         few_registers(k);
         if (!PLAIN && ((q.starts >> k) & 1u)) w.ch.state(p.h0, q.seq(p, k), p.D, h);
-        if constexpr (HAS_Z)
-          if (k % 2 == 0) slope = parked[kSlope][k / 2][threadIdx.x];
         float dz[kV];
 #pragma unroll
         for (int e = 0; e < kV; ++e) {
           const float b = m[k][e] * si[k][e] * x.at(k, e);
           prev[k][e] = h[e];
           h[e] = __builtin_fmaf(a[k][e], h[e], b);
-          if (HAS_Z) dz[e] = slope[k % 2 * kV + e] * h[e];
+          if (HAS_Z) dz[e] = slope[k][e] * h[e];
         }
         if (HAS_Z && (PLAIN || ((q.there >> k) & 1u))) store_row<T>(p, p.dz, tile, k, w, dz);
       }
 #pragma unroll
       for (int k = kTok - 1; k >= 0; --k) {
         few_registers(k);
-        if (k % 2) {
-          closed = parked[0][k / 2][threadIdx.x];
-          if constexpr (HAS_I) closed_i = parked[kRestI][k / 2][threadIdx.x];
-        }
+        if constexpr (!SUMMARY)
+          if (k % 2) {
+            closed = parked[0][k / 2][threadIdx.x];
+            if constexpr (kParkS) {
+              const floatx4 s = parked[kS][k / 2][threadIdx.x];
+#pragma unroll
+              for (int e = 0; e < kV; ++e) sr[k - 1][e] = s[e], sr[k][e] = s[kV + e];
+            }
+            if constexpr (HAS_I) closed_i = parked[kRestI][k / 2][threadIdx.x];
+          }
         if (!PLAIN) {
           if (!((q.there >> k) & 1u)) continue;
           if ((q.ends >> k) & 1u) w.ch.state(p.dhfin, q.seq(p, k), p.D, u);
