@@ -17,8 +17,8 @@
 //                 that start there and end there or in the next chunk; of longer runs
 //                 each chunk leaves its part (few tokens: others write the rows without one)
 //   embed_join    adds these parts
-// 16384 tokens as frequent as words, 32768 x 2048, bf16 rows into an fp32 table, us: 4.7, 8.9, 43.7 (224 MB of
-// zeros at 5.1 TB/s, the second pass beside them), 27 (67 MB read at random, 45 written), 6.3; all bytes
+// 16384 tokens as frequent as words, 32768 x 2048, bf16 rows into an fp32 table, us: 4.6, 10.0, 42.0 (224 MB of
+// zeros at 5.3 TB/s, the second pass beside them), 26 (67 MB read at random, 45 written), 6.2; all bytes
 // at 5.0 TB/s would take 67.  Few tokens of a narrow table are bound by the launches, two to three.
 #include "model.hpp"
 
@@ -41,7 +41,7 @@ __device__ __forceinline__ uint32_t key_of(const EmbedParams& p, int64_t t) {
 }
 
 // ---------------------------------------------------------------------------
-// lookup: a thread a piece of a row (16384 rows of 2048, fp32 to bf16: 23.6 us; 256 of bf16: 3.0)
+// lookup: a thread a piece of a row (16384 rows of 2048, fp32 to bf16: 24.1 us; 256 of bf16: 2.8)
 // ---------------------------------------------------------------------------
 template <typename X, typename T, bool FULL, bool NT>
 __global__ __launch_bounds__(kThreads) void embed_fwd_kernel(EmbedParams p, uint32_t pieces, uint32_t count) {
@@ -183,7 +183,7 @@ __device__ __forceinline__ void sort_tile(const EmbedParams& p, int tile, int32_
       p.key1[to] = (int32_t)k;
       p.pos1[to] = pos[j];
       // one lane for all of a key (and of a tile that they land in: two at most), or a frequent id's tokens
-      // wait for each other (16384 tokens, 10 % of one id: 17 us, now 9)
+      // wait for each other (16384 tokens, 10 % of one id: 17 us, now 10)
       uint64_t equal = same;
       for (int b = 0; b < p.bits2; ++b) {
         const uint32_t bit = k >> (p.bits1 + b) & 1u;

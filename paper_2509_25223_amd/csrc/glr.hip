@@ -22,8 +22,8 @@
 // pass before leaves each chunk's pair, at the price of reading x, r, i (backward: r, dO, z) twice.
 //
 // What bounds it: HBM and the vector ALU together.  bf16, both gates, normalized, 4 x 4096 x 4096: forward 168 to
-// 184 us from card to card (671 MB, 3.6 to 4.0 TB/s; vector ALUs busy 53 % of the time), backward 282 to 290 (1.2 GB,
-// 4.2 TB/s, 56 %).  Its 2 channels x 8 tokens x 6 values take 252 registers with both gates, two waves a SIMD; what they do
+// 184 us from card to card (671 MB, 3.6 to 4.0 TB/s; vector ALUs at work 54 % of the time), backward 280 to 296 (1.2 GB,
+// 4.2 TB/s, 57 %).  Its 2 channels x 8 tokens x 6 values take 252 registers with both gates, two waves a SIMD; what they do
 // not hold lies in LDS, each thread's own (96 KB).  fp32 with both gates spills 30 of them (116 bytes a lane), the bf16
 // forward with both gates 2.  Measured there and not kept: 16 waves a workgroup and loads a tile further ahead (the same
 // time), 16 tokens a stretch (spills), two workgroups a CU of 32 channels each, half lines (forward 205 us, backward 336).
@@ -634,8 +634,8 @@ __global__ __launch_bounds__(kGlrThreads) __attribute__((amdgpu_waves_per_eu(2, 
 }
 
 // Single tokens: a thread owns 4 channels of a sequence, whose state it reads before it
-// writes (in place works: a row's last piece is its own, in part).  256 x 4096, bf16: 5.3 us for 18.9 MB, in
-// most part a launch and one trip to memory.
+// writes (in place works: a row's last piece is its own, in part).  256 x 4096, bf16: 5.2 us for 18.9 MB, in
+// most part a launch and one trip to memory; 5 and 8 tokens at once 11.8 and 16.1, what 61 and 92 MB take.
 constexpr int kDecV = 4;
 template <typename T, bool HAS_I, bool HAS_Z, bool NORM, bool FULL>
 __global__ __launch_bounds__(kThreads) void glr_decode_kernel(GlrParams p, uint32_t pieces, uint32_t count) {
@@ -703,8 +703,8 @@ void glr_plan(GlrParams& p, bool packed) {
   const int64_t blocks = blocks_of(p), ntok = p.map.ntok;
   constexpr int64_t tile = kTile;
   // Whole sequences where they give every CU a workgroup: then no pass before is needed.  Else chunks, for two
-  // workgroups a CU (16384 x 2048: 124 us, one a CU 139; 4 sequences of 4096 x 4096 with gradients 447, cut in
-  // two each 775).
+  // workgroups a CU (16384 x 2048: 124 us, one a CU 139).  4096 x 4096 with gradients, us: 1 to 3 sequences, cut, 190, 341,
+  // 509; 4, whole, 441 (cut in two each 775); 5 and 8, whole, in a second round of workgroups, 736 and 925.
   constexpr int64_t cus = 256;
   const int64_t apart = max((int64_t)1, cus / blocks), want = max((int64_t)1, 2 * cus / blocks);
   p.apart = 0;

@@ -5,10 +5,10 @@
 // A row is read once, into registers: with its largest value mx known, the sums are of 2^((x - mx) k),
 // k = scale log2 e, and of these times (x - mx) k.  A row longer than the registers of a
 // workgroup hold, or one of few rows, is read in parts by several, each leaving its largest
-// value, sums and alternatives, which logprob_join merges.  Many rows are bound by HBM (16384 x 32768
-// of bf16: 174 us for 1.07 GB, 6.2 TB/s; 4001 x 50001 with five alternatives 109 us, 3.7 TB/s, where
-// the search costs each wave some 30 us), few by latency (one of 32768 in fp32 with twenty alternatives: 9.9 us; 64 of
-// 131072 with eight: 9.7, and 6.1 to join them).  All sums are fp32, in one order.
+// value, sums and alternatives, which logprob_join merges.  Many rows are bound by HBM and the vector ALU
+// (16384 x 32768 of bf16: 176 us for 1.07 GB, 6.1 TB/s, the ALUs at work 93 % of the time; 4001 x 50001 96 us, 4.2 TB/s,
+// 106 with five alternatives), few by latency (one of 32768 in fp32 with twenty alternatives: 10.1 us; 64 of
+// 131072 with eight: 10.9, and 6.2 to join them).  All sums are fp32, in one order.
 //
 // Alternatives: values are compared as whole numbers in their order (0: none, -inf or NaN).
 // Of a wave's 64 lanes' largest values the q-th is a bound that q values of the wave reach (its upper
