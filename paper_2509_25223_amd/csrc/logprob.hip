@@ -664,8 +664,8 @@ template <typename T, int L, int N> hipError_t backward(const LogprobParams& p, 
 }
 // Lanes of a row, as many as hold it in registers for two rows of 1024 on a CU (fp32: 20480 logits, bf16: 40960); of
 // few rows more, for latency.  us: 16384 x 32768 of bf16 415 (2.15 GB, the 5.2 TB/s of a large copy), rows at 400 422;
-// 3000 x 20003 of fp32 76 and 77.  Longer: 4001 x 50001 of bf16 157, at 400 309; 2000 x 151936 of fp32 387, at 100 665, at
-// 400 816; 1 x 131072 of fp32 2.4, 18, 22.
+// 3000 x 20003 of fp32 76 and 77.  Longer: 4001 x 50001 of bf16 145, at 400 309; 2000 x 151936 of fp32 396, at 100 665, at
+// 400 816; 1 x 131072 of fp32 2.3, 18, 22.
 template <typename T> hipError_t backward(const LogprobParams& p, hipStream_t stream) {
   const int64_t pieces = (p.V + kPiece<T> - 1) / kPiece<T>;
   const int nt = p.n * p.V * (int64_t)sizeof(T) > kNtBytes;

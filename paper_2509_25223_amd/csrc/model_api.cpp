@@ -165,7 +165,8 @@ extern "C" rla_status rla_logprob_forward(const rla_logprob_problem* q, const vo
     if (!aligned(o.at, 4)) return RLA_ERR_VALUE;
   if (!apart(outs, ins)) return RLA_ERR_VALUE;
   unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
-  st = check_workspace(logprob_plan(p, q->dtype == RLA_BF16, ws), workspace, workspace_bytes);
+  const size_t size = logprob_plan(p, q->dtype == RLA_BF16, ws);
+  st = check_workspace(p.parts == 1 ? 0 : size, workspace, workspace_bytes);
   if (st != RLA_OK) return st;
   p.x = logits;
   p.targets.p = targets;
@@ -233,6 +234,7 @@ rla_status check_glr_scan(const rla_glr_problem* q, GlrParams& p) {
 
 struct GlrPlan {
   size_t map = 0, sum = 0, ck = 0, pA = 0, total = 0;
+  size_t used = 0;   // by this call: as far as its own cut needs the room
 };
 GlrPlan plan_glr(const rla_glr_problem* q, const GlrParams& p, bool backward) {
   GlrPlan w;
@@ -243,11 +245,16 @@ GlrPlan plan_glr(const rla_glr_problem* q, const GlrParams& p, bool backward) {
     return at;
   };
   const size_t D = (size_t)p.D;
-  if (q->cu_seqlens) w.map = take(token_map_bytes(p.map.ntok, p.map.nseq));
+  if (q->cu_seqlens) {
+    w.map = take(token_map_bytes(p.map.ntok, p.map.nseq));
+    w.used = off;
+  }
   w.sum = take(8 * (size_t)p.room_sum * D);
+  if (!p.apart) w.used = off;
   if (backward) {
     w.ck = take(4 * (size_t)p.room_tiles * D);
     w.pA = take(4 * (size_t)p.room_chunks * D);
+    w.used = off;
   }
   w.total = off;
   return w;
@@ -303,7 +310,7 @@ extern "C" rla_status rla_glr_forward(const rla_glr_problem* q, const void* x, c
   const size_t sbytes = state_bytes(p);
   if (!aligned(o, elem(q->dtype)) || !aligned(h_final, 4) || overlap(h_init, sbytes, h_final, sbytes)) return RLA_ERR_VALUE;
   const GlrPlan w = plan_glr(q, p, save != 0);
-  st = check_workspace(w.total, workspace, workspace_bytes);
+  st = check_workspace(w.used, workspace, workspace_bytes);
   if (st != RLA_OK) return st;
   const Bytes outs[] = {{o, (size_t)p.map.ntok * p.D * elem(q->dtype)}, {h_final, sbytes}};
   if (!glr_apart(q, p, nullptr, nullptr, outs)) return RLA_ERR_VALUE;

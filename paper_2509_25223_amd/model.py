@@ -8,7 +8,8 @@ Activations are bf16 or fp32; their rows may lie further apart than they are wid
 every other tensor is contiguous.  Token ids are int64 or int32.  Parameters,
 their gradients, states and statistics are fp32 (an embedding table may be bf16).
 Outputs and workspaces are allocated (on `stream`, if given) unless passed
-in.  A call runs on its tensors' GPU, whichever is the current one; a stream has
+in; a workspace sized for a call serves smaller ones, and outputs lie over no inputs
+but where a function says so.  A call runs on its tensors' GPU, whichever is the current one; a stream has
 to be that GPU's.
 """
 from __future__ import annotations
@@ -368,7 +369,7 @@ def rla_glr_backward(x, r, A, dO, i=None, z=None, normalize=True, h0=None, dh_fi
 
 def rla_glr_decode(x, r, A, i=None, z=None, normalize=True, h_in=None, h_out=None, out=None, stream=None):
     """A few new tokens x [B, T, D] onto the states h_in [B, D] (None: zeros).
-    Returns (o, h_out); h_out=h_in updates in place."""
+    Returns (o, h_out); h_out=h_in updates in place, and out may be x, r, i or z."""
     _lib()
     if x is not None and x.dim() != 3:
         raise ValueError("x must be [B, T, D]")

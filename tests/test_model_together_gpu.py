@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2509_25223_amd as rla
+from paper_2509_25223_amd import model
 from tests import layer_reference as lref
 from tests import model_reference as ref
 
@@ -308,3 +309,25 @@ def test_more_rows_than_a_launch(device):
     out = rla.rla_embed_forward(ids, table)
     some = torch.tensor([0, (1 << 23) - 1, 1 << 23, n - 1], device=device)
     assert torch.equal(out[some], table[ids[some]])
+
+
+def test_calls_that_use_no_workspace(device):
+    """Rows that a workgroup takes each, and whole sequences, need none from the caller, whatever room smaller calls
+    have in one that is sized for them."""
+    lib = model._lib()
+    x = torch.randn(300, 65536, device=device)
+    y = torch.zeros(300, dtype=torch.int64, device=device)
+    problem = rla.make_logprob_problem(x)
+    assert rla.rla_logprob_workspace_size(problem) > 0
+    out, lse = torch.empty(2, 300, device=device)
+    stream = torch.cuda.current_stream().cuda_stream
+    assert lib.rla_logprob_forward(problem, x.data_ptr(), y.data_ptr(), out.data_ptr(), lse.data_ptr(), None, None, None, None, 0,
+                                   stream) == 0
+    want = rla.rla_logprob_forward(x, y)
+    assert torch.equal(out, want["logprob"]) and torch.equal(lse, want["lse"])
+    u, A = torch.randn(256, 30, 64, device=device), -torch.rand(64, device=device)
+    problem, o = rla.make_glr_problem(u), torch.empty_like(u)
+    assert rla.rla_glr_workspace_size(problem, rla.RLA_GLR_FORWARD) > 0
+    assert lib.rla_glr_forward(problem, u.data_ptr(), u.data_ptr(), A.data_ptr(), None, None, None, o.data_ptr(), None, 0, None, 0,
+                               stream) == 0
+    assert torch.equal(o, rla.rla_glr_forward(u, u, A)[0])
