@@ -679,12 +679,13 @@ template <typename T> hipError_t backward(const LogprobParams& p, hipStream_t st
   if (!few && pieces <= 1536) return backward<T, 256, 6>(p, nt, stream);
   // (a few rows of bf16, whose digits are the outputs': sooner done by several workgroups each, 1 x 32768 2.7, not 4.7)
   if (!few || sizeof(T) == 4) {
+    const int64_t n = (pieces + 1023) / 1024;
     if constexpr (sizeof(T) == 4)
-      if (pieces <= 1024) return backward<T, 1024, 1>(p, nt, stream);
-    if (pieces <= 2048) return backward<T, 1024, 2>(p, nt, stream);
-    if (pieces <= 3072) return backward<T, 1024, 3>(p, nt, stream);
-    if (pieces <= 4096) return backward<T, 1024, 4>(p, nt, stream);
-    if (pieces <= 5120) return backward<T, 1024, 5>(p, nt, stream);
+      if (n <= 1) return backward<T, 1024, 1>(p, nt, stream);
+    if (n <= 2) return backward<T, 1024, 2>(p, nt, stream);
+    if (n <= 3) return backward<T, 1024, 3>(p, nt, stream);
+    if (n <= 4) return backward<T, 1024, 4>(p, nt, stream);
+    if (n <= 5) return backward<T, 1024, 5>(p, nt, stream);
   }
   constexpr int64_t span = kLongLanes * kPiece<T>;
   const int64_t segs = (p.V + span - 1) / span;
